@@ -44,7 +44,8 @@
  *  - A query at logical position a sees keys 0..a (causal, bottom-right).
  *  - Supported: block_size 16, head_dim 64 or 128, num_q_heads a multiple of
  *    num_kv_heads; dtype PA_BF16 (MFMA path, float32 accumulation) or PA_F32
- *    (float32 throughout).  Integers are int32; num_blocks * block_size must
+ *    (float32 throughout).  The pa_kv8_* calls work on an 8-bit cache whose
+ *    layout is given there.  Integers are int32; num_blocks * block_size must
  *    be below 2^31.
  *  - Not thread-safe per pool; device calls on one stream are ordered.
  */
@@ -67,7 +68,11 @@ typedef enum {
   PA_ERR_LAUNCH = -5        /* the HIP runtime rejected a launch                */
 } pa_status;
 
-typedef enum { PA_F32 = 0, PA_BF16 = 1 } pa_dtype;
+typedef enum {
+  PA_F32 = 0,
+  PA_BF16 = 1,
+  PA_BF16_KV8 = 2 /* launch plans only: bf16 queries over the 8-bit cache */
+} pa_dtype;
 
 /* Message describing the calling thread's most recent error ("" if none). */
 const char* pa_last_error(void);
@@ -462,6 +467,135 @@ int pa_attn_decode_noalloc(const void* q, const void* k_cache, const void* v_cac
                            int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
                            int32_t block_size, float scale, int32_t dtype, int32_t* plan,
                            const pa_plan_info* info, void* out, float* lse, void* stream);
+
+/* ------------------------------------------------------------------------ *
+ * The 8-bit cache (paper: Section 2 and Section 6, Table "playbook": KV      *
+ * memory bounds how many requests fit and how fast decode streams it).       *
+ * ------------------------------------------------------------------------ */
+
+/* A cache of half the bf16 cache's bytes, over the same blocks, block tables
+ * and pool:
+ *   k_cache[num_blocks][num_kv_heads][head_dim/64][16][64]   bytes
+ *   v_cache[num_blocks][num_kv_heads][head_dim][16]          bytes
+ *   scales[num_blocks][num_kv_heads][2]                      bytes
+ * Key dim d of the token at offset o is k_cache[block][h][d/64][o][d%64], value
+ * dim d v_cache[block][h][d][o]: e4m3 codes (1 sign, 4 exponent, 3 mantissa
+ * bits, largest finite value 448, no infinities).  scales[block][h][0] is the
+ * keys' scale, [1] the values': the power of two 2^e as the byte e + 127, e of
+ * -100 .. 120.  A code c stands for c * 2^e, which bf16 and float32 hold exactly
+ * (beyond bf16's largest value: infinity).
+ *
+ * Storing: a block's e is the smallest with amax <= 448 * 2^e, amax the largest
+ * finite magnitude among its new tokens' keys (values) of that kv-head; where
+ * the block holds earlier tokens of the sequence, the larger of that and the
+ * block's e, and where e grew the earlier tokens' codes are rounded again (the
+ * shift is by a power of two, so a code only loses bits below 2^(e-9)).  A code
+ * is x / 2^e rounded to nearest even; infinities and NaN are stored as NaN.
+ * e does not shrink while a block fills: tokens rolled back (pa_seq_truncate)
+ * may leave it larger than the rest needs.
+ *
+ * The calls below find rows by the launch's metadata, as pa_build_metadata
+ * writes it: rows cu_seqlens[r] .. cu_seqlens[r+1]-1 are sequence r's last
+ * positions.  Sequences without rows are skipped.  A block that gets new
+ * tokens must be in one sequence's table only (pool blocks are). */
+
+/* Quantise the keys/values of n_tokens new tokens into the cache.
+ * k_new, v_new: n_tokens rows of [num_kv_heads][head_dim] (dtype PA_BF16 or
+ * PA_F32), k_stride and v_stride elements apart (rows of a larger matrix, such
+ * as a projection's output, need no copy).  n_tokens = cu_seqlens[n_seqs]; rows
+ * past it, positions past the table's width or below zero and block ids outside
+ * [0, num_blocks) are skipped.  Slots behind a sequence's last token keep their
+ * bytes.  All pointers are caller-owned device memory; asynchronous on stream;
+ * allocates nothing.  The result depends on the order of appends to a block (as
+ * said above), not on the launch.  Errors: PA_ERR_ARG (NULL pointer with rows to
+ * store, negative size, a row stride below num_kv_heads * head_dim, rows or
+ * caches not 16-byte aligned), PA_ERR_UNSUPPORTED (head_dim, block_size, dtype),
+ * PA_ERR_LAUNCH. */
+int pa_kv8_append(const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+                  const int32_t* block_table, int32_t max_blocks_per_seq, const int32_t* seq_lens,
+                  const int32_t* cu_seqlens, int32_t n_seqs, int32_t n_tokens, void* k_cache,
+                  void* v_cache, uint8_t* scales, int32_t num_blocks, int32_t num_kv_heads,
+                  int32_t head_dim, int32_t block_size, int32_t dtype, void* stream);
+
+/* Read tokens back as rows, the inverse of pa_kv8_append with the same
+ * arguments: rows cu_seqlens[r] .. cu_seqlens[r+1]-1 of k_out and v_out receive
+ * sequence r's last positions (a whole context with cu_seqlens summing
+ * seq_lens), each value c * 2^e exactly, in dtype.  Rows that pa_kv8_append
+ * would skip, and what lies between rows, are left as they were.  Errors as
+ * pa_kv8_append. */
+int pa_kv8_read(void* k_out, int64_t k_stride, void* v_out, int64_t v_stride,
+                const int32_t* block_table, int32_t max_blocks_per_seq, const int32_t* seq_lens,
+                const int32_t* cu_seqlens, int32_t n_seqs, int32_t n_tokens, const void* k_cache,
+                const void* v_cache, const uint8_t* scales, int32_t num_blocks,
+                int32_t num_kv_heads, int32_t head_dim, int32_t block_size, int32_t dtype,
+                void* stream);
+
+/* Attention over the 8-bit cache: pa_attn_prefill, pa_attn_decode,
+ * pa_attn_verify and pa_attn_decode_noalloc with bf16 queries and outputs, k_t
+ * and v_t the values that the codes stand for.  Plans are built with dtype
+ * PA_BF16_KV8 (pa_attn_plan, pa_prepare_launch; the workspace bounds hold for
+ * them too).  Arguments, layouts, ownership and errors as for those calls; q,
+ * out and the caches must be 16-byte aligned (PA_ERR_ARG). */
+int pa_kv8_attn_prefill(const void* q, const void* k_cache, const void* v_cache,
+                        const uint8_t* scales, int32_t num_blocks, const int32_t* block_table,
+                        int32_t max_blocks_per_seq, const int32_t* seq_lens,
+                        const int32_t* cu_seqlens_q, int32_t n_seqs, int32_t total_q,
+                        int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                        int32_t block_size, float scale, int32_t* plan, const pa_plan_info* info,
+                        void* workspace, size_t workspace_bytes, void* out, float* lse,
+                        void* stream);
+int pa_kv8_attn_decode(const void* q, const void* k_cache, const void* v_cache,
+                       const uint8_t* scales, int32_t num_blocks, const int32_t* block_table,
+                       int32_t max_blocks_per_seq, const int32_t* seq_lens,
+                       const int32_t* cu_seqlens_q, int32_t n_seqs, int32_t total_q,
+                       int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                       int32_t block_size, float scale, int32_t* plan, const pa_plan_info* info,
+                       void* workspace, size_t workspace_bytes, void* out, float* lse,
+                       void* stream);
+int pa_kv8_attn_verify(const void* q, const void* k_cache, const void* v_cache,
+                       const uint8_t* scales, int32_t num_blocks, const int32_t* block_table,
+                       int32_t max_blocks_per_seq, const int32_t* seq_lens,
+                       const int32_t* cu_seqlens_q, int32_t n_seqs, int32_t total_q,
+                       int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                       int32_t block_size, float scale, int32_t* plan, const pa_plan_info* info,
+                       void* workspace, size_t workspace_bytes, void* out, float* lse,
+                       void* stream);
+int pa_kv8_attn_decode_noalloc(const void* q, const void* k_cache, const void* v_cache,
+                               const uint8_t* scales, int32_t num_blocks,
+                               const int32_t* block_table, int32_t max_blocks_per_seq,
+                               const int32_t* seq_lens, const int32_t* cu_seqlens_q,
+                               int32_t n_seqs, int32_t total_q, int32_t num_q_heads,
+                               int32_t num_kv_heads, int32_t head_dim, int32_t block_size,
+                               float scale, int32_t* plan, const pa_plan_info* info, void* out,
+                               float* lse, void* stream);
+
+/* Norms of queries and keys for each head and the rotation by position, in one
+ * pass over a step's rows, on their way from the projection to the append and
+ * the attention call.  For token t, head h of q (of k likewise, with k_weight):
+ *   x = q[t][h], with PA_QK_NORM x = x / sqrt(mean(x^2) + eps) * q_weight
+ *   (a NULL weight: ones);
+ *   pairs (a, b) of the first rot_dim dims turn by the position's angles:
+ *   (a cos - b sin, b cos + a sin), where pair i is dims (i, i + rot_dim/2), or
+ *   (2i, 2i+1) with PA_ROPE_INTERLEAVED; the other dims stay.
+ * Computed in float32, rounded once to dtype.  cos_sin[n_positions][rot_dim]:
+ * float32, the position's rot_dim/2 cosines, then the sines.  positions[n_tokens]:
+ * a token whose position is outside [0, n_positions) is skipped, its rows of
+ * q_out and k_out stay as they were (use -1 for padding).  q: rows of
+ * [num_q_heads][head_dim] q_stride elements apart, k: of [num_kv_heads][head_dim]
+ * k_stride apart; q_out, k_out: packed rows; q_out == q and k_out == k are
+ * allowed for packed rows, other overlaps are not.  Weights: head_dim values of
+ * dtype.  Either head count may be 0 (its pointers are then not read).
+ * All pointers are caller-owned device memory; asynchronous on stream;
+ * allocates nothing.  Errors: PA_ERR_ARG (NULL pointer with rows to do, bad
+ * sizes, strides, flags or eps, rows or weights not 16-byte aligned),
+ * PA_ERR_UNSUPPORTED (head_dim, dtype), PA_ERR_LAUNCH. */
+enum { PA_QK_NORM = 1, PA_ROPE_INTERLEAVED = 2 };
+int pa_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                    const int32_t* positions, int32_t n_tokens, const float* cos_sin,
+                    int32_t n_positions, int32_t rot_dim, const void* q_weight,
+                    const void* k_weight, float eps, int32_t flags, void* q_out, void* k_out,
+                    int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t dtype,
+                    void* stream);
 
 /* Timing hook, for callers that time attention calls on the device
  * (benchmarks, profilers) without event packets between kernels: the next

@@ -10,12 +10,13 @@ from __future__ import annotations
 
 import numpy as np
 
+from . import kv8
 from .apc import PrefixCacheOracle
 from .attention import kv_append, new_cache, paged_attention
 
 
 class OracleReplay:
-    def __init__(self, wl, store_values: bool = True):
+    def __init__(self, wl, store_values: bool = True, kv8: bool = False):
         cfg = wl.cfg
         self.wl = wl
         self.pool = PrefixCacheOracle(wl.num_blocks, cfg.block_size, wl.free_order)
@@ -26,7 +27,17 @@ class OracleReplay:
                                                    cfg.head_dim, cfg.block_size)
             self.k_cache = self.k_cache.astype(np.float32)
             self.v_cache = self.v_cache.astype(np.float32)
+            if kv8:  # an 8-bit cache: the values its codes stand for (oracle.kv8)
+                self.exps = np.zeros((wl.num_blocks, cfg.num_kv_heads, 2), dtype=np.int64)
+        self.kv8 = kv8
         self.n_cached = {}
+
+    def _append(self, md, k, v):
+        if self.kv8:
+            kv8.append(self.k_cache, self.v_cache, self.exps, md["block_table"], md["seq_lens"],
+                       md["cu_seqlens_q"], k, v)
+        else:
+            kv_append(self.k_cache, self.v_cache, md["slot_mapping"], k, v)
 
     def _apply(self, op):
         p = self.pool
@@ -42,7 +53,7 @@ class OracleReplay:
             if self.store_values:
                 k, v = op.k.get(), op.v.get()
                 md = p.metadata([op.seq_id], [len(k)], self.wl.max_blocks_per_seq)
-                kv_append(self.k_cache, self.v_cache, md["slot_mapping"], k, v)
+                self._append(md, k, v)
         else:
             raise ValueError(op.kind)
 
@@ -61,7 +72,7 @@ class OracleReplay:
         res = {"meta": md, "n_cached": dict(self.n_cached)}
         if self.store_values:
             k_new, v_new = launch.k_new.get(), launch.v_new.get()
-            kv_append(self.k_cache, self.v_cache, md["slot_mapping"], k_new, v_new)
+            self._append(md, k_new, v_new)
             if attend:
                 q = launch.q.get()
                 out, lse = paged_attention(q, self.k_cache, self.v_cache, md["block_table"],

@@ -16,7 +16,8 @@ LIB_PATH = os.path.join(_HERE, "libpa.so")
 
 PA_OK, PA_ERR_ARG, PA_ERR_UNSUPPORTED, PA_ERR_NO_BLOCKS, PA_ERR_UNKNOWN_SEQ, PA_ERR_LAUNCH = (
     0, -1, -2, -3, -4, -5)
-PA_F32, PA_BF16 = 0, 1
+PA_F32, PA_BF16, PA_BF16_KV8 = 0, 1, 2
+QK_NORM, ROPE_INTERLEAVED = 1, 2
 OP_ADD, OP_EXTEND, OP_TRUNCATE, OP_FREE = 0, 1, 2, 3
 KIND_PREFILL, KIND_DECODE, KIND_VERIFY = 0, 1, 2
 _CODES = {PA_ERR_ARG: "arg", PA_ERR_UNSUPPORTED: "unsupported", PA_ERR_NO_BLOCKS: "no_blocks",
@@ -30,7 +31,9 @@ EXPORTS = ["pa_last_error", "pa_abi_version", "pa_pool_create", "pa_pool_destroy
            "pa_attn_prefill", "pa_attn_decode", "pa_attn_verify", "pa_pool_set_eviction",
            "pa_pool_get_stats", "pa_pool_kv_waste", "pa_form_batches", "pa_prepare_launch",
            "pa_stage_upload", "pa_attn_workspace_size", "pa_attn_decode_workspace_size",
-           "pa_attn_decode_noalloc", "pa_set_launch_events"]
+           "pa_attn_decode_noalloc", "pa_kv8_append", "pa_kv8_read", "pa_kv8_attn_prefill",
+           "pa_kv8_attn_decode", "pa_kv8_attn_verify", "pa_kv8_attn_decode_noalloc",
+           "pa_qk_norm_rope", "pa_set_launch_events"]
 
 
 class PaError(RuntimeError):
@@ -65,6 +68,7 @@ class PlanInfo(C.Structure):
 _lib = None
 _torch = None  # the torch module, once a call needed it
 _attn = {}     # attention entry point of each launch kind
+_kv8_attn = {}  # and over the 8-bit cache
 _P = C.c_void_p
 _I32P = C.POINTER(C.c_int32)
 _I64P = C.POINTER(C.c_int64)
@@ -119,6 +123,15 @@ def lib():
         sig[name] = attn
     # decode without the workspace pair
     sig["pa_attn_decode_noalloc"] = (C.c_int, attn[1][:18] + attn[1][20:])
+    rows = [_P, i64, _P, i64, _P, i32, _P, _P, i32, i32, _P, _P, _P, i32, i32, i32, i32, i32, _P]
+    sig["pa_kv8_append"] = sig["pa_kv8_read"] = (C.c_int, rows)
+    # the scales behind the caches, and no dtype
+    kv8 = attn[1][:3] + [_P] + attn[1][3:15] + attn[1][16:]
+    for name in ("pa_kv8_attn_prefill", "pa_kv8_attn_decode", "pa_kv8_attn_verify"):
+        sig[name] = (C.c_int, kv8)
+    sig["pa_kv8_attn_decode_noalloc"] = (C.c_int, kv8[:18] + kv8[20:])
+    sig["pa_qk_norm_rope"] = (C.c_int, [_P, i64, _P, i64, _P, i32, _P, i32, i32, _P, _P, f32, i32,
+                                        _P, _P, i32, i32, i32, i32, _P])
     sig["pa_set_launch_events"] = (C.c_int, [_P, _P])
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -126,6 +139,8 @@ def lib():
         fn.argtypes = args
     _attn.update({KIND_PREFILL: L.pa_attn_prefill, KIND_DECODE: L.pa_attn_decode,
                   KIND_VERIFY: L.pa_attn_verify})
+    _kv8_attn.update({KIND_PREFILL: L.pa_kv8_attn_prefill, KIND_DECODE: L.pa_kv8_attn_decode,
+                      KIND_VERIFY: L.pa_kv8_attn_verify})
     _lib = L
     return L
 
@@ -594,3 +609,145 @@ def attention_decode_noalloc(q, k_cache, v_cache, block_table, seq_lens, cu_seql
         _dptr(seq_lens), _dptr(cu_seqlens_q), seq_lens.numel(), total_q, hq, hkv, d, bs,
         float(scale), _dtype_code(q), _dptr(plan_dev), C.byref(info), _dptr(out), _dptr(lse),
         _stream(stream)))
+
+
+# -- the 8-bit cache -----------------------------------------------------------
+def kv8_cache_shapes(num_blocks: int, num_kv_heads: int, head_dim: int, block_size: int = 16):
+    """Shapes of an 8-bit cache's (k_cache, v_cache, scales); the caches are
+    torch.float8_e4m3fn, the scales torch.uint8 (exponent + 127 of keys and of
+    values).  Contents need no initialisation."""
+    return ((num_blocks, num_kv_heads, head_dim // 64, block_size, 64),
+            (num_blocks, num_kv_heads, head_dim, block_size), (num_blocks, num_kv_heads, 2))
+
+
+def kv8_cache_dims(k_cache, v_cache, scales):
+    """(num_blocks, num_kv_heads, head_dim, block_size) of an 8-bit cache."""
+    nb, hkv, d, bs = v_cache.shape
+    if k_cache.shape != (nb, hkv, d // 64, bs, 64) or scales.shape != (nb, hkv, 2):
+        raise PaError(PA_ERR_ARG, "8-bit cache: k_cache, v_cache and scales differ in shape")
+    t = _torch or _torch_module()
+    if not (k_cache.dtype == v_cache.dtype == t.float8_e4m3fn and scales.dtype == t.uint8):
+        raise PaError(PA_ERR_UNSUPPORTED, f"8-bit cache of {k_cache.dtype}, {v_cache.dtype} and "
+                      f"{scales.dtype} (supported: float8_e4m3fn with uint8 scales)")
+    if not (k_cache.is_contiguous() and v_cache.is_contiguous() and scales.is_contiguous()):
+        raise PaError(PA_ERR_ARG, "8-bit cache: tensors must be contiguous")
+    return nb, hkv, d, bs
+
+
+def _row_stride(t, heads: int, d: int, what: str) -> int:
+    """Elements between the rows of a [T, heads, d] tensor whose rows are packed
+    (a slice of a larger matrix's columns is)."""
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d:
+        raise PaError(PA_ERR_ARG, f"{what}: shape {tuple(t.shape)}, expected [T, {heads}, {d}]")
+    s = t.stride()
+    if t.numel() and ((d > 1 and s[2] != 1) or (heads > 1 and s[1] != d)):
+        raise PaError(PA_ERR_ARG, f"{what}: a row's heads must be packed")
+    return s[0] if t.shape[0] > 1 else heads * d
+
+
+def _metadata(block_table, seq_lens, cu_seqlens):
+    """Checked (block table pointer, its width, seq_lens, cu_seqlens, n_seqs)."""
+    t = _torch or _torch_module()
+    n = seq_lens.numel()
+    if block_table.dim() != 2 or block_table.shape[0] < n or cu_seqlens.numel() < n + 1:
+        raise PaError(PA_ERR_ARG, f"metadata of {n} sequences: block_table "
+                      f"{tuple(block_table.shape)}, cu_seqlens {cu_seqlens.numel()}")
+    for m in (block_table, seq_lens, cu_seqlens):
+        if m.dtype != t.int32 or not m.is_contiguous():
+            raise PaError(PA_ERR_ARG, "metadata must be contiguous int32")
+    return _dptr(block_table), block_table.shape[1], _dptr(seq_lens), _dptr(cu_seqlens), n
+
+
+def _kv8_rows(fn, k, v, block_table, seq_lens, cu_seqlens, k_cache, v_cache, scales, stream):
+    nb, hkv, d, bs = kv8_cache_dims(k_cache, v_cache, scales)
+    if k.shape[0] != v.shape[0] or k.dtype != v.dtype:
+        raise PaError(PA_ERR_ARG, "keys and values differ in rows or dtype")
+    ks, vs = _row_stride(k, hkv, d, "keys"), _row_stride(v, hkv, d, "values")
+    _check(fn(_dptr(k), ks, _dptr(v), vs, *_metadata(block_table, seq_lens, cu_seqlens),
+              k.shape[0], _dptr(k_cache), _dptr(v_cache), _dptr(scales), nb, hkv, d, bs,
+              _dtype_code(k), _stream(stream)))
+
+
+def kv8_append(k_new, v_new, block_table, seq_lens, cu_seqlens, k_cache, v_cache, scales,
+               stream=None):
+    """Quantise new K/V ([T, Hkv, D] device tensors, rows at any stride) into
+    the 8-bit cache: rows cu_seqlens[r] .. cu_seqlens[r + 1] are sequence r's
+    last positions."""
+    _kv8_rows((_lib or lib()).pa_kv8_append, k_new, v_new, block_table, seq_lens, cu_seqlens,
+              k_cache, v_cache, scales, stream)
+
+
+def kv8_read(k_out, v_out, block_table, seq_lens, cu_seqlens, k_cache, v_cache, scales,
+             stream=None):
+    """Read tokens of the 8-bit cache into k_out and v_out ([T, Hkv, D]); rows
+    as kv8_append's."""
+    _kv8_rows((_lib or lib()).pa_kv8_read, k_out, v_out, block_table, seq_lens, cu_seqlens,
+              k_cache, v_cache, scales, stream)
+
+
+def _kv8_attn_args(q, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlens_q, plan_dev,
+                   info, out, lse, scale):
+    nb, hkv, d, bs = kv8_cache_dims(k_cache, v_cache, scales)
+    total_q, hq, dq = q.shape
+    t = _torch or _torch_module()
+    if q.dtype != t.bfloat16 or out.dtype != t.bfloat16:
+        raise PaError(PA_ERR_UNSUPPORTED, f"queries {q.dtype}, output {out.dtype} (supported: bf16)")
+    if dq != d or out.shape != q.shape or not (q.is_contiguous() and out.is_contiguous()):
+        raise PaError(PA_ERR_ARG, "q and out must be contiguous [T, Hq, D] of the cache's head_dim")
+    if lse is not None and (lse.dtype != t.float32 or lse.shape != (total_q, hq)
+                            or not lse.is_contiguous()):
+        raise PaError(PA_ERR_ARG, "lse must be contiguous float32 [T, Hq]")
+    bt, width, sl, cu, n = _metadata(block_table, seq_lens, cu_seqlens_q)
+    return (_dptr(q), _dptr(k_cache), _dptr(v_cache), _dptr(scales), nb, bt, width, sl, cu, n,
+            total_q, hq, hkv, d, bs, float(d ** -0.5 if scale is None else scale),
+            _dptr(plan_dev), C.byref(info))
+
+
+def kv8_attention(kind: int, q, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlens_q,
+                  plan_dev, info: PlanInfo, workspace, out, lse=None, scale=None, stream=None):
+    """Paged attention over the 8-bit cache (prefill / decode / verify by
+    ``kind``), with a plan built for PA_BF16_KV8."""
+    if _lib is None:
+        lib()
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(_kv8_attn[kind](*_kv8_attn_args(q, k_cache, v_cache, scales, block_table, seq_lens,
+                                           cu_seqlens_q, plan_dev, info, out, lse, scale),
+                           _dptr(workspace), ws_bytes, _dptr(out), _dptr(lse), _stream(stream)))
+
+
+def kv8_attention_decode_noalloc(q, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlens_q,
+                                 plan_dev, info: PlanInfo, out, lse=None, scale=None, stream=None):
+    """Decode over the 8-bit cache with the split-K partials in the library's
+    per-device array (as attention_decode_noalloc)."""
+    _check((_lib or lib()).pa_kv8_attn_decode_noalloc(
+        *_kv8_attn_args(q, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlens_q, plan_dev,
+                        info, out, lse, scale), _dptr(out), _dptr(lse), _stream(stream)))
+
+
+def qk_norm_rope(q, k, positions, cos_sin, q_out, k_out, q_weight=None, k_weight=None,
+                 eps: float = 1e-6, norm: bool = True, interleaved: bool = False, stream=None):
+    """Normalise (``norm``) and rotate queries [T, Hq, D] and keys [T, Hkv, D]
+    (rows at any stride) by their int32 positions and the float32 table cos_sin
+    [n_positions, rot_dim] (cosines, then sines), into packed q_out and k_out."""
+    t = _torch or _torch_module()
+    T, hq, d = q.shape
+    if k.dim() != 3 or k.shape[0] != T:
+        raise PaError(PA_ERR_ARG, f"k: shape {tuple(k.shape)}, expected [{T}, Hkv, {d}]")
+    hkv = k.shape[1]
+    for x, w, what in ((q_out, hq, "q_out"), (k_out, hkv, "k_out")):
+        if x.shape != (T, w, d) or not x.is_contiguous() or x.dtype != q.dtype:
+            raise PaError(PA_ERR_ARG, f"{what} must be contiguous [{T}, {w}, {d}] of q's dtype")
+    for w, what in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if w is not None and (w.numel() != d or w.dtype != q.dtype or not w.is_contiguous()):
+            raise PaError(PA_ERR_ARG, f"{what} must be {d} contiguous values of q's dtype")
+    if k.dtype != q.dtype or positions.numel() != T or positions.dtype != t.int32 or \
+            not positions.is_contiguous():
+        raise PaError(PA_ERR_ARG, "k of q's dtype and one contiguous int32 position per token")
+    if cos_sin.dim() != 2 or cos_sin.dtype != t.float32 or not cos_sin.is_contiguous():
+        raise PaError(PA_ERR_ARG, "cos_sin must be contiguous float32 [n_positions, rot_dim]")
+    _check((_lib or lib()).pa_qk_norm_rope(
+        _dptr(q), _row_stride(q, hq, d, "q"), _dptr(k), _row_stride(k, hkv, d, "k"),
+        _dptr(positions), T, _dptr(cos_sin), cos_sin.shape[0], cos_sin.shape[1], _dptr(q_weight),
+        _dptr(k_weight), float(eps),
+        (QK_NORM if norm else 0) | (ROPE_INTERLEAVED if interleaved else 0), _dptr(q_out),
+        _dptr(k_out), hq, hkv, d, _dtype_code(q), _stream(stream)))

@@ -2,6 +2,7 @@
 // on the caller's stream.  See include/pa.h for the contract of each call.
 #include <hip/hip_runtime.h>
 
+#include <cstdint>
 #include <mutex>
 
 #include "internal.h"
@@ -9,8 +10,8 @@
 
 namespace pa {
 namespace dev {
-int launch_attn_bf16(const void* q, const void* kc, const void* vc, int32_t num_blocks,
-                     const int32_t* bt, int32_t max_blocks, const int32_t* seq_lens,
+int launch_attn_bf16(const void* q, const void* kc, const void* vc, const uint8_t* scales,
+                     int32_t num_blocks, const int32_t* bt, int32_t max_blocks, const int32_t* seq_lens,
                      const int32_t* cu_q, int32_t hq, int32_t hkv, int32_t d, float scale,
                      const int32_t* plan, int32_t grid, int32_t n_tile, int32_t n_merge,
                      int32_t merge_narrow, bool wide_rows, bool tail, int64_t partial_rows, void* ws, void* out,
@@ -23,6 +24,21 @@ int launch_attn_f32(const void* q, const void* kc, const void* vc, int32_t num_b
 int launch_kv_append(const void* kn, const void* vn, const int32_t* slots, int32_t n, void* kc,
                      void* vc, int32_t nb, int32_t hkv, int32_t d, int32_t dtype,
                      hipStream_t stream);
+int launch_kv8_append(const void* kn, int64_t k_stride, const void* vn, int64_t v_stride,
+                      const int32_t* bt, int32_t max_blocks, const int32_t* seq_lens,
+                      const int32_t* cu, int32_t n_seqs, int32_t n, void* kc, void* vc,
+                      uint8_t* scales, int32_t nb, int32_t hkv, int32_t d, int32_t dtype,
+                      hipStream_t stream);
+int launch_kv8_read(void* k_out, int64_t k_stride, void* v_out, int64_t v_stride,
+                    const int32_t* bt, int32_t max_blocks, const int32_t* seq_lens,
+                    const int32_t* cu, int32_t n_seqs, int32_t n, const void* kc, const void* vc,
+                    const uint8_t* scales, int32_t nb, int32_t hkv, int32_t d, int32_t dtype,
+                    hipStream_t stream);
+int launch_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                        const int32_t* positions, int32_t n, const float* cos_sin,
+                        int32_t n_positions, int32_t rot, const void* qw, const void* kw, float eps,
+                        int32_t flags, void* q_out, void* k_out, int32_t hq, int32_t hkv, int32_t d,
+                        int32_t dtype, hipStream_t stream);
 int launch_stage_upload(const void* src, void* dst, int64_t n_dwords, hipStream_t stream);
 }  // namespace dev
 
@@ -45,6 +61,37 @@ int check_shape(const char* fn, int32_t num_blocks, int32_t num_kv_heads, int32_
     return fail(PA_ERR_UNSUPPORTED, "%s: block_size %d (supported: 16)", fn, block_size);
   if (dtype != PA_F32 && dtype != PA_BF16)
     return fail(PA_ERR_UNSUPPORTED, "%s: dtype %d (supported: PA_F32, PA_BF16)", fn, dtype);
+  return PA_OK;
+}
+
+// Rows read and written 16 bytes at a time.
+bool aligned16(const void* p, int64_t stride, int32_t dtype) {
+  return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && stride * (dtype == PA_BF16 ? 2 : 4) % 16 == 0;
+}
+
+// Checks shared by the two calls that move rows between memory and the 8-bit cache.
+// *work: whether there is anything to do.
+int check_kv8_rows(const char* fn, const void* k_rows, int64_t k_stride, const void* v_rows,
+                   int64_t v_stride, const int32_t* block_table, int32_t max_blocks_per_seq,
+                   const int32_t* seq_lens, const int32_t* cu_seqlens, int32_t n_seqs,
+                   int32_t n_tokens, const void* k_cache, const void* v_cache, const void* scales,
+                   int32_t num_blocks, int32_t num_kv_heads, int32_t head_dim, int32_t block_size,
+                   int32_t dtype, bool* work) {
+  const int rc = check_shape(fn, num_blocks, num_kv_heads, head_dim, block_size, dtype);
+  if (rc) return rc;
+  if (n_seqs < 0 || n_tokens < 0 || max_blocks_per_seq < 1)
+    return fail(PA_ERR_ARG, "%s: negative size or max_blocks_per_seq < 1", fn);
+  *work = n_seqs > 0 && n_tokens > 0;
+  if (!*work) return PA_OK;
+  if (!k_rows || !v_rows || !block_table || !seq_lens || !cu_seqlens || !k_cache || !v_cache || !scales)
+    return fail(PA_ERR_ARG, "%s: NULL device pointer", fn);
+  const int64_t row = int64_t(num_kv_heads) * head_dim;
+  if (k_stride < row || v_stride < row)
+    return fail(PA_ERR_ARG, "%s: row strides %lld and %lld, a token's heads take %lld", fn,
+                (long long)k_stride, (long long)v_stride, (long long)row);
+  if (!aligned16(k_rows, k_stride, dtype) || !aligned16(v_rows, v_stride, dtype) ||
+      !aligned16(k_cache, 0, dtype) || !aligned16(v_cache, 0, dtype))
+    return fail(PA_ERR_ARG, "%s: rows and caches must be 16-byte aligned", fn);
   return PA_OK;
 }
 
@@ -85,11 +132,11 @@ int attn_common(const char* fn, int32_t want_kind, const void* q, const void* k_
                 int32_t head_dim, int32_t block_size, float scale, int32_t dtype,
                 const int32_t* plan, const pa_plan_info* info, void* workspace,
                 size_t workspace_bytes, void* out, float* lse, void* stream,
-                bool noalloc = false) {
+                bool noalloc = false, bool kv8 = false, const uint8_t* scales = nullptr) {
   clear_error();
   const hipEvent_t ev_start = t_ev_start, ev_stop = t_ev_stop;
   t_ev_start = t_ev_stop = nullptr;
-  int rc = check_shape(fn, num_blocks, num_kv_heads, head_dim, block_size, dtype);
+  int rc = check_shape(fn, num_blocks, num_kv_heads, head_dim, block_size, kv8 ? PA_BF16 : dtype);
   if (rc) return rc;
   if (num_q_heads <= 0 || num_q_heads % num_kv_heads)
     return fail(PA_ERR_ARG, "%s: num_q_heads %d must be a positive multiple of num_kv_heads %d",
@@ -122,8 +169,13 @@ int attn_common(const char* fn, int32_t want_kind, const void* q, const void* k_
     }
     return PA_OK;
   }
-  if (!q || !k_cache || !v_cache || !block_table || !seq_lens || !cu_seqlens_q || !out)
+  if (!q || !k_cache || !v_cache || !block_table || !seq_lens || !cu_seqlens_q || !out ||
+      (kv8 && !scales))
     return fail(PA_ERR_ARG, "%s: NULL device pointer", fn);
+  // the 8-bit calls are new, so they can ask for what the kernels' 16-byte accesses need
+  if (kv8 && ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k_cache) |
+               reinterpret_cast<uintptr_t>(v_cache) | reinterpret_cast<uintptr_t>(out)) & 15))
+    return fail(PA_ERR_ARG, "%s: q, out and caches must be 16-byte aligned", fn);
   if (dtype == PA_F32) {
     rc = dev::launch_attn_f32(q, k_cache, v_cache, num_blocks, block_table, max_blocks_per_seq,
                               seq_lens, cu_seqlens_q, n_seqs, total_q, num_q_heads, num_kv_heads,
@@ -164,7 +216,7 @@ int attn_common(const char* fn, int32_t want_kind, const void* q, const void* k_
       return fail(PA_ERR_ARG, "%s: workspace of %zu bytes, plan needs %lld", fn, workspace_bytes,
                   (long long)info->workspace_bytes);
     const int64_t partial_rows = info->partial_rows;
-    rc = dev::launch_attn_bf16(q, k_cache, v_cache, num_blocks, block_table, max_blocks_per_seq,
+    rc = dev::launch_attn_bf16(q, k_cache, v_cache, scales, num_blocks, block_table, max_blocks_per_seq,
                                seq_lens, cu_seqlens_q, num_q_heads, num_kv_heads, head_dim, scale,
                                plan, info->grid, info->n_shared_items + info->n_tile_items,
                                n_merge,
@@ -242,6 +294,97 @@ int pa_stage_upload(void* dst, const void* src, int64_t bytes, void* stream) {
   return PA_OK;
 }
 
+int pa_kv8_append(const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+                  const int32_t* block_table, int32_t max_blocks_per_seq, const int32_t* seq_lens,
+                  const int32_t* cu_seqlens, int32_t n_seqs, int32_t n_tokens, void* k_cache,
+                  void* v_cache, uint8_t* scales, int32_t num_blocks, int32_t num_kv_heads,
+                  int32_t head_dim, int32_t block_size, int32_t dtype, void* stream) {
+  pa::clear_error();
+  bool work = false;
+  int rc = pa::check_kv8_rows("pa_kv8_append", k_new, k_stride, v_new, v_stride, block_table,
+                              max_blocks_per_seq, seq_lens, cu_seqlens, n_seqs, n_tokens, k_cache,
+                              v_cache, scales, num_blocks, num_kv_heads, head_dim, block_size,
+                              dtype, &work);
+  if (rc || !work) return rc;
+  rc = pa::dev::launch_kv8_append(k_new, k_stride, v_new, v_stride, block_table,
+                                  max_blocks_per_seq, seq_lens, cu_seqlens, n_seqs, n_tokens,
+                                  k_cache, v_cache, scales, num_blocks, num_kv_heads, head_dim,
+                                  dtype, static_cast<hipStream_t>(stream));
+  if (rc)
+    return pa::fail(PA_ERR_LAUNCH, "pa_kv8_append: %s",
+                    hipGetErrorString(static_cast<hipError_t>(rc)));
+  return PA_OK;
+}
+
+int pa_kv8_read(void* k_out, int64_t k_stride, void* v_out, int64_t v_stride,
+                const int32_t* block_table, int32_t max_blocks_per_seq, const int32_t* seq_lens,
+                const int32_t* cu_seqlens, int32_t n_seqs, int32_t n_tokens, const void* k_cache,
+                const void* v_cache, const uint8_t* scales, int32_t num_blocks,
+                int32_t num_kv_heads, int32_t head_dim, int32_t block_size, int32_t dtype,
+                void* stream) {
+  pa::clear_error();
+  bool work = false;
+  int rc = pa::check_kv8_rows("pa_kv8_read", k_out, k_stride, v_out, v_stride, block_table,
+                              max_blocks_per_seq, seq_lens, cu_seqlens, n_seqs, n_tokens, k_cache,
+                              v_cache, scales, num_blocks, num_kv_heads, head_dim, block_size,
+                              dtype, &work);
+  if (rc || !work) return rc;
+  rc = pa::dev::launch_kv8_read(k_out, k_stride, v_out, v_stride, block_table, max_blocks_per_seq,
+                                seq_lens, cu_seqlens, n_seqs, n_tokens, k_cache, v_cache, scales,
+                                num_blocks, num_kv_heads, head_dim, dtype,
+                                static_cast<hipStream_t>(stream));
+  if (rc)
+    return pa::fail(PA_ERR_LAUNCH, "pa_kv8_read: %s",
+                    hipGetErrorString(static_cast<hipError_t>(rc)));
+  return PA_OK;
+}
+
+int pa_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                    const int32_t* positions, int32_t n_tokens, const float* cos_sin,
+                    int32_t n_positions, int32_t rot_dim, const void* q_weight,
+                    const void* k_weight, float eps, int32_t flags, void* q_out, void* k_out,
+                    int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t dtype,
+                    void* stream) {
+  using pa::fail;
+  static const char* fn = "pa_qk_norm_rope";
+  pa::clear_error();
+  if (num_q_heads < 0 || num_kv_heads < 0 || num_q_heads + int64_t(num_kv_heads) < 1)
+    return fail(PA_ERR_ARG, "%s: num_q_heads %d and num_kv_heads %d", fn, num_q_heads, num_kv_heads);
+  if (head_dim != 64 && head_dim != 128)
+    return fail(PA_ERR_UNSUPPORTED, "%s: head_dim %d (supported: 64, 128)", fn, head_dim);
+  if (dtype != PA_F32 && dtype != PA_BF16)
+    return fail(PA_ERR_UNSUPPORTED, "%s: dtype %d (supported: PA_F32, PA_BF16)", fn, dtype);
+  if (flags & ~(PA_QK_NORM | PA_ROPE_INTERLEAVED))
+    return fail(PA_ERR_ARG, "%s: flags 0x%x", fn, flags);
+  if (n_tokens < 0 || n_positions < 0)
+    return fail(PA_ERR_ARG, "%s: negative size", fn);
+  if (rot_dim < 0 || rot_dim > head_dim || rot_dim % 2)
+    return fail(PA_ERR_ARG, "%s: rot_dim %d must be even, of 0 .. %d", fn, rot_dim, head_dim);
+  if ((flags & PA_QK_NORM) && !(eps >= 0.f && eps < __builtin_huge_valf()))
+    return fail(PA_ERR_ARG, "%s: eps must be finite and not negative", fn);
+  if (n_tokens == 0) return PA_OK;
+  if (!positions || (rot_dim > 0 && n_positions > 0 && !cos_sin) ||
+      (num_q_heads > 0 && (!q || !q_out)) || (num_kv_heads > 0 && (!k || !k_out)))
+    return fail(PA_ERR_ARG, "%s: NULL device pointer", fn);
+  if ((num_q_heads > 0 && q_stride < int64_t(num_q_heads) * head_dim) ||
+      (num_kv_heads > 0 && k_stride < int64_t(num_kv_heads) * head_dim))
+    return fail(PA_ERR_ARG, "%s: row strides %lld and %lld, a token's heads take %lld and %lld", fn,
+                (long long)q_stride, (long long)k_stride, (long long)num_q_heads * head_dim,
+                (long long)num_kv_heads * head_dim);
+  if ((num_q_heads > 0 && (!pa::aligned16(q, q_stride, dtype) || !pa::aligned16(q_out, 0, dtype))) ||
+      (num_kv_heads > 0 && (!pa::aligned16(k, k_stride, dtype) || !pa::aligned16(k_out, 0, dtype))) ||
+      !pa::aligned16(q_weight, 0, dtype) || !pa::aligned16(k_weight, 0, dtype) ||
+      (reinterpret_cast<uintptr_t>(cos_sin) & 3))
+    return fail(PA_ERR_ARG, "%s: rows and weights must be 16-byte aligned", fn);
+  const int rc = pa::dev::launch_qk_norm_rope(
+      q, q_stride, k, k_stride, positions, n_tokens, cos_sin, n_positions, rot_dim, q_weight,
+      k_weight, eps, flags, q_out, k_out, num_q_heads, num_kv_heads, head_dim, dtype,
+      static_cast<hipStream_t>(stream));
+  if (rc)
+    return fail(PA_ERR_LAUNCH, "%s: %s", fn, hipGetErrorString(static_cast<hipError_t>(rc)));
+  return PA_OK;
+}
+
 #define PA_ATTN_ARGS                                                                            \
   const void *q, const void *k_cache, const void *v_cache, int32_t num_blocks,                  \
       const int32_t *block_table, int32_t max_blocks_per_seq, const int32_t *seq_lens,          \
@@ -275,6 +418,37 @@ int pa_attn_decode_noalloc(const void* q, const void* k_cache, const void* v_cac
                          num_blocks, block_table, max_blocks_per_seq, seq_lens, cu_seqlens_q,
                          n_seqs, total_q, num_q_heads, num_kv_heads, head_dim, block_size, scale,
                          dtype, plan, info, nullptr, 0, out, lse, stream, /*noalloc=*/true);
+}
+
+#define PA_KV8_ATTN_ARGS                                                                        \
+  const void *q, const void *k_cache, const void *v_cache, const uint8_t *scales,               \
+      int32_t num_blocks, const int32_t *block_table, int32_t max_blocks_per_seq,               \
+      const int32_t *seq_lens, const int32_t *cu_seqlens_q, int32_t n_seqs, int32_t total_q,    \
+      int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t block_size,          \
+      float scale, int32_t *plan, const pa_plan_info *info
+#define PA_KV8_ATTN_PASS                                                                        \
+  q, k_cache, v_cache, num_blocks, block_table, max_blocks_per_seq, seq_lens, cu_seqlens_q,     \
+      n_seqs, total_q, num_q_heads, num_kv_heads, head_dim, block_size, scale, PA_BF16_KV8, plan, \
+      info
+
+int pa_kv8_attn_prefill(PA_KV8_ATTN_ARGS, void* workspace, size_t workspace_bytes, void* out,
+                        float* lse, void* stream) {
+  return pa::attn_common("pa_kv8_attn_prefill", PA_KIND_PREFILL, PA_KV8_ATTN_PASS, workspace,
+                         workspace_bytes, out, lse, stream, false, true, scales);
+}
+int pa_kv8_attn_decode(PA_KV8_ATTN_ARGS, void* workspace, size_t workspace_bytes, void* out,
+                       float* lse, void* stream) {
+  return pa::attn_common("pa_kv8_attn_decode", PA_KIND_DECODE, PA_KV8_ATTN_PASS, workspace,
+                         workspace_bytes, out, lse, stream, false, true, scales);
+}
+int pa_kv8_attn_verify(PA_KV8_ATTN_ARGS, void* workspace, size_t workspace_bytes, void* out,
+                       float* lse, void* stream) {
+  return pa::attn_common("pa_kv8_attn_verify", PA_KIND_VERIFY, PA_KV8_ATTN_PASS, workspace,
+                         workspace_bytes, out, lse, stream, false, true, scales);
+}
+int pa_kv8_attn_decode_noalloc(PA_KV8_ATTN_ARGS, void* out, float* lse, void* stream) {
+  return pa::attn_common("pa_kv8_attn_decode_noalloc", PA_KIND_DECODE, PA_KV8_ATTN_PASS, nullptr, 0,
+                         out, lse, stream, /*noalloc=*/true, true, scales);
 }
 
 int pa_set_launch_events(void* start_event, void* stop_event) {

@@ -25,6 +25,11 @@
 // k-elements are eight consecutive keys: then V^T operands are single 16-byte
 // reads of the cache's [head_dim][block] value layout.
 //
+// The same items read the 8-bit cache (KV8): e4m3 values with a power-of-two
+// scale per (block, kv-head) of keys and of values.  e4m3 holds four significant
+// bits, so a value times its scale is a bf16 number: operands are converted
+// exactly, and an item computes what it would over a bf16 cache of those numbers.
+//
 // Scores are scaled by scale * log2(e) and exponentiated with exp2; the
 // natural-log LSE is recovered as ln2 * (m + log2 l).
 #include <hip/hip_ext.h>
@@ -38,7 +43,7 @@ namespace {
 
 struct AttnArgs {
   const __bf16* q;
-  const __bf16* kc;
+  const __bf16* kc;  // KV8: the caches' bytes
   const __bf16* vc;
   const int32_t* bt;
   const int32_t* seq_lens;
@@ -55,6 +60,7 @@ struct AttnArgs {
   int32_t group;
   int32_t merge_narrow;  // narrow merge-group templates, or -1: as the plan says
   float scale_log2;
+  const uint8_t* scales;  // KV8: [num_blocks][hkv][2], exponent + 127 of keys and of values
 };
 
 // Row r of a tile's K buffer holds key perm32(r): bits 2 and 3 swapped.
@@ -116,6 +122,19 @@ __device__ __forceinline__ void copy16_to_lds(const void* base, int bytes, uint3
                                            STREAM ? kCachePolicyNonTemporal : 0);
 }
 
+// Power of two of a scale byte (exponent + 127).
+__device__ __forceinline__ float scale8(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// Four e4m3 values times a power of two, as bf16 (exact).
+__device__ __forceinline__ u32x2 bf16_of_e4m3(uint32_t x, float scale) {
+  return u32x2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, false)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, true))};
+}
+__device__ __forceinline__ u32x4 bf16_of_e4m3(uint32_t x0, uint32_t x1, float scale) {
+  const u32x2 a = bf16_of_e4m3(x0, scale), b = bf16_of_e4m3(x1, scale);
+  return u32x4{a[0], a[1], b[0], b[1]};
+}
+
 // Sum of the eight bf16 values of a vector added to acc (v_dot2 with ones).
 __device__ __forceinline__ float add_bf16x8(bf16x8 v, float acc) {
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -166,7 +185,12 @@ __device__ __forceinline__ float max_halves(float x) {
 // step t, then the score MFMAs of step t + 1 and the PV MFMAs of step t, beside
 // the softmax of the SIMD's other wavefronts.  K of step t + 2 and V^T of step t + 1 are copied into the LDS
 // buffers freed by steps t and t - 1 during step t.
-template <int D, int NSUB, bool SHARED, bool FULL, bool STREAM = false>
+//
+// KV8: a step's K and V^T pass through registers, where they become bf16, into
+// the same LDS tiles: step t begins by storing K of step t + 2 and V^T of step
+// t + 1, loaded during step t - 1, and loads the next.  Each value is converted
+// once per workgroup, not once per wavefront that reads it.
+template <int D, int NSUB, bool KV8, bool SHARED, bool FULL, bool STREAM = false>
 __device__ __forceinline__ void tile_item(const int32_t* it, int g, int poff, const AttnArgs& a,
                                           TileSmem<D, NSUB>& sm) {
   constexpr int KT = 32 * NSUB;     // keys per step
@@ -246,9 +270,10 @@ __device__ __forceinline__ void tile_item(const int32_t* it, int g, int poff, co
     voff[i] = (uint32_t)((d * kBlock + 8 * h) * 2);
   }
   const int32_t* bt = a.bt + (int64_t)key_seq * a.max_blocks;
-  const char* kbase = reinterpret_cast<const char*>(a.kc + (int64_t)g * kBlock * D);
-  const char* vbase = reinterpret_cast<const char*>(a.vc + (int64_t)g * D * kBlock);
-  const int64_t blk_bytes = (int64_t)a.hkv * kBlock * D * 2;  // one block, all kv-heads
+  // KV8: half the bytes, as many values
+  const char* kbase = reinterpret_cast<const char*>(a.kc + (int64_t)g * kBlock * D / (KV8 ? 2 : 1));
+  const char* vbase = reinterpret_cast<const char*>(a.vc + (int64_t)g * D * kBlock / (KV8 ? 2 : 1));
+  const int64_t blk_bytes = (int64_t)a.hkv * kBlock * D * (KV8 ? 1 : 2);  // one block, all kv-heads
 
   // Block ids of a step (wave-uniform), clamped into the cache when the
   // window of 64 table entries is fetched.  Blocks at or past kend read the
@@ -291,6 +316,67 @@ __device__ __forceinline__ void tile_item(const int32_t* it, int g, int poff, co
     for (int i = 0; i < NI; ++i)
       copy16_to_lds<STREAM>(vbase + copy_block(blk, i), kHeadBytes, voff[i],
                             &sm.v[buf][512 * (4 * i + w)]);
+  };
+
+  // KV8 staging: a wavefront loads 1 KB pieces, 16 bytes per lane: piece 4 i + w
+  // of a step is 64 head dims of block (4 i + w) / (D / 64).  Of K a lane takes
+  // 16 dims of one slot and writes two 16-byte units; eight neighbouring lanes
+  // (four slots) write in distinct banks.  Of V^T it takes one dim's 16 keys.
+  static_assert(!KV8 || NSUB == 2, "8-bit staging: 64-key steps");
+  constexpr int NR = KV8 ? NSUB * D / 128 : 1;
+  u32x4 rk[NR], rv[NR];      // raw K and V^T on their way
+  uint32_t ek[NR], ev[NR];   // their blocks' scale bytes
+  const int slot8 = (lane >> 1) & 15, pos8 = key_slot_pos(slot8);
+  const uint32_t koff8 = slot8 * 64 + 32 * hh + 16 * (lane & 1);
+  const uint32_t kdst8 = hh * 64 + 4 * pos8 + ((2 * (lane & 1)) ^ ((pos8 >> 2) & 3));
+  const uint8_t* scales = a.scales + 2 * g;
+  auto piece_block = [&](const int64_t (&blk)[NB], int i) {
+    if constexpr (D == 128) return (w >> 1) ? blk[2 * i + 1] : blk[2 * i];
+    else return (w >> 1) ? ((w & 1) ? blk[3] : blk[2]) : ((w & 1) ? blk[1] : blk[0]);
+  };
+  const uint32_t piece_off = D == 128 ? (w & 1) * 1024 : 0;  // of a piece in its block
+  auto raw16 = [](const char* p) {
+    if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+    else return ld16(p);
+  };
+  // a block is 16 D hkv bytes, its scales are 2 hkv
+  auto scale_at = [&](int64_t blk, int side) -> uint32_t { return scales[(uint64_t)blk / (8 * D) + side]; };
+  auto load_k8 = [&](const int64_t (&blk)[NB]) {
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+      const int64_t b = piece_block(blk, i);
+      rk[i] = raw16(kbase + b + piece_off + koff8);
+      ek[i] = scale_at(b, 0);
+    }
+  };
+  auto load_v8 = [&](const int64_t (&blk)[NB]) {
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+      const int64_t b = piece_block(blk, i);
+      rv[i] = raw16(vbase + b + piece_off + 16 * lane);
+      ev[i] = scale_at(b, 1);
+    }
+  };
+  auto store_k8 = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+      const float sc = scale8(ek[i]);
+      // units of 16 bytes; a piece fills two 32-dim groups (128 units) of the tile
+      __bf16* p = &sm.k[buf][8 * (128 * (4 * i + w) + kdst8)];
+      __bf16* p1 = &sm.k[buf][8 * (128 * (4 * i + w) + (kdst8 ^ 1))];
+      st16(p, bf16_of_e4m3(rk[i][0], rk[i][1], sc));
+      st16(p1, bf16_of_e4m3(rk[i][2], rk[i][3], sc));
+    }
+  };
+  auto store_v8 = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+      const float sc = scale8(ev[i]);
+      const int d = lane, sw = vswz(d);  // vswz(64 + d) == vswz(d)
+      __bf16* p = &sm.v[buf][8 * (128 * (4 * i + w) + 2 * d)];
+      st16(p + 8 * sw, bf16_of_e4m3(rv[i][0], rv[i][1], sc));
+      st16(p + 8 * (1 - sw), bf16_of_e4m3(rv[i][2], rv[i][3], sc));
+    }
   };
 
   // LDS operand addresses: per lane, the byte offset of its K unit for each
@@ -357,19 +443,33 @@ __device__ __forceinline__ void tile_item(const int32_t* it, int g, int poff, co
   // Probabilities of a step as bf16 B operands: p[u][kk] holds keys
   // 32 u + 16 kk + 8 hh + 0..7 (the perm32 order makes them consecutive).
   // Returns this lane's row sum: the bf16 probabilities the PV product uses,
-  // two per v_dot2, in two chains.
+  // two per v_dot2, in two chains.  KV8 sums the float32 probabilities, so that the
+  // log-sum-exp of rows of few keys does not carry the rounding to bf16.
   auto exps = [&](const f32x16 (&s)[NSUB], bf16x8 (&p)[NSUB][2]) {
+    if constexpr (KV8) {
+      float l0 = 0.f, l1 = 0.f;
 #pragma unroll
-    for (int u = 0; u < NSUB; ++u)
+      for (int u = 0; u < NSUB; ++u)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) p[u][e >> 3][e & 7] = (__bf16)fast_exp2(fmaf(s[u][e], c, -mc));
-    float l0 = 0.f, l1 = 0.f;
+        for (int e = 0; e < 16; ++e) {
+          const float x = fast_exp2(fmaf(s[u][e], c, -mc));
+          p[u][e >> 3][e & 7] = (__bf16)x;
+          (e < 8 ? l0 : l1) += x;
+        }
+      return l0 + l1;
+    } else {
 #pragma unroll
-    for (int u = 0; u < NSUB; ++u) {
-      l0 = add_bf16x8(p[u][0], l0);
-      l1 = add_bf16x8(p[u][1], l1);
+      for (int u = 0; u < NSUB; ++u)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) p[u][e >> 3][e & 7] = (__bf16)fast_exp2(fmaf(s[u][e], c, -mc));
+      float l0 = 0.f, l1 = 0.f;
+#pragma unroll
+      for (int u = 0; u < NSUB; ++u) {
+        l0 = add_bf16x8(p[u][0], l0);
+        l1 = add_bf16x8(p[u][1], l1);
+      }
+      return l0 + l1;
     }
-    return l0 + l1;
   };
   // The reference only has to keep the probabilities in range (their relative
   // precision does not depend on it), and the row sum, which is needed
@@ -422,13 +522,30 @@ __device__ __forceinline__ void tile_item(const int32_t* it, int g, int poff, co
     // (for the K copy) and used again one step ahead (for the V^T copy)
     int64_t blk[2][NB] = {};
     step_blocks(kv0, blk[0]);
-    issue_k(blk[0], 0);
-    issue_v(blk[0], 0);
-    if (ntiles > 1) {
-      step_blocks(kv0 + KT, blk[1]);
-      issue_k(blk[1], 1);
+    if constexpr (KV8) {
+      load_k8(blk[0]);
+      load_v8(blk[0]);
+      store_k8(0);
+      store_v8(0);
+      if (ntiles > 1) {
+        step_blocks(kv0 + KT, blk[1]);
+        load_k8(blk[1]);
+        load_v8(blk[1]);  // stored in step 0
+        store_k8(1);
+        if (ntiles > 2) {
+          step_blocks(kv0 + 2 * KT, blk[0]);
+          load_k8(blk[0]);
+        }
+      }
+    } else {
+      issue_k(blk[0], 0);
+      issue_v(blk[0], 0);
+      if (ntiles > 1) {
+        step_blocks(kv0 + KT, blk[1]);
+        issue_k(blk[1], 1);
+      }
+      wait_vmem();
     }
-    wait_vmem();
     __syncthreads();
     // Wavefronts without rows (items of fewer than kTileRows rows) only help
     // with the copies and pass the barriers.
@@ -443,16 +560,33 @@ __device__ __forceinline__ void tile_item(const int32_t* it, int g, int poff, co
     }
     __syncthreads();  // K buffer 0 is refilled next
 
+    // KV8: K of step t + 2 and V^T of step t + 1 into LDS, the next on their way
+    auto stage8 = [&](int t, auto buf_c) {
+      constexpr int buf = decltype(buf_c)::value;
+      store_v8(1 - buf);
+      if (t + 2 < ntiles) {
+        store_k8(buf);
+        load_v8(blk[buf]);  // of step t + 2, whose blocks were found one step earlier
+        if (t + 3 < ntiles) {
+          step_blocks(kv0 + KT * (t + 3), blk[1 - buf]);
+          load_k8(blk[1 - buf]);
+        }
+      }
+    };
     // One pipelined step: softmax + PV of step t, scores of step t + 1.
     // buf_c = t % 2, the LDS buffer pair of step t (a compile-time constant).
     auto step = [&](int t, auto mask_next, auto buf_c) {
       constexpr int buf = decltype(buf_c)::value;
       const int t0 = kv0 + KT * t;
-      if (t + 2 < ntiles) {
-        step_blocks(t0 + 2 * KT, blk[buf]);
-        issue_k(blk[buf], buf);
+      if constexpr (KV8) {
+        stage8(t, buf_c);
+      } else {
+        if (t + 2 < ntiles) {
+          step_blocks(t0 + 2 * KT, blk[buf]);
+          issue_k(blk[buf], buf);
+        }
+        issue_v(blk[1 - buf], 1 - buf);  // blocks of step t + 1, found one step earlier
       }
-      issue_v(blk[1 - buf], 1 - buf);  // blocks of step t + 1, found one step earlier
       bf16x8 p[NSUB][2];
       f32x16 sn[NSUB];
       probs(s, p);
@@ -467,20 +601,24 @@ __device__ __forceinline__ void tile_item(const int32_t* it, int g, int poff, co
       pv(buf_c, p);
       __builtin_amdgcn_s_setprio(0);
       if constexpr (decltype(mask_next)::value) mask(t0 + KT, sn);
-      wait_vmem();
+      if constexpr (!KV8) wait_vmem();  // KV8: the barrier waits for the stores into LDS
       __syncthreads();
 #pragma unroll
       for (int u = 0; u < NSUB; ++u) s[u] = sn[u];
     };
     auto idle_step = [&](int t, auto buf_c) {
-      constexpr int buf = decltype(buf_c)::value;
-      const int t0 = kv0 + KT * t;
-      if (t + 2 < ntiles) {
-        step_blocks(t0 + 2 * KT, blk[buf]);
-        issue_k(blk[buf], buf);
+      if constexpr (KV8) {
+        stage8(t, buf_c);
+      } else {
+        constexpr int buf = decltype(buf_c)::value;
+        const int t0 = kv0 + KT * t;
+        if (t + 2 < ntiles) {
+          step_blocks(t0 + 2 * KT, blk[buf]);
+          issue_k(blk[buf], buf);
+        }
+        issue_v(blk[1 - buf], 1 - buf);
+        wait_vmem();
       }
-      issue_v(blk[1 - buf], 1 - buf);
-      wait_vmem();
       __syncthreads();
     };
     // steps [t, lim) with the given masking, two at a time so that each
@@ -744,6 +882,209 @@ __device__ __forceinline__ void row_item(const int32_t* it, int g, int poff, con
   }
 }
 
+// A row item's result for the row in this lane's column: output and log-sum-exp of
+// (token, q-head) where prow < 0, else partial row prow.
+template <int D>
+__device__ __forceinline__ void store_row(const AttnArgs& a, const f32x4 (&acc)[D / 16], float l, float mc,
+                                          int token, int hq, int prow, int g4) {
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  const float lse_v = l > 0.f ? kLn2 * (mc + __log2f(l)) : kNegInf;
+  if (prow < 0) {
+    __bf16* op = a.out + ((int64_t)token * a.hq + hq) * D + 4 * g4;
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) {
+      __bf16 o4[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o4[e] = (__bf16)(acc[dt][e] * inv);
+      *reinterpret_cast<u32x2*>(op + 16 * dt) = __builtin_bit_cast(u32x2, o4);
+    }
+    if (a.lse && g4 == 0) a.lse[(int64_t)token * a.hq + hq] = lse_v;
+  } else {
+    float* op = a.ws_o + (int64_t)prow * D + 4 * g4;
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) *reinterpret_cast<f32x4*>(op + 16 * dt) = acc[dt] * inv;
+    if (g4 == 0) a.ws_lse[prow] = l == l ? lse_v : l;
+  }
+}
+
+// Row item over the 8-bit cache: as row_item, in steps of 64 keys (four blocks),
+// so that every load is 16 bytes per lane of 64 contiguous bytes of a key or a
+// dimension's 16 keys.  Score tile tt takes tokens 4 tt .. 4 tt + 3 of each of the
+// four blocks: row j is token 4 tt + j % 4 of block j / 4, and lane (j, g4)'s
+// elements are keys 4 tt + e of block g4, the block whose values the lane holds as
+// A operand of the PV product (16 keys of dimension 16 dt + j: two k-steps).  The
+// score's k-steps take dims 64 c + 16 g4 + 8 u .. + 7, the halves u of a lane's load.
+template <int D, int NC>
+__device__ __forceinline__ void row_item8(const int32_t* it, int g, int poff, const AttnArgs& a) {
+  constexpr int KC = D / 64;  // 64-dim groups of a key
+  constexpr int DT = D / 16;  // 16-row tiles of O^T
+  constexpr int kStep = 64;
+  const int r = it[I_SEQ];
+  if (r < 0) return;
+  const int row0 = it[I_ROW0], nrows = it[I_NROWS];
+  const int kv0 = it[I_KV0], part = it[I_PART] < 0 ? -1 : it[I_PART] + poff;
+  const int lane = threadIdx.x & 63, j = lane & 15, g4 = lane >> 4;
+  const int L = a.seq_lens[r];
+  const int qs = a.cu_q[r], n = a.cu_q[r + 1] - qs;
+  // at most kRowItemBlocks blocks per item, as in row_item
+  const int kv1 = min(min(it[I_KV1], L), kv0 + kRowItemBlocks * kBlock);
+  const int G = a.group;
+
+  bool valid[NC];
+  int qi[NC], hq[NC], apos[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    valid[c] = 16 * c + j < nrows;
+    const int rho = row0 + 16 * c + j;
+    qi[c] = rho / G;
+    hq[c] = g * G + (rho - qi[c] * G);
+    apos[c] = valid[c] ? L - n + qi[c] : -1;
+  }
+  const int amin = L - n + row0 / G;
+
+  bf16x8 qf[NC][2 * KC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const __bf16* qp = a.q + ((int64_t)(qs + qi[c]) * a.hq + hq[c]) * D + 16 * g4;
+#pragma unroll
+    for (int ks = 0; ks < 2 * KC; ++ks)
+      qf[c][ks] = as_bf16x8(valid[c] ? ld16(qp + 64 * (ks / 2) + 8 * (ks % 2)) : zero16());
+  }
+  f32x4 acc[NC][DT];
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) acc[c][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const float cs = a.scale_log2;
+  float m[NC], mc[NC], l[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) m[c] = kNegInf, mc[c] = 0.f, l[c] = 0.f;
+
+  // One register set for K and one for V^T, reloaded as in row_item.  Blocks at
+  // or past kv1 read the item's last block again.
+  const uint8_t* kc = reinterpret_cast<const uint8_t*>(a.kc);
+  const uint8_t* vc = reinterpret_cast<const uint8_t*>(a.vc);
+  const int last = kv1 > kv0 ? (kv1 - 1) / kBlock : kv0 / kBlock;
+  BlockSpan win;
+  win.init(a.bt + (int64_t)r * a.max_blocks, a.max_blocks, kv0 / kBlock);
+  auto block_of = [&](int jb) {  // per lane
+    const int id = __shfl(win.ids, (min(jb, last) - win.base) & 63, 64);
+    return (int64_t)clamp_block(id, a.num_blocks) * a.hkv + g;
+  };
+  u32x4 kreg[4][KC], vreg[DT];
+  uint32_t ek = 0, ev = 0;
+  auto load_k = [&](int t0) {
+    const int64_t b = block_of(t0 / kBlock + (j >> 2));
+    const uint8_t* p = kc + b * (kBlock * D) + (j & 3) * 64 + 16 * g4;
+#pragma unroll
+    for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+      for (int c = 0; c < KC; ++c)
+        kreg[tt][c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + 1024 * c + 256 * tt));
+    ek = a.scales[2 * b];
+  };
+  auto load_v = [&](int t0) {
+    const int64_t b = block_of(t0 / kBlock + g4);
+    const uint8_t* p = vc + b * (kBlock * D) + j * kBlock;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+      vreg[dt] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + 256 * dt));
+    ev = a.scales[2 * b + 1];
+  };
+
+  if (kv0 < kv1) {
+    load_k(kv0);
+    load_v(kv0);
+  }
+  for (int t0 = kv0; t0 < kv1; t0 += kStep) {
+    const bool more = t0 + kStep < kv1;
+    f32x4 s[NC][4];
+    const float sk = scale8(ek);
+#pragma unroll
+    for (int tt = 0; tt < 4; ++tt) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c) s[c][tt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < 2 * KC; ++ks) {
+        const u32x4 x = kreg[tt][ks / 2];
+        const bf16x8 k = as_bf16x8(bf16_of_e4m3(x[2 * (ks % 2)], x[2 * (ks % 2) + 1], sk));
+#pragma unroll
+        for (int c = 0; c < NC; ++c) s[c][tt] = mfma16(k, qf[c][ks], s[c][tt]);
+      }
+    }
+    if (more) load_k(t0 + kStep);
+    // Lane (j, g4), element e of score tile tt holds key t0 + 16 g4 + 4 tt + e.
+    const bool masked = t0 + kStep - 1 > amin || !more;  // wave-uniform
+    if (masked) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int key = t0 + 16 * g4 + 4 * tt + e;
+            s[c][tt][e] = (key <= apos[c] && key < kv1) ? s[c][tt][e] : kNegInf;
+          }
+      // zero values of keys at or past kv1 (slots that may never have been written)
+      const int keep = kv1 - (t0 + 16 * g4);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int b = min(max(keep - 4 * k, 0), 4);
+        const uint32_t mask = b == 4 ? ~0u : (1u << (8 * b)) - 1u;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) vreg[dt][k] &= mask;
+      }
+    }
+    bf16x8 pb[NC][2];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      float mx = kNegInf;
+#pragma unroll
+      for (int tt = 0; tt < 4; ++tt)
+        mx = fmaxf(mx, fmaxf(fmaxf(s[c][tt][0], s[c][tt][1]), fmaxf(s[c][tt][2], s[c][tt][3])));
+      mx = fmaxf(mx, wave_xor(mx, 16));
+      mx = fmaxf(mx, wave_xor(mx, 32));
+      if (__any(mx != kNegInf && (m[c] == kNegInf || mx * cs > mc[c] + 8.f))) {
+        const float mnew = fmaxf(m[c], mx);
+        const float mcn = mnew == kNegInf ? 0.f : mnew * cs;
+        const float alpha = m[c] == kNegInf ? 0.f : fast_exp2(mc[c] - mcn);
+        l[c] *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) acc[c][dt] *= alpha;
+        m[c] = mnew;
+        mc[c] = mcn;
+      }
+#pragma unroll
+      for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p = fast_exp2(fmaf(s[c][tt][e], cs, -mc[c]));
+          l[c] += p;
+          pb[c][tt >> 1][4 * (tt & 1) + e] = (__bf16)p;
+        }
+    }
+    const float sv = scale8(ev);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const bf16x8 v = as_bf16x8(bf16_of_e4m3(vreg[dt][2 * u], vreg[dt][2 * u + 1], sv));
+#pragma unroll
+        for (int c = 0; c < NC; ++c) acc[c][dt] = mfma16(v, pb[c][u], acc[c][dt]);
+      }
+    if (more) load_v(t0 + kStep);
+  }
+
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    l[c] += wave_xor(l[c], 16);
+    l[c] += wave_xor(l[c], 32);
+  }
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+    if (valid[c]) store_row<D>(a, acc[c], l[c], mc[c], qs + qi[c], hq[c], part < 0 ? -1 : part + 16 * c + j, g4);
+}
+
 // MIX bits: 1 = tile and shared items, 2 = row items of at most 16 rows,
 // 4 = row items of up to 32 rows, 8 = wildcard workgroups (tail lists).
 // Separate instantiations keep a pure prefill or pure decode launch from
@@ -756,7 +1097,7 @@ constexpr int waves_per_eu() {
   return MIX == 2 || D == 64 ? 3 : kTileWavesPerEu;
 }
 
-template <int D, int MIX>
+template <int D, int MIX, bool KV8 = false>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(waves_per_eu<D, MIX>()))) void attn_bf16_kernel(AttnArgs a) {
   const int32_t* plan = a.plan;
   // this workgroup's kv-head and template (the dispatch list follows the
@@ -794,7 +1135,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(waves_per_e
         auto run = [&](int q, int c) {
           const int tw = plan[tab[q] + c];
           const int tg = tw >> kDispatchHeadShift;
-          tile_item<D, kTileSub, false, true>(tiles + (tw & kDispatchIndexMask) * kItemWords, tg,
+          tile_item<D, kTileSub, KV8, false, true>(tiles + (tw & kDispatchIndexMask) * kItemWords, tg,
                                               tg * plan[H_HEAD_PARTIAL], a, sm);
         };
         for (;;) {
@@ -842,17 +1183,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(waves_per_e
     }
     if (ti < n_shared) {
       const int32_t* it = plan + plan[H_SHARED_OFF] + ti * kSharedWords;
-      if (it[S_NROWS] > kTileRows - 32) tile_item<D, kTileSub, true, true>(it, g, poff, a, sm);
-      else tile_item<D, kTileSub, true, false>(it, g, poff, a, sm);
+      if (it[S_NROWS] > kTileRows - 32) tile_item<D, kTileSub, KV8, true, true>(it, g, poff, a, sm);
+      else tile_item<D, kTileSub, KV8, true, false>(it, g, poff, a, sm);
       return;
     }
     if (ti < n_tile) {
       const int32_t* it = plan + plan[H_TILE_OFF] + (ti - n_shared) * kItemWords;
       // every wavefront has rows: the plain path; otherwise idle ones skip
       // compute, and a few-row sequence's private keys are streamed
-      if (it[I_NROWS] > kTileRows - 32) tile_item<D, kTileSub, false, true>(it, g, poff, a, sm);
-      else if (it[I_FLAGS] & kItemStream) tile_item<D, kTileSub, false, false, true>(it, g, poff, a, sm);
-      else tile_item<D, kTileSub, false, false>(it, g, poff, a, sm);
+      if (it[I_NROWS] > kTileRows - 32) tile_item<D, kTileSub, KV8, false, true>(it, g, poff, a, sm);
+      else if (it[I_FLAGS] & kItemStream) tile_item<D, kTileSub, KV8, false, false, true>(it, g, poff, a, sm);
+      else tile_item<D, kTileSub, KV8, false, false>(it, g, poff, a, sm);
       return;
     }
   }
@@ -863,11 +1204,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(waves_per_e
           plan + plan[H_ROW_OFF] + (ti - n_tile + (threadIdx.x >> 6)) * kItemWords;
       if constexpr ((MIX & 4) != 0) {
         if (it[I_NROWS] > 16) {
-          row_item<D, 2>(it, g, poff, a);
+          if constexpr (KV8) row_item8<D, 2>(it, g, poff, a);
+          else row_item<D, 2>(it, g, poff, a);
           return;
         }
       }
-      row_item<D, 1>(it, g, poff, a);
+      if constexpr (KV8) row_item8<D, 1>(it, g, poff, a);
+      else row_item<D, 1>(it, g, poff, a);
     }
   }
 }
@@ -965,7 +1308,7 @@ __global__ __launch_bounds__(kMergeRows * 32) void merge_kernel(AttnArgs a) {
 
 }  // namespace
 
-int launch_attn_bf16(const void* q, const void* kc, const void* vc, int32_t num_blocks,
+int launch_attn_bf16(const void* q, const void* kc, const void* vc, const uint8_t* scales, int32_t num_blocks,
                      const int32_t* bt, int32_t max_blocks, const int32_t* seq_lens,
                      const int32_t* cu_q, int32_t hq, int32_t hkv, int32_t d, float scale,
                      const int32_t* plan, int32_t grid, int32_t n_tile, int32_t n_merge,
@@ -975,6 +1318,7 @@ int launch_attn_bf16(const void* q, const void* kc, const void* vc, int32_t num_
   a.q = static_cast<const __bf16*>(q);
   a.kc = static_cast<const __bf16*>(kc);
   a.vc = static_cast<const __bf16*>(vc);
+  a.scales = scales;
   a.bt = bt;
   a.seq_lens = seq_lens;
   a.cu_q = cu_q;
@@ -998,22 +1342,30 @@ int launch_attn_bf16(const void* q, const void* kc, const void* vc, int32_t num_
     // the caller's timing events ride on the dispatches (start on the first
     // kernel, stop on the last): no event packets between the kernels
     hipEvent_t stop_here = n_merge > 0 ? nullptr : ev_stop;
-#define PA_LAUNCH(DD, MM)                                                                     \
-  hipExtLaunchKernelGGL((attn_bf16_kernel<DD, MM>), dim3(grid), dim3(256), 0, stream, ev_start, \
+#define PA_LAUNCH(DD, MM, K8)                                                                 \
+  hipExtLaunchKernelGGL((attn_bf16_kernel<DD, MM, K8>), dim3(grid), dim3(256), 0, stream, ev_start, \
                         stop_here, 0, a)
-#define PA_LAUNCH_D(DD)                      \
-  switch (mix) {                             \
-    case 1: PA_LAUNCH(DD, 1); break;         \
-    case 2: PA_LAUNCH(DD, 2); break;         \
-    case 6: PA_LAUNCH(DD, 6); break;         \
-    case 9: PA_LAUNCH(DD, 9); break;         \
-    case 15: PA_LAUNCH(DD, 15); break;       \
-    default: PA_LAUNCH(DD, 7); break;        \
+#define PA_LAUNCH_D(DD, K8)                      \
+  switch (mix) {                                 \
+    case 1: PA_LAUNCH(DD, 1, K8); break;         \
+    case 2: PA_LAUNCH(DD, 2, K8); break;         \
+    case 6: PA_LAUNCH(DD, 6, K8); break;         \
+    case 9: PA_LAUNCH(DD, 9, K8); break;         \
+    case 15: PA_LAUNCH(DD, 15, K8); break;       \
+    default: PA_LAUNCH(DD, 7, K8); break;        \
   }
     if (d == 128) {
-      PA_LAUNCH_D(128);
+      if (scales) {
+        PA_LAUNCH_D(128, true);
+      } else {
+        PA_LAUNCH_D(128, false);
+      }
     } else {
-      PA_LAUNCH_D(64);
+      if (scales) {
+        PA_LAUNCH_D(64, true);
+      } else {
+        PA_LAUNCH_D(64, false);
+      }
     }
 #undef PA_LAUNCH_D
 #undef PA_LAUNCH

@@ -331,7 +331,7 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
     return pa::fail(PA_ERR_UNSUPPORTED, "pa_attn_plan: head_dim %d (supported: 64, 128)", head_dim);
   if (block_size != 16)
     return pa::fail(PA_ERR_UNSUPPORTED, "pa_attn_plan: block_size %d (supported: 16)", block_size);
-  if (dtype != PA_F32 && dtype != PA_BF16)
+  if (dtype != PA_F32 && dtype != PA_BF16 && dtype != PA_BF16_KV8)
     return pa::fail(PA_ERR_UNSUPPORTED, "pa_attn_plan: dtype %d", dtype);
   if (block_table && max_blocks_per_seq < 1)
     return pa::fail(PA_ERR_ARG, "pa_attn_plan: max_blocks_per_seq %d < 1", max_blocks_per_seq);
@@ -377,7 +377,7 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
   std::array<std::vector<Ref>, pa::kXcdQueues> tail;
   int64_t n_shared_wg = 0, n_tile_wg = 0, n_quads = 0;
 
-  if (dtype == PA_BF16) {
+  if (dtype != PA_F32) {
     auto qlen = [&](int32_t r) { return cu_seqlens_q[r + 1] - cu_seqlens_q[r]; };
     // Sequences with few rows (decode, verification) get split key ranges and
     // may join a cascade group.  Their private keys run on one single-wave
@@ -853,7 +853,7 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
   const int64_t group_off = row_off + int64_t(sorted_rows.size()) * pa::kItemWords;
   const int64_t member_off = group_off + int64_t(t_groups.size()) * pa::kGroupWords;
   const int64_t words = member_off + head_members;
-  if (dtype == PA_BF16 &&
+  if (dtype != PA_F32 &&
       (num_kv_heads >= (1 << (31 - pa::kDispatchHeadShift)) ||
        t_shared.size() + t_tiles.size() + sorted_rows.size() >= size_t(pa::kWildcard)))
     return pa::fail(PA_ERR_ARG, "pa_attn_plan: launch too large");
@@ -921,7 +921,7 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
   h[pa::H_N_WILD] = int32_t(n_tail);  // one wildcard per tail item
   h[pa::H_CTR_OFF] = int32_t(ctr_off);
   h[pa::H_N_GROUP_NARROW] = int32_t(n_narrow);
-  if (dtype == PA_BF16) {
+  if (dtype != PA_F32) {
     int32_t* p = plan + dispatch_off;
     auto word = [](const Ref& r) { return (r.first << pa::kDispatchHeadShift) | r.second; };
     for (const auto& r : dispatch) *p++ = word(r);

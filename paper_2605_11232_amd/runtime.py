@@ -119,18 +119,27 @@ class Staging:
 
 class DeviceReplay:
     def __init__(self, wl, device: str = "cuda", kind: str | None = None, num_cus: int = 0,
-                 cascade: bool = True, stage_kernel: bool = True):
+                 cascade: bool = True, stage_kernel: bool = True, kv8: bool = False):
         cfg = wl.cfg
         self.wl, self.cfg, self.device = wl, cfg, torch.device(device)
         self.tdtype = torch_dtype(cfg.dtype)
         self.dcode = B.PA_BF16 if cfg.dtype == "bf16" else B.PA_F32
+        self.kv8 = kv8  # an 8-bit cache (bf16 queries)
         self.pool = B.Pool(wl.num_blocks, cfg.block_size, wl.free_order, evict=wl.evict)
         # keys in the grouped layout [block][head][dim / 32][slot position][32]
         shape_k = (wl.num_blocks, cfg.num_kv_heads, cfg.head_dim // 32, cfg.block_size, 32)
         shape_v = (wl.num_blocks, cfg.num_kv_heads, cfg.head_dim, cfg.block_size)
         # Uninitialised on purpose: the kernels must never read unwritten slots.
-        self.k_cache = torch.empty(shape_k, dtype=self.tdtype, device=self.device)
-        self.v_cache = torch.empty(shape_v, dtype=self.tdtype, device=self.device)
+        cdtype = self.tdtype
+        if kv8:
+            if cfg.dtype != "bf16":
+                raise ValueError("an 8-bit cache takes bf16 queries")
+            self.dcode, cdtype = B.PA_BF16_KV8, torch.float8_e4m3fn
+            shape_k, shape_v, shape_s = B.kv8_cache_shapes(wl.num_blocks, cfg.num_kv_heads,
+                                                           cfg.head_dim, cfg.block_size)
+            self.scales = torch.empty(shape_s, dtype=torch.uint8, device=self.device)
+        self.k_cache = torch.empty(shape_k, dtype=cdtype, device=self.device)
+        self.v_cache = torch.empty(shape_v, dtype=cdtype, device=self.device)
         self.kind = kind
         self.num_cus = num_cus
         self.cascade = cascade
@@ -146,7 +155,12 @@ class DeviceReplay:
         slots = torch.from_numpy(md["slot_mapping"]).to(dev)
         kt = torch.from_numpy(k).to(dev, self.tdtype)
         vt = torch.from_numpy(v).to(dev, self.tdtype)
-        B.kv_append(kt, vt, slots, self.k_cache, self.v_cache)
+        if self.kv8:
+            bt, sl, cu = (torch.from_numpy(md[k]).to(dev)
+                          for k in ("block_table", "seq_lens", "cu_seqlens_q"))
+            B.kv8_append(kt, vt, bt, sl, cu, self.k_cache, self.v_cache, self.scales)
+        else:
+            B.kv_append(kt, vt, slots, self.k_cache, self.v_cache)
 
     def apply(self, op):
         p = self.pool
@@ -286,7 +300,11 @@ class DeviceReplay:
         """KV append of the launch; records the caller's staging guard after
         it unless record_guard is False (the guard is then the start event the
         caller hands to ``attend``)."""
-        B.kv_append(p.k_new, p.v_new, p.slots, self.k_cache, self.v_cache, stream)
+        if self.kv8:
+            B.kv8_append(p.k_new, p.v_new, p.block_table, p.seq_lens, p.cu, self.k_cache,
+                         self.v_cache, self.scales, stream)
+        else:
+            B.kv_append(p.k_new, p.v_new, p.slots, self.k_cache, self.v_cache, stream)
         guard = getattr(p, "guard", None)
         if guard is not None and record_guard:
             guard.record(stream)
@@ -296,6 +314,11 @@ class DeviceReplay:
         last kernel dispatches (pa_set_launch_events)."""
         if events is not None:
             B.set_launch_events(*events)
+        if self.kv8:
+            B.kv8_attention(KIND[p.kind], p.q, self.k_cache, self.v_cache, self.scales,
+                            p.block_table, p.seq_lens, p.cu, p.plan, p.info, p.ws, p.out, p.lse,
+                            stream=stream)
+            return
         B.attention(KIND[p.kind], p.q, self.k_cache, self.v_cache, p.block_table, p.seq_lens, p.cu,
                     p.plan, p.info, p.ws, p.out, p.lse, stream=stream)
 
