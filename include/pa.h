@@ -587,7 +587,7 @@ int pa_kv8_attn_decode_noalloc(const void* q, const void* k_cache, const void* v
  * dtype.  Either head count may be 0 (its pointers are then not read).
  * All pointers are caller-owned device memory; asynchronous on stream;
  * allocates nothing.  Errors: PA_ERR_ARG (NULL pointer with rows to do, bad
- * sizes, strides, flags or eps, rows or weights not 16-byte aligned),
+ * sizes, strides, flags or eps, rows, weights or table not 16-byte aligned),
  * PA_ERR_UNSUPPORTED (head_dim, dtype), PA_ERR_LAUNCH. */
 enum { PA_QK_NORM = 1, PA_ROPE_INTERLEAVED = 2 };
 int pa_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stride,

@@ -620,52 +620,104 @@ def kv8_cache_shapes(num_blocks: int, num_kv_heads: int, head_dim: int, block_si
             (num_blocks, num_kv_heads, head_dim, block_size), (num_blocks, num_kv_heads, 2))
 
 
-def kv8_cache_dims(k_cache, v_cache, scales):
-    """(num_blocks, num_kv_heads, head_dim, block_size) of an 8-bit cache."""
+# The calls below check every tensor they take (types, shapes, strides, device): a
+# kernel given the wrong one reads past its buffers.  The checks are one expression
+# of attribute reads; what is wrong is looked for only when it fails, as a call of
+# few rows waits for the host (an append's checks and marshalling 9.5 us written
+# plainly, 5 so, where the kernel takes 4).
+def _refuse(code: int, checks):
+    """Raise for the first (holds, message) that does not hold."""
+    for holds, msg in checks:
+        if not holds:
+            raise PaError(code, msg)
+
+
+def _refuse_cache(t, k_cache, v_cache, scales):
     nb, hkv, d, bs = v_cache.shape
-    if k_cache.shape != (nb, hkv, d // 64, bs, 64) or scales.shape != (nb, hkv, 2):
-        raise PaError(PA_ERR_ARG, "8-bit cache: k_cache, v_cache and scales differ in shape")
-    t = _torch or _torch_module()
-    if not (k_cache.dtype == v_cache.dtype == t.float8_e4m3fn and scales.dtype == t.uint8):
-        raise PaError(PA_ERR_UNSUPPORTED, f"8-bit cache of {k_cache.dtype}, {v_cache.dtype} and "
-                      f"{scales.dtype} (supported: float8_e4m3fn with uint8 scales)")
-    if not (k_cache.is_contiguous() and v_cache.is_contiguous() and scales.is_contiguous()):
-        raise PaError(PA_ERR_ARG, "8-bit cache: tensors must be contiguous")
-    return nb, hkv, d, bs
+    _refuse(PA_ERR_UNSUPPORTED, [(
+        k_cache.dtype == v_cache.dtype == t.float8_e4m3fn and scales.dtype == t.uint8,
+        f"8-bit cache of {k_cache.dtype}, {v_cache.dtype} and {scales.dtype} (supported: "
+        "float8_e4m3fn with uint8 scales)")])
+    _refuse(PA_ERR_ARG, [
+        (k_cache.shape == (nb, hkv, d // 64, bs, 64) and scales.shape == (nb, hkv, 2),
+         "8-bit cache: k_cache, v_cache and scales differ in shape"),
+        (k_cache.is_contiguous() and v_cache.is_contiguous() and scales.is_contiguous(),
+         "8-bit cache: tensors must be contiguous")])
 
 
-def _row_stride(t, heads: int, d: int, what: str) -> int:
-    """Elements between the rows of a [T, heads, d] tensor whose rows are packed
-    (a slice of a larger matrix's columns is)."""
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d:
-        raise PaError(PA_ERR_ARG, f"{what}: shape {tuple(t.shape)}, expected [T, {heads}, {d}]")
-    s = t.stride()
-    if t.numel() and ((d > 1 and s[2] != 1) or (heads > 1 and s[1] != d)):
-        raise PaError(PA_ERR_ARG, f"{what}: a row's heads must be packed")
-    return s[0] if t.shape[0] > 1 else heads * d
-
-
-def _metadata(block_table, seq_lens, cu_seqlens):
-    """Checked (block table pointer, its width, seq_lens, cu_seqlens, n_seqs)."""
-    t = _torch or _torch_module()
+def _refuse_metadata(t, block_table, seq_lens, cu_seqlens):
     n = seq_lens.numel()
-    if block_table.dim() != 2 or block_table.shape[0] < n or cu_seqlens.numel() < n + 1:
-        raise PaError(PA_ERR_ARG, f"metadata of {n} sequences: block_table "
-                      f"{tuple(block_table.shape)}, cu_seqlens {cu_seqlens.numel()}")
-    for m in (block_table, seq_lens, cu_seqlens):
-        if m.dtype != t.int32 or not m.is_contiguous():
-            raise PaError(PA_ERR_ARG, "metadata must be contiguous int32")
-    return _dptr(block_table), block_table.shape[1], _dptr(seq_lens), _dptr(cu_seqlens), n
+    _refuse(PA_ERR_ARG, [
+        (block_table.dim() == 2 and block_table.shape[0] >= n and cu_seqlens.numel() > n,
+         f"metadata of {n} sequences: block_table {tuple(block_table.shape)}, cu_seqlens "
+         f"{cu_seqlens.numel()}"),
+        (all(m.dtype == t.int32 and m.is_contiguous()
+             for m in (block_table, seq_lens, cu_seqlens)),
+         "metadata must be contiguous int32")])
+
+
+def _refuse_device(*tensors):
+    t = _torch or _torch_module()
+    now = t.cuda.current_device() if t.cuda.is_available() else None
+    for x in tensors:
+        if x is not None and x.get_device() != now:
+            raise PaError(PA_ERR_ARG, f"tensor on {x.device}: all tensors must be on the current "
+                          f"GPU ({now})")
+
+
+def _stream_on(device: int, stream) -> int:
+    """The stream's handle, or the current one's; -1 where the current device is
+    not ``device``."""
+    t = _torch
+    if device < 0 or t.cuda.current_device() != device:
+        return -1
+    if stream is None:
+        return t._C._cuda_getCurrentRawStream(device)
+    return int(getattr(stream, "cuda_stream", stream))
+
+
+def _packed_rows(t, T: int, heads: int, d: int):
+    """Elements between the rows of [T, heads, d] tensor t if each row's heads are
+    packed (a column slice of a larger matrix, too), else None."""
+    if t.dim() != 3 or t.shape != (T, heads, d):
+        return None
+    s0, s1, s2 = t.stride()
+    if T and heads and not (s2 == 1 and (s1 == d or heads == 1)):
+        return None
+    return s0 if T > 1 else heads * d
 
 
 def _kv8_rows(fn, k, v, block_table, seq_lens, cu_seqlens, k_cache, v_cache, scales, stream):
-    nb, hkv, d, bs = kv8_cache_dims(k_cache, v_cache, scales)
-    if k.shape[0] != v.shape[0] or k.dtype != v.dtype:
-        raise PaError(PA_ERR_ARG, "keys and values differ in rows or dtype")
-    ks, vs = _row_stride(k, hkv, d, "keys"), _row_stride(v, hkv, d, "values")
-    _check(fn(_dptr(k), ks, _dptr(v), vs, *_metadata(block_table, seq_lens, cu_seqlens),
-              k.shape[0], _dptr(k_cache), _dptr(v_cache), _dptr(scales), nb, hkv, d, bs,
-              _dtype_code(k), _stream(stream)))
+    t = _torch or _torch_module()
+    nb, hkv, d, bs = v_cache.shape
+    T, n, i32, e4m3 = k.shape[0], seq_lens.numel(), t.int32, t.float8_e4m3fn
+    ks, vs = _packed_rows(k, T, hkv, d), _packed_rows(v, T, hkv, d)
+    rows, width = block_table.shape if block_table.dim() == 2 else (-1, 0)
+    dev = v_cache.get_device()
+    st = _stream_on(dev, stream)
+    if not (ks is not None and vs is not None and k.dtype == v.dtype
+            and k_cache.dtype == e4m3 and v_cache.dtype == e4m3 and scales.dtype == t.uint8
+            and k_cache.shape == (nb, hkv, d // 64, bs, 64) and scales.shape == (nb, hkv, 2)
+            and k_cache.is_contiguous() and v_cache.is_contiguous() and scales.is_contiguous()
+            and rows >= n and cu_seqlens.numel() > n
+            and block_table.dtype == i32 and seq_lens.dtype == i32 and cu_seqlens.dtype == i32
+            and block_table.is_contiguous() and seq_lens.is_contiguous()
+            and cu_seqlens.is_contiguous()
+            and st >= 0 and k.get_device() == v.get_device() == k_cache.get_device()
+            == scales.get_device() == block_table.get_device() == seq_lens.get_device()
+            == cu_seqlens.get_device() == dev):
+        _refuse_cache(t, k_cache, v_cache, scales)
+        _refuse(PA_ERR_ARG, [
+            (ks is not None and vs is not None,
+             f"rows {tuple(k.shape)} of strides {k.stride()} and {tuple(v.shape)} of "
+             f"{v.stride()}, expected [T, {hkv}, {d}] with a row's heads packed"),
+            (k.dtype == v.dtype, "keys and values differ in dtype")])
+        _refuse_metadata(t, block_table, seq_lens, cu_seqlens)
+        _dtype_code(k)
+        _refuse_device(k, v, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlens)
+    _check(fn(k.data_ptr(), ks, v.data_ptr(), vs, block_table.data_ptr(), width,
+              seq_lens.data_ptr(), cu_seqlens.data_ptr(), n, T, k_cache.data_ptr(),
+              v_cache.data_ptr(), scales.data_ptr(), nb, hkv, d, bs, _dtype_code(k), st))
 
 
 def kv8_append(k_new, v_new, block_table, seq_lens, cu_seqlens, k_cache, v_cache, scales,
@@ -686,21 +738,54 @@ def kv8_read(k_out, v_out, block_table, seq_lens, cu_seqlens, k_cache, v_cache, 
 
 
 def _kv8_attn_args(q, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlens_q, plan_dev,
-                   info, out, lse, scale):
-    nb, hkv, d, bs = kv8_cache_dims(k_cache, v_cache, scales)
-    total_q, hq, dq = q.shape
+                   info, out, lse, scale, stream, workspace):
+    """(arguments up to the plan info, stream) of a call over the 8-bit cache."""
     t = _torch or _torch_module()
-    if q.dtype != t.bfloat16 or out.dtype != t.bfloat16:
-        raise PaError(PA_ERR_UNSUPPORTED, f"queries {q.dtype}, output {out.dtype} (supported: bf16)")
-    if dq != d or out.shape != q.shape or not (q.is_contiguous() and out.is_contiguous()):
-        raise PaError(PA_ERR_ARG, "q and out must be contiguous [T, Hq, D] of the cache's head_dim")
-    if lse is not None and (lse.dtype != t.float32 or lse.shape != (total_q, hq)
-                            or not lse.is_contiguous()):
-        raise PaError(PA_ERR_ARG, "lse must be contiguous float32 [T, Hq]")
-    bt, width, sl, cu, n = _metadata(block_table, seq_lens, cu_seqlens_q)
-    return (_dptr(q), _dptr(k_cache), _dptr(v_cache), _dptr(scales), nb, bt, width, sl, cu, n,
-            total_q, hq, hkv, d, bs, float(d ** -0.5 if scale is None else scale),
-            _dptr(plan_dev), C.byref(info))
+    nb, hkv, d, bs = v_cache.shape
+    total_q, hq, dq = q.shape
+    n, i32, e4m3 = seq_lens.numel(), t.int32, t.float8_e4m3fn
+    rows, width = block_table.shape if block_table.dim() == 2 else (-1, 0)
+    dev = v_cache.get_device()
+    st = _stream_on(dev, stream)
+    if not (q.dtype == t.bfloat16 and out.dtype == t.bfloat16 and dq == d
+            and out.shape == q.shape and q.is_contiguous() and out.is_contiguous()
+            and k_cache.dtype == e4m3 and v_cache.dtype == e4m3 and scales.dtype == t.uint8
+            and k_cache.shape == (nb, hkv, d // 64, bs, 64) and scales.shape == (nb, hkv, 2)
+            and k_cache.is_contiguous() and v_cache.is_contiguous() and scales.is_contiguous()
+            and rows >= n and cu_seqlens_q.numel() > n
+            and block_table.dtype == i32 and seq_lens.dtype == i32 and cu_seqlens_q.dtype == i32
+            and block_table.is_contiguous() and seq_lens.is_contiguous()
+            and cu_seqlens_q.is_contiguous()
+            and plan_dev.dtype == i32 and plan_dev.numel() >= info.plan_words
+            and plan_dev.is_contiguous()
+            and (lse is None or (lse.dtype == t.float32 and lse.shape == (total_q, hq)
+                                 and lse.is_contiguous() and lse.get_device() == dev))
+            and (workspace is None or (workspace.is_contiguous()
+                                       and workspace.get_device() == dev))
+            and st >= 0 and q.get_device() == out.get_device() == k_cache.get_device()
+            == scales.get_device() == block_table.get_device() == seq_lens.get_device()
+            == cu_seqlens_q.get_device() == plan_dev.get_device() == dev):
+        _refuse_cache(t, k_cache, v_cache, scales)
+        _refuse(PA_ERR_UNSUPPORTED, [
+            (q.dtype == out.dtype == t.bfloat16,
+             f"queries {q.dtype}, output {out.dtype} (supported: bfloat16)")])
+        _refuse(PA_ERR_ARG, [
+            (dq == d and out.shape == q.shape and q.is_contiguous() and out.is_contiguous(),
+             "q and out must be contiguous [T, Hq, D] of the cache's head_dim"),
+            (lse is None or (lse.dtype == t.float32 and lse.shape == (total_q, hq)
+                             and lse.is_contiguous()), "lse must be contiguous float32 [T, Hq]"),
+            (plan_dev.dtype == i32 and plan_dev.is_contiguous()
+             and plan_dev.numel() >= info.plan_words,
+             f"plan: {plan_dev.numel()} words of {plan_dev.dtype}, its info says "
+             f"{info.plan_words} of int32"),
+            (workspace is None or workspace.is_contiguous(), "workspace must be contiguous")])
+        _refuse_metadata(t, block_table, seq_lens, cu_seqlens_q)
+        _refuse_device(q, out, lse, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlens_q,
+                       plan_dev, workspace)
+    return (q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), scales.data_ptr(), nb,
+            block_table.data_ptr(), width, seq_lens.data_ptr(), cu_seqlens_q.data_ptr(), n,
+            total_q, hq, hkv, d, bs, d ** -0.5 if scale is None else scale, plan_dev.data_ptr(),
+            C.byref(info)), st
 
 
 def kv8_attention(kind: int, q, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlens_q,
@@ -709,19 +794,20 @@ def kv8_attention(kind: int, q, k_cache, v_cache, scales, block_table, seq_lens,
     ``kind``), with a plan built for PA_BF16_KV8."""
     if _lib is None:
         lib()
+    args, st = _kv8_attn_args(q, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlens_q,
+                              plan_dev, info, out, lse, scale, stream, workspace)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(_kv8_attn[kind](*_kv8_attn_args(q, k_cache, v_cache, scales, block_table, seq_lens,
-                                           cu_seqlens_q, plan_dev, info, out, lse, scale),
-                           _dptr(workspace), ws_bytes, _dptr(out), _dptr(lse), _stream(stream)))
+    _check(_kv8_attn[kind](*args, _dptr(workspace), ws_bytes, out.data_ptr(), _dptr(lse), st))
 
 
 def kv8_attention_decode_noalloc(q, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlens_q,
                                  plan_dev, info: PlanInfo, out, lse=None, scale=None, stream=None):
     """Decode over the 8-bit cache with the split-K partials in the library's
     per-device array (as attention_decode_noalloc)."""
-    _check((_lib or lib()).pa_kv8_attn_decode_noalloc(
-        *_kv8_attn_args(q, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlens_q, plan_dev,
-                        info, out, lse, scale), _dptr(out), _dptr(lse), _stream(stream)))
+    fn = (_lib or lib()).pa_kv8_attn_decode_noalloc
+    args, st = _kv8_attn_args(q, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlens_q,
+                              plan_dev, info, out, lse, scale, stream, None)
+    _check(fn(*args, out.data_ptr(), _dptr(lse), st))
 
 
 def qk_norm_rope(q, k, positions, cos_sin, q_out, k_out, q_weight=None, k_weight=None,
@@ -730,24 +816,40 @@ def qk_norm_rope(q, k, positions, cos_sin, q_out, k_out, q_weight=None, k_weight
     (rows at any stride) by their int32 positions and the float32 table cos_sin
     [n_positions, rot_dim] (cosines, then sines), into packed q_out and k_out."""
     t = _torch or _torch_module()
+    fn = (_lib or lib()).pa_qk_norm_rope
     T, hq, d = q.shape
-    if k.dim() != 3 or k.shape[0] != T:
-        raise PaError(PA_ERR_ARG, f"k: shape {tuple(k.shape)}, expected [{T}, Hkv, {d}]")
     hkv = k.shape[1]
-    for x, w, what in ((q_out, hq, "q_out"), (k_out, hkv, "k_out")):
-        if x.shape != (T, w, d) or not x.is_contiguous() or x.dtype != q.dtype:
-            raise PaError(PA_ERR_ARG, f"{what} must be contiguous [{T}, {w}, {d}] of q's dtype")
-    for w, what in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        if w is not None and (w.numel() != d or w.dtype != q.dtype or not w.is_contiguous()):
-            raise PaError(PA_ERR_ARG, f"{what} must be {d} contiguous values of q's dtype")
-    if k.dtype != q.dtype or positions.numel() != T or positions.dtype != t.int32 or \
-            not positions.is_contiguous():
-        raise PaError(PA_ERR_ARG, "k of q's dtype and one contiguous int32 position per token")
-    if cos_sin.dim() != 2 or cos_sin.dtype != t.float32 or not cos_sin.is_contiguous():
-        raise PaError(PA_ERR_ARG, "cos_sin must be contiguous float32 [n_positions, rot_dim]")
-    _check((_lib or lib()).pa_qk_norm_rope(
-        _dptr(q), _row_stride(q, hq, d, "q"), _dptr(k), _row_stride(k, hkv, d, "k"),
-        _dptr(positions), T, _dptr(cos_sin), cos_sin.shape[0], cos_sin.shape[1], _dptr(q_weight),
-        _dptr(k_weight), float(eps),
-        (QK_NORM if norm else 0) | (ROPE_INTERLEAVED if interleaved else 0), _dptr(q_out),
-        _dptr(k_out), hq, hkv, d, _dtype_code(q), _stream(stream)))
+    qs, ks = _packed_rows(q, T, hq, d), _packed_rows(k, T, hkv, d)
+    dt, dev = q.dtype, q_out.get_device()
+    st = _stream_on(dev, stream)
+    n_pos, rot = cos_sin.shape if cos_sin.dim() == 2 else (-1, 0)
+    if not (qs is not None and ks is not None and k.dtype == dt
+            and q_out.dtype == dt and q_out.shape == (T, hq, d) and q_out.is_contiguous()
+            and k_out.dtype == dt and k_out.shape == (T, hkv, d) and k_out.is_contiguous()
+            and positions.dtype == t.int32 and positions.numel() == T
+            and positions.is_contiguous() and n_pos >= 0 and cos_sin.dtype == t.float32
+            and cos_sin.is_contiguous()
+            and all([w is None or (w.dtype == dt and w.numel() == d and w.is_contiguous()
+                                   and w.get_device() == dev) for w in (q_weight, k_weight)])
+            and st >= 0 and q.get_device() == k.get_device() == k_out.get_device()
+            == positions.get_device() == cos_sin.get_device() == dev):
+        _refuse(PA_ERR_ARG, [
+            (qs is not None and ks is not None,
+             f"q {tuple(q.shape)} of strides {q.stride()} and k {tuple(k.shape)} of "
+             f"{k.stride()}: expected [T, Hq, D] and [T, Hkv, D] with a row's heads packed"),
+            (k.dtype == dt, "q and k differ in dtype")]
+            + [(x.shape == (T, h, d) and x.is_contiguous() and x.dtype == dt,
+                f"{what} must be contiguous [{T}, {h}, {d}] of q's dtype")
+               for x, h, what in ((q_out, hq, "q_out"), (k_out, hkv, "k_out"))]
+            + [(w is None or (w.numel() == d and w.dtype == dt and w.is_contiguous()),
+                f"{what} must be {d} contiguous values of q's dtype")
+               for w, what in ((q_weight, "q_weight"), (k_weight, "k_weight"))]
+            + [(positions.numel() == T and positions.dtype == t.int32
+                and positions.is_contiguous(), "one contiguous int32 position per token"),
+               (n_pos >= 0 and cos_sin.dtype == t.float32 and cos_sin.is_contiguous(),
+                "cos_sin must be contiguous float32 [n_positions, rot_dim]")])
+        _refuse_device(q, k, q_out, k_out, positions, cos_sin, q_weight, k_weight)
+    _check(fn(q.data_ptr(), qs, k.data_ptr(), ks, positions.data_ptr(), T, cos_sin.data_ptr(),
+              n_pos, rot, _dptr(q_weight), _dptr(k_weight), eps,
+              (QK_NORM if norm else 0) | (ROPE_INTERLEAVED if interleaved else 0),
+              q_out.data_ptr(), k_out.data_ptr(), hq, hkv, d, _dtype_code(q), st))

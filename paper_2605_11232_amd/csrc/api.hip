@@ -374,8 +374,8 @@ int pa_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_st
   if ((num_q_heads > 0 && (!pa::aligned16(q, q_stride, dtype) || !pa::aligned16(q_out, 0, dtype))) ||
       (num_kv_heads > 0 && (!pa::aligned16(k, k_stride, dtype) || !pa::aligned16(k_out, 0, dtype))) ||
       !pa::aligned16(q_weight, 0, dtype) || !pa::aligned16(k_weight, 0, dtype) ||
-      (reinterpret_cast<uintptr_t>(cos_sin) & 3))
-    return fail(PA_ERR_ARG, "%s: rows and weights must be 16-byte aligned", fn);
+      !pa::aligned16(cos_sin, 0, PA_F32))
+    return fail(PA_ERR_ARG, "%s: rows, weights and the table must be 16-byte aligned", fn);
   const int rc = pa::dev::launch_qk_norm_rope(
       q, q_stride, k, k_stride, positions, n_tokens, cos_sin, n_positions, rot_dim, q_weight,
       k_weight, eps, flags, q_out, k_out, num_q_heads, num_kv_heads, head_dim, dtype,

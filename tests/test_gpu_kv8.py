@@ -396,6 +396,9 @@ ROPE = [
     (13, 4, 0, 128, 128, False, True, "bf16", False),
     (13, 0, 3, 64, 48, False, True, "f32", False),
     (40, 64, 8, 64, 16, True, True, "bf16", True),
+    # enough rows for two of them a lane, heads that do not fill the last wavefront
+    (3600, 33, 4, 128, 128, False, True, "bf16", True),
+    (7200, 33, 4, 64, 32, True, False, "bf16", False),
 ]
 
 
