@@ -918,7 +918,7 @@ template <int D, int NC>
 __device__ __forceinline__ void row_item8(const int32_t* it, int g, int poff, const AttnArgs& a) {
   constexpr int KC = D / 64;  // 64-dim groups of a key
   constexpr int DT = D / 16;  // 16-row tiles of O^T
-  constexpr int kStep = 64;
+  constexpr int kStep = kKeyStep8;
   const int r = it[I_SEQ];
   if (r < 0) return;
   const int row0 = it[I_ROW0], nrows = it[I_NROWS];

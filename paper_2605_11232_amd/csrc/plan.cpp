@@ -384,7 +384,13 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
     // row item per key range when it holds all their rows (at most 32), else
     // on tile items, whose four wavefronts share each key tile through LDS.
     auto is_row = [&](int32_t r) { return qlen(r) > 0 && qlen(r) * G <= pa::kRowSeqRows; };
-    auto on_tiles = [&](int32_t r) { return qlen(r) * G > pa::kRowItemRows; };
+    // Over the 8-bit cache those run as two row items that read the same keys.
+    const bool kv8 = dtype == PA_BF16_KV8;
+    bool few_tiles = !kv8;
+    auto on_tiles = [&](int32_t r) { return few_tiles && qlen(r) * G > pa::kRowItemRows; };
+    auto row_pieces = [&](int32_t r) { return cdiv(qlen(r) * G, pa::kRowItemRows); };
+    const int64_t row_step = kv8 ? pa::kKeyStep8 : pa::kKeyStep;
+    const double key_bytes = head_dim * (kv8 ? 2 : 4);  // a key and its value
 
     // Cascade groups: few-row sequences with the same first block and
     // q_len whose leading blocks coincide share those keys; attention over
@@ -434,17 +440,21 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
     // aim for enough single-wave items to keep kRowWavesPerCu wavefronts per
     // CU busy, a split target of at least kMinRowKeys and at most 1024 keys
     // per item (halved for the tail below).
-    int64_t row_keys = 0, long_tiles = 0, longest_row = 0;
+    int64_t row_keys = 0, item_keys = 0, long_tiles = 0, longest_row = 0;
     std::vector<FewTile> few;  // sequences on_tiles: private keys, rows
     for (int32_t r = 0; r < n_seqs; ++r) {
       const int64_t keys = seq_lens[r] - kstart[r];
       if (!is_row(r)) long_tiles += cdiv(int64_t(qlen(r)) * G, pa::kTileRows) * num_kv_heads;
       else if (on_tiles(r)) few.push_back({keys, int64_t(qlen(r)) * G, cgroup[r] >= 0});
-      else row_keys += keys * num_kv_heads, longest_row = std::max(longest_row, keys);
+      else {
+        row_keys += keys * num_kv_heads;
+        item_keys += keys * num_kv_heads * row_pieces(r);
+        longest_row = std::max(longest_row, keys);
+      }
     }
     const bool long_seqs = long_tiles > 0;
     // what the row items take, in steps of the whole chip
-    const double row_steps = double(row_keys) * head_dim * 4 / kStepBytes;
+    const double row_steps = double(row_keys) * key_bytes / kStepBytes;
     int64_t longest_prefix = 0;
     for (int32_t S : cg_keys) longest_prefix = std::max<int64_t>(longest_prefix, S);
     // Beside a shared prefix of several coarse chunks the items stay whole, as the
@@ -463,8 +473,8 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
     // private parts (the workspace bound).
     std::vector<int64_t> row_chunk;
     auto split_rows = [&](int64_t least) {
-      int64_t chunk = std::max<int64_t>(least, cdiv(row_keys, std::max<int64_t>(1, target_waves)));
-      chunk = cdiv(chunk, pa::kKeyStep) * pa::kKeyStep;
+      int64_t chunk = std::max<int64_t>(least, cdiv(item_keys, std::max<int64_t>(1, target_waves)));
+      chunk = cdiv(chunk, row_step) * row_step;
       // a row item's block ids fit one wavefront (64 lanes): at most 1024 keys
       chunk = std::min<int64_t>(chunk, int64_t(pa::kRowItemBlocks) * block_size);
       row_chunk.assign(n_seqs, chunk);
@@ -473,7 +483,7 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
       for (int32_t r = 0; r < n_seqs; ++r)
         if (is_row(r) && !on_tiles(r)) by_len.push_back({int64_t(seq_lens[r] - kstart[r]), r});
       std::sort(by_len.begin(), by_len.end());
-      const int64_t half = std::max<int64_t>(pa::kKeyStep, chunk / 2 / pa::kKeyStep * pa::kKeyStep);
+      const int64_t half = std::max<int64_t>(row_step, chunk / 2 / row_step * row_step);
       int64_t acc = 0;
       for (const auto& [len, r] : by_len) {
         acc += len * num_kv_heads;
@@ -497,7 +507,7 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
     };
     for (int32_t S : cg_keys) cg_chunks.push_back(int32_t(cdiv(S, pa::kSharedChunk)));
     const bool small_rows =
-        !long_seqs && cdiv(row_keys, kSmallRowKeys) <= (head_dim == 64 ? 6 : 3) * int64_t(num_cus);
+        !long_seqs && cdiv(item_keys, kSmallRowKeys) <= (head_dim == 64 ? 6 : 3) * int64_t(num_cus);
     split_rows(small_rows ? kSmallRowKeys : kMinRowKeys);
     count_all_private();
 
@@ -524,7 +534,7 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
         if (qlen(r) == 0) continue;
         const int64_t keys = seq_lens[r] - kstart[r];
         if (is_row(r)) {
-          rest += double(keys) * num_kv_heads * head_dim * 4 / kStepBytes;
+          rest += double(keys) * num_kv_heads * key_bytes / kStepBytes;
           int64_t per = cdiv(keys, n_private[r]);
           // without long sequences' tiles, rows of the usual length as of the small
           // launches' (992 shared keys in two chunks beside them: 64 requests of 240-800
@@ -553,14 +563,22 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
     // A decode plan that fits pa_attn_decode_noalloc's array with the coarser
     // splits keeps fitting it.
     if (kind == PA_KIND_DECODE) {
-      int64_t parts = 0;  // times G rows, per kv-head
-      for (int32_t r = 0; r < n_seqs; ++r)
-        parts += n_private[r] + (cgroup[r] >= 0 ? cg_chunks[cgroup[r]] : 0);
-      if (parts * num_q_heads * (head_dim + 1) * 4 > int64_t(PA_NOALLOC_WORKSPACE_BYTES)) {
+      auto fits = [&] {
+        int64_t parts = 0;  // times G rows, per kv-head
+        for (int32_t r = 0; r < n_seqs; ++r)
+          parts += n_private[r] + (cgroup[r] >= 0 ? cg_chunks[cgroup[r]] : 0);
+        return parts * num_q_heads * (head_dim + 1) * 4 <= int64_t(PA_NOALLOC_WORKSPACE_BYTES);
+      };
+      if (!fits()) {
         for (size_t c = 0; c < cg_keys.size(); ++c) cg_chunks[c] = int32_t(cdiv(cg_keys[c], pa::kSharedChunk));
         split_rows(kMinRowKeys);
         tile_keys = kPrivateTileKeys;
         count_all_private();
+        // more than 32 heads per kv-head over the 8-bit cache: long tile items, too
+        if (kv8 && !fits()) {
+          few_tiles = true;
+          count_all_private();
+        }
       }
     }
     // Decode of more than 64 heads per kv-head runs on these tiles, and whole
@@ -571,7 +589,7 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
       for (int32_t r = 0; r < n_seqs; ++r) {
         if (qlen(r) == 0) continue;
         const int64_t keys = seq_lens[r] - kstart[r];
-        launch_steps += double(keys) * num_kv_heads * head_dim * 4 / kStepBytes;
+        launch_steps += double(keys) * num_kv_heads * key_bytes / kStepBytes;
         if (is_row(r))
           other_steps = std::max(other_steps, cdiv(cdiv(keys, n_private[r]), pa::kTileStep));
       }
@@ -591,7 +609,7 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
         if (qlen(r) == 0) continue;
         if (is_row(r)) ng += cdiv(qlen(r) * G, pa::kMergeRows);
         if (is_row(r))
-          (on_tiles(r) ? nt : nr) += n_private[r];
+          (on_tiles(r) ? nt : nr) += n_private[r] * (on_tiles(r) ? 1 : row_pieces(r));
         else
           nt += cdiv(int64_t(qlen(r)) * G, pa::kTileRows);
       }
@@ -609,7 +627,7 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
       if (is_row(r)) {
         const int32_t k0s = kstart[r];
         const bool tiled = on_tiles(r);
-        const int64_t kstep = tiled ? pa::kTileStep : pa::kKeyStep;
+        const int64_t kstep = tiled ? pa::kTileStep : row_step;
         // parts 0 .. first-1 are the shared prefix's key chunks
         const int32_t first = cgroup[r] >= 0 ? cg_chunks[cgroup[r]] : 0;
         const int32_t nsplit = n_private[r];
@@ -636,8 +654,11 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
             t_tiles.push_back({r, 0, 0, rows, int32_t(k0), int32_t(k1), part, pa::kItemStream});
             tile_cost.push_back((k1 - k0) * rows);
           } else {
-            t_rows.push_back({r, 0, 0, rows, int32_t(k0), int32_t(k1), part, 0});
-            row_cost.push_back(k1 - k0);
+            for (int32_t row0 = 0; row0 < rows; row0 += pa::kRowItemRows) {
+              t_rows.push_back({r, 0, row0, std::min(pa::kRowItemRows, rows - row0), int32_t(k0),
+                                int32_t(k1), part < 0 ? -1 : part + row0, 0});
+              row_cost.push_back(k1 - k0);
+            }
           }
         }
       } else {

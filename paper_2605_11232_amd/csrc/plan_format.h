@@ -126,6 +126,7 @@ constexpr int32_t kMergeRows = 4;     // rows per merge group (half a wavefront 
 constexpr int32_t kWideGroupParts = kTileRows / kMergeRows;  // merge workgroups of a wide group
 constexpr int32_t kRowSeqRows = 64;   // sequences with at most this many rows use row items
 constexpr int32_t kKeyStep = 32;      // keys per row-item inner iteration
+constexpr int32_t kKeyStep8 = 64;     // and over the 8-bit cache
 constexpr int32_t kRowItemBlocks = 64;  // most blocks (of 16 keys) one row item spans
 constexpr int32_t kTileStep = 64;     // keys per tile-item inner iteration
 constexpr int32_t kSharedChunk = 6144;  // most shared keys one cascade item covers

@@ -241,3 +241,39 @@ def test_binding_refusals():
     bad("arg", B.qk_norm_rope, q, rows, pos, tab, q, rows.float())
     bad("arg", B.qk_norm_rope, q, rows, pos, tab, q, rows, q_weight=torch.zeros(d))
     bad("arg", B.qk_norm_rope, q, rows.float(), pos, tab, q, rows)
+
+
+@pytest.mark.parametrize("seed", range(30))
+def test_plans_cover_every_row_once(seed):
+    """Random launches over the 8-bit cache, prefixes shared, rows of every item
+    kind (sequences of 33 to 64 rows run as two row items)."""
+    from tests.test_capi_host import check_plan, parse_plan
+    r = np.random.default_rng(seed)
+    n, hkv, G = int(r.integers(1, 40)), int(r.choice([1, 2, 8])), int(r.choice([1, 4, 7, 8, 40, 64]))
+    L = r.integers(1, 4000, size=n)
+    q = np.minimum(L, r.choice([1, 2, 5, 8, 9, 33, 300], size=n))
+    kind, n_q = B.KIND_PREFILL, 0
+    if seed % 3:
+        n_q = 1 if seed % 3 == 1 else 5
+        L = np.maximum(L, n_q)
+        q[:] = n_q
+        kind = B.KIND_DECODE if n_q == 1 else B.KIND_VERIFY
+    cu = np.concatenate([[0], np.cumsum(q)])
+    mb = int((L.max() + 15) // 16)
+    bt = np.full((n, mb), -1, np.int32)
+    nxt, prefix = 0, int(r.integers(0, 200))
+    for s in range(n):
+        nb = int((L[s] + 15) // 16)
+        pb = min(nb - 1, prefix) if r.random() < 0.6 else 0
+        bt[s, :pb] = 10 ** 6 + np.arange(pb)
+        bt[s, pb:nb] = nxt + np.arange(nb - pb)
+        nxt += nb - pb
+    D = int(r.choice([64, 128]))
+    plan, info = B.plan(kind, n_q, L, cu, hkv * G, hkv, D, 16, B.PA_BF16_KV8, block_table=bt)
+    check_plan(plan, info, L, cu, G, hkv, D)
+    _, _, tiles, rows, _ = parse_plan(plan)
+    assert all(q[t[0]] * G <= 64 for t in rows if t[0] >= 0)
+    if kind != B.KIND_DECODE:
+        assert all(q[t[0]] * G > 64 for t in tiles)
+    else:  # tiles only where the array of the call without workspace asks for them
+        assert info.workspace_bytes <= B.NOALLOC_WORKSPACE_BYTES
