@@ -187,9 +187,11 @@ __device__ __forceinline__ float max_halves(float x) {
 // buffers freed by steps t and t - 1 during step t.
 //
 // KV8: a step's K and V^T pass through registers, where they become bf16, into
-// the same LDS tiles: step t begins by storing K of step t + 2 and V^T of step
-// t + 1, loaded during step t - 1, and loads the next.  Each value is converted
-// once per workgroup, not once per wavefront that reads it.
+// the same LDS tiles: step t stores K of step t + 2 and V^T of step t + 1, loaded
+// during step t - 1, and loads the next.  Each value is converted once per
+// workgroup, not once per wavefront that reads it: 32 prompts on 2048 cached tokens
+// take 795 us against 752 over a bf16 cache, of which the conversions are 32 VALU
+// instructions in about 160 a step and the float32 sums 16.
 template <int D, int NSUB, bool KV8, bool SHARED, bool FULL, bool STREAM = false>
 __device__ __forceinline__ void tile_item(const int32_t* it, int g, int poff, const AttnArgs& a,
                                           TileSmem<D, NSUB>& sm) {
@@ -324,56 +326,57 @@ __device__ __forceinline__ void tile_item(const int32_t* it, int g, int poff, co
   // (four slots) write in distinct banks.  Of V^T it takes one dim's 16 keys.
   static_assert(!KV8 || NSUB == 2, "8-bit staging: 64-key steps");
   constexpr int NR = KV8 ? NSUB * D / 128 : 1;
-  u32x4 rk[NR], rv[NR];      // raw K and V^T on their way
-  uint32_t ek[NR], ev[NR];   // their blocks' scale bytes
+  u32x4 rk[NR], rv[NR];   // raw K and V^T on their way
+  int64_t blk8[2][NR];    // byte offsets of the blocks of this wavefront's pieces, by step % 2
+  uint32_t sc8[2][NR];    // their scales: keys' byte, values' byte
   const int slot8 = (lane >> 1) & 15, pos8 = key_slot_pos(slot8);
-  const uint32_t koff8 = slot8 * 64 + 32 * hh + 16 * (lane & 1);
-  const uint32_t kdst8 = hh * 64 + 4 * pos8 + ((2 * (lane & 1)) ^ ((pos8 >> 2) & 3));
-  const uint8_t* scales = a.scales + 2 * g;
-  auto piece_block = [&](const int64_t (&blk)[NB], int i) {
-    if constexpr (D == 128) return (w >> 1) ? blk[2 * i + 1] : blk[2 * i];
-    else return (w >> 1) ? ((w & 1) ? blk[3] : blk[2]) : ((w & 1) ? blk[1] : blk[0]);
-  };
   const uint32_t piece_off = D == 128 ? (w & 1) * 1024 : 0;  // of a piece in its block
-  auto raw16 = [](const char* p) {
-    if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
-    else return ld16(p);
-  };
-  // a block is 16 D hkv bytes, its scales are 2 hkv
-  auto scale_at = [&](int64_t blk, int side) -> uint32_t { return scales[(uint64_t)blk / (8 * D) + side]; };
-  auto load_k8 = [&](const int64_t (&blk)[NB]) {
+  const uint32_t koff8 = piece_off + slot8 * 64 + 32 * hh + 16 * (lane & 1);
+  const uint32_t kdst8 = hh * 64 + 4 * pos8 + ((2 * (lane & 1)) ^ ((pos8 >> 2) & 3));
+  // Blocks and scales of a step's pieces.  A block is 16 D hkv bytes, its scales are 2
+  // hkv; the pair is in an aligned word, loaded into a scalar register.
+  auto step_blocks8 = [&](int t0, int s) {
+    const int jb = t0 / kBlock;
+    win.seek(jb);
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
-      const int64_t b = piece_block(blk, i);
-      rk[i] = raw16(kbase + b + piece_off + koff8);
-      ek[i] = scale_at(b, 0);
+      const uint64_t id = (uint32_t)win.at(jb + (D == 128 ? 2 * i + (w >> 1) : w));
+      blk8[s][i] = (int64_t)(id * (uint32_t)blk_bytes);
+      const uint64_t p = reinterpret_cast<uint64_t>(a.scales) + 2 * (id * (uint32_t)a.hkv + g);
+      sc8[s][i] = *reinterpret_cast<const __attribute__((address_space(4))) uint32_t*>(p & ~uint64_t(3)) >>
+                  (8 * (uint32_t(p) & 2));
     }
   };
-  auto load_v8 = [&](const int64_t (&blk)[NB]) {
-#pragma unroll
-    for (int i = 0; i < NR; ++i) {
-      const int64_t b = piece_block(blk, i);
-      rv[i] = raw16(vbase + b + piece_off + 16 * lane);
-      ev[i] = scale_at(b, 1);
-    }
+  // The wave-uniform address in scalar registers, the lane's offset in a vector one.
+  auto raw16 = [](const char* base, uint32_t off) {
+    const __amdgpu_buffer_rsrc_t r =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), (short)0, 16 * D, 0x00020000);
+    return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, STREAM ? kCachePolicyNonTemporal : 0));
   };
-  auto store_k8 = [&](int buf) {
+  auto load_k8 = [&](int s) {
+#pragma unroll
+    for (int i = 0; i < NR; ++i) rk[i] = raw16(kbase + blk8[s][i], koff8);
+  };
+  auto load_v8 = [&](int s) {
+#pragma unroll
+    for (int i = 0; i < NR; ++i) rv[i] = raw16(vbase + blk8[s][i], piece_off + 16 * lane);
+  };
+  auto store_k8 = [&](int s) {
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
-      const float sc = scale8(ek[i]);
+      const float sc = scale8(sc8[s][i] & 255);
       // units of 16 bytes; a piece fills two 32-dim groups (128 units) of the tile
-      __bf16* p = &sm.k[buf][8 * (128 * (4 * i + w) + kdst8)];
-      __bf16* p1 = &sm.k[buf][8 * (128 * (4 * i + w) + (kdst8 ^ 1))];
-      st16(p, bf16_of_e4m3(rk[i][0], rk[i][1], sc));
-      st16(p1, bf16_of_e4m3(rk[i][2], rk[i][3], sc));
+      __bf16* p = &sm.k[s][8 * (128 * (4 * i + w))];
+      st16(p + 8 * kdst8, bf16_of_e4m3(rk[i][0], rk[i][1], sc));
+      st16(p + 8 * (kdst8 ^ 1), bf16_of_e4m3(rk[i][2], rk[i][3], sc));
     }
   };
-  auto store_v8 = [&](int buf) {
+  auto store_v8 = [&](int s) {
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
-      const float sc = scale8(ev[i]);
-      const int d = lane, sw = vswz(d);  // vswz(64 + d) == vswz(d)
-      __bf16* p = &sm.v[buf][8 * (128 * (4 * i + w) + 2 * d)];
+      const float sc = scale8(sc8[s][i] >> 8 & 255);
+      const int sw = vswz(lane);  // vswz(64 + d) == vswz(d)
+      __bf16* p = &sm.v[s][8 * (128 * (4 * i + w) + 2 * lane)];
       st16(p + 8 * sw, bf16_of_e4m3(rv[i][0], rv[i][1], sc));
       st16(p + 8 * (1 - sw), bf16_of_e4m3(rv[i][2], rv[i][3], sc));
     }
@@ -521,23 +524,24 @@ __device__ __forceinline__ void tile_item(const int32_t* it, int g, int poff, co
     // blk[t % 2]: byte offsets of step t's blocks, found two steps ahead
     // (for the K copy) and used again one step ahead (for the V^T copy)
     int64_t blk[2][NB] = {};
-    step_blocks(kv0, blk[0]);
     if constexpr (KV8) {
-      load_k8(blk[0]);
-      load_v8(blk[0]);
+      step_blocks8(kv0, 0);
+      load_k8(0);
+      load_v8(0);
       store_k8(0);
       store_v8(0);
       if (ntiles > 1) {
-        step_blocks(kv0 + KT, blk[1]);
-        load_k8(blk[1]);
-        load_v8(blk[1]);  // stored in step 0
+        step_blocks8(kv0 + KT, 1);
+        load_k8(1);
+        load_v8(1);  // stored in step 0
         store_k8(1);
         if (ntiles > 2) {
-          step_blocks(kv0 + 2 * KT, blk[0]);
-          load_k8(blk[0]);
+          step_blocks8(kv0 + 2 * KT, 0);
+          load_k8(0);
         }
       }
     } else {
+      step_blocks(kv0, blk[0]);
       issue_k(blk[0], 0);
       issue_v(blk[0], 0);
       if (ntiles > 1) {
@@ -566,10 +570,10 @@ __device__ __forceinline__ void tile_item(const int32_t* it, int g, int poff, co
       store_v8(1 - buf);
       if (t + 2 < ntiles) {
         store_k8(buf);
-        load_v8(blk[buf]);  // of step t + 2, whose blocks were found one step earlier
+        load_v8(buf);  // of step t + 2, whose blocks were found one step earlier
         if (t + 3 < ntiles) {
-          step_blocks(kv0 + KT * (t + 3), blk[1 - buf]);
-          load_k8(blk[1 - buf]);
+          step_blocks8(kv0 + KT * (t + 3), 1 - buf);
+          load_k8(1 - buf);
         }
       }
     };
@@ -578,9 +582,7 @@ __device__ __forceinline__ void tile_item(const int32_t* it, int g, int poff, co
     auto step = [&](int t, auto mask_next, auto buf_c) {
       constexpr int buf = decltype(buf_c)::value;
       const int t0 = kv0 + KT * t;
-      if constexpr (KV8) {
-        stage8(t, buf_c);
-      } else {
+      if constexpr (!KV8) {
         if (t + 2 < ntiles) {
           step_blocks(t0 + 2 * KT, blk[buf]);
           issue_k(blk[buf], buf);
@@ -598,6 +600,9 @@ __device__ __forceinline__ void tile_item(const int32_t* it, int g, int poff, co
       // keep the row-sum additions in this region, where they overlap the
       // score MFMAs, instead of letting them sink past the barrier
       asm volatile("" : "+v"(l));
+      // The conversions go beside the matrix instructions (12 prompts of 512 tokens at
+      // head_dim 64 98.5 us, 101.9 at the step's start; head_dim 128 even).
+      if constexpr (KV8) stage8(t, buf_c);
       pv(buf_c, p);
       __builtin_amdgcn_s_setprio(0);
       if constexpr (decltype(mask_next)::value) mask(t0 + KT, sn);

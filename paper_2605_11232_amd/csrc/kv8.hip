@@ -2,15 +2,16 @@
 //
 // A (block, kv-head) holds 16 tokens of e4m3 keys [D/64][16][64] and values
 // [D][16], and a power-of-two scale for each of the two (a byte, exponent + 127).
-// One workgroup owns one (sequence, block, kv-head) of the launch, so that the
-// scale, which needs all of the block's new tokens, and the codes of earlier
-// tokens, which are rounded again where the scale grows, are found and written by
-// one workgroup: no atomics and no second launch, and the result does not depend
-// on how the work is split.
+// One wavefront owns one (sequence, block, kv-head) of the
+// launch, so that the scale, which needs all of the block's new tokens, and the codes
+// of earlier tokens, which are rounded again where the scale grows, are found and
+// written by one: no atomics and no second launch, and the result does not depend on
+// how the work is split.
 //
-// Workgroups find their block in cu_seqlens: sequence r owns the slots
-// cu[r] / 16 + 2 r up to the next sequence's first, at least as many as the
-// blocks that its rows touch (n rows touch at most n / 16 + 2).
+// They find their block in cu_seqlens: sequence r owns the slots cu[r] / 16 + 2 r up
+// to the next sequence's first, at least as many as the blocks that its rows touch (n
+// rows touch at most n / 16 + 2); or each row a slot, of which a block's first one
+// does the work.
 #include "device_common.h"
 
 namespace pa {
@@ -28,6 +29,8 @@ struct Kv8Args {
   uint8_t* scales;
   int64_t k_stride, v_stride;
   int32_t max_blocks, n_seqs, n_tokens, num_blocks, hkv;
+  int64_t slots;    // (sequence, block) slots of the launch
+  bool by_token;    // a slot per row, not per block
 };
 
 // One block of the launch and its rows.
@@ -37,15 +40,16 @@ struct BlockRows {
   int row0;        // row of offset off0
 };
 
-// Largest r of [0, n) with cu[r] / 16 + 2 r <= x: each round compares 64 evenly
-// spaced sequences, one per lane.
-__device__ __forceinline__ int find_seq(const int32_t* cu, int n, int x) {
+// Largest r of [0, n) with key(cu[r], r) <= x (keys rise with r): each round compares
+// 64 evenly spaced sequences, one per lane.
+template <class Key>
+__device__ __forceinline__ int find_seq(const int32_t* cu, int n, int x, Key key) {
   const int lane = threadIdx.x & 63;
   int lo = 0, hi = n;
   while (hi - lo > 1) {
     const int step = (hi - lo + 63) / 64;
     const int i = lo + lane * step;
-    const bool below = i < hi && cu[i < hi ? i : lo] / kBlock + 2 * i <= x;
+    const bool below = i < hi && key(cu[i < hi ? i : lo], i) <= x;
     const int c = max(1, __popcll(__ballot(below)));
     lo += (c - 1) * step;
     hi = min(lo + step, hi);
@@ -55,12 +59,25 @@ __device__ __forceinline__ int find_seq(const int32_t* cu, int n, int x) {
 
 __device__ __forceinline__ BlockRows find_rows(const Kv8Args& a, int slot, int h) {
   BlockRows b{-1, 0, 0, 0};
-  const int r = find_seq(a.cu, a.n_seqs, slot);
-  const int c0 = a.cu[r], n = a.cu[r + 1] - c0, L = a.seq_lens[r];
+  int r, c0, n, L;
+  int64_t j;  // logical block
+  if (a.by_token) {
+    // row `slot` is a block's first one; a guess that is right in a decode step, where
+    // every sequence has one row, saves the search
+    r = min(slot, a.n_seqs - 1);
+    if (a.cu[r] != slot || a.cu[r + 1] != slot + 1)
+      r = find_seq(a.cu, a.n_seqs, slot, [](int c, int) { return c; });
+    c0 = a.cu[r], n = a.cu[r + 1] - c0, L = a.seq_lens[r];
+    const int row = slot - c0, pos = L - n + row;
+    if (row < 0 || row >= n || pos < 0 || (row > 0 && pos % kBlock)) return b;
+    j = pos / kBlock;
+  } else {
+    r = find_seq(a.cu, a.n_seqs, slot, [](int c, int i) { return c / kBlock + 2 * i; });
+    c0 = a.cu[r], n = a.cu[r + 1] - c0, L = a.seq_lens[r];
+    j = (L - n) / kBlock + (int64_t)slot - (c0 / kBlock + 2 * r);
+  }
   const int first = L - n;  // first row's position
-  if (n <= 0 || first < 0 || c0 < 0) return b;
-  const int64_t j = first / kBlock + (int64_t)slot - (c0 / kBlock + 2 * r);
-  if (j < 0 || j * kBlock >= L || j >= a.max_blocks) return b;
+  if (n <= 0 || first < 0 || c0 < 0 || j < 0 || j * kBlock >= L || j >= a.max_blocks) return b;
   const int p0 = int(j) * kBlock;
   b.off0 = max(first - p0, 0);
   b.off1 = min(L - p0, kBlock);
@@ -99,184 +116,218 @@ __device__ __forceinline__ uint32_t first_bytes(uint32_t old, uint32_t x, int ke
   return (old & m) | (x & ~m);
 }
 
+// Eight values of T as loaded, and as float32.
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, float (&x)[8]);
-template <>
-__device__ __forceinline__ void load8<float>(const float* p, float (&x)[8]) {
-  const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+struct Raw8 {
+  u32x4 x[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
-}
-template <>
-__device__ __forceinline__ void load8<__bf16>(const __bf16* p, float (&x)[8]) {
-  const bf16x8 a = as_bf16x8(ld16(p));
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = float(a[i]);
+    for (size_t i = 0; i < sizeof(T) / 2; ++i) x[i] = ld16(p + 16 / sizeof(T) * i);
+  }
+  __device__ __forceinline__ float at(int i) const {
+    if constexpr (sizeof(T) == 2) return __uint_as_float(i % 2 ? x[0][i / 2] & 0xFFFF0000u : x[0][i / 2] << 16);
+    else return __uint_as_float(x[i / 4][i % 4]);
+  }
+};
+
+// Order of a wavefront's own LDS accesses: the hardware keeps it, this the compiler.
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
 }
 
+// Transpose of 4 x 4 bytes: byte i of word k becomes byte k of word i.
+__device__ __forceinline__ void transpose4(uint32_t (&w)[4]) {
+  const uint32_t a = __builtin_amdgcn_perm(w[1], w[0], 0x05010400), b = __builtin_amdgcn_perm(w[1], w[0], 0x07030602);
+  const uint32_t c = __builtin_amdgcn_perm(w[3], w[2], 0x05010400), d = __builtin_amdgcn_perm(w[3], w[2], 0x07030602);
+  w[0] = __builtin_amdgcn_perm(c, a, 0x05040100);
+  w[1] = __builtin_amdgcn_perm(c, a, 0x07060302);
+  w[2] = __builtin_amdgcn_perm(d, b, 0x05040100);
+  w[3] = __builtin_amdgcn_perm(d, b, 0x07060302);
+}
+
+// One wavefront per (block, kv-head).  D / 8 lanes hold a token's keys, the next as
+// many its values, 8 dims a lane; 64 / (D / 4) tokens at a time, all loads issued
+// before the first is used.  The keys' codes go straight to the cache, the values'
+// through LDS, where a lane takes a square of 4 dims x 4 tokens and transposes it.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void kv8_append_kernel(const T* __restrict__ k_new,
                                                          const T* __restrict__ v_new, Kv8Args a) {
-  constexpr int CH = D / 8;             // 8-dim chunks of a row
-  constexpr int U = 2 * kBlock * CH / 256;  // chunks of K and V per thread
-  __shared__ float amax_sh[2][4];
-  __shared__ uint8_t vt[kBlock][D + 8];
-  const int tid = threadIdx.x, w = tid >> 6;
-  const int h = blockIdx.x % a.hkv;
-  const BlockRows b = find_rows(a, blockIdx.x / a.hkv, h);
+  constexpr int LR = D / 8;            // lanes of a row
+  constexpr int TI = 64 / (2 * LR);    // tokens at a time
+  constexpr int NI = kBlock / TI;
+  constexpr int SQ = D / 64;           // squares of a lane
+  __shared__ __align__(16) uint8_t vt_sh[4][kBlock][D + 8];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t i = (int64_t)blockIdx.x * 4 + w;
+  const int64_t slot = i / a.hkv;
+  if (slot >= a.slots) return;
+  const int h = int(i - slot * a.hkv);
+  const BlockRows b = find_rows(a, int(slot), h);
   if (b.bh < 0) return;
+  uint8_t (*vt)[D + 8] = vt_sh[w];
+  const int c = lane % LR, side = lane / LR % 2, sub = lane / (2 * LR);
+  const int e_old = min(max(int(a.scales[2 * b.bh + side]) - kExpBias, kExpMin), kExpMax);
 
-  // chunk c of thread tid: K's for c < 16 CH, V's after; token offset, then dims
-  float x[U][8];
-  float mx[2] = {0.f, 0.f};
+  Raw8<T> x[NI];
+  const T* src = (side ? v_new + (int64_t)b.row0 * a.v_stride : k_new + (int64_t)b.row0 * a.k_stride) + (int64_t)h * D + 8 * c;
+  const int64_t stride = side ? a.v_stride : a.k_stride;
+  auto has = [&](int u) { return u * TI + sub >= b.off0 && u * TI + sub < b.off1; };
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int c = u * 256 + tid, side = c / (kBlock * CH);
-    const int o = c / CH % kBlock, part = c % CH;
-    if (o < b.off0 || o >= b.off1) continue;
-    const int64_t row = b.row0 + o - b.off0;
-    load8((side ? v_new + row * a.v_stride : k_new + row * a.k_stride) + (int64_t)h * D + 8 * part, x[u]);
-    float m = 0.f;
+  for (int u = 0; u < NI; ++u)
+    if (has(u)) x[u].load(src + (u * TI + sub - b.off0) * stride);
+  float mx = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const bool finite = fabsf(x[u][i]) < __builtin_huge_valf();
-      m = fmaxf(m, finite ? fabsf(x[u][i]) : 0.f);
-      x[u][i] = finite ? x[u][i] : __builtin_nanf("");
-    }
-    if (side) mx[1] = fmaxf(mx[1], m);
-    else mx[0] = fmaxf(mx[0], m);
+  for (int u = 0; u < NI; ++u)
+    if (has(u))
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float v = fabsf(x[u].at(k));
+        mx = fmaxf(mx, v < __builtin_huge_valf() ? v : 0.f);
+      }
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1)
+    if (m != LR) mx = fmaxf(mx, wave_xor(mx, m));
+  int e = exponent_of(mx), grow = 0;  // of this lane's side; how far it grew for earlier tokens
+  if (b.off0 > 0) {
+    grow = min(max(e - e_old, 0), 126);
+    e = max(e, e_old);
   }
-#pragma unroll
-  for (int s = 0; s < 2; ++s) {
-#pragma unroll
-    for (int k = 32; k >= 1; k >>= 1) mx[s] = fmaxf(mx[s], wave_xor(mx[s], k));
-    if ((tid & 63) == 0) amax_sh[s][w] = mx[s];
-  }
-  __syncthreads();
-  int e[2], grow[2];  // exponents, and how far they grew for earlier tokens
-#pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    e[s] = exponent_of(fmaxf(fmaxf(amax_sh[s][0], amax_sh[s][1]), fmaxf(amax_sh[s][2], amax_sh[s][3])));
-    grow[s] = 0;
-    if (b.off0 > 0) {
-      // (bounded: the earlier tokens may never have been stored)
-      const int was = min(max(int(a.scales[2 * b.bh + s]) - kExpBias, kExpMin), kExpMax);
-      grow[s] = min(max(e[s] - was, 0), 126);
-      e[s] = max(e[s], was);
-    }
-  }
-  __syncthreads();  // every thread has read the scales
-  if (tid < 2) a.scales[2 * b.bh + tid] = uint8_t((tid ? e[1] : e[0]) + kExpBias);
+  if (sub == 0 && c == 0) a.scales[2 * b.bh + side] = uint8_t(e + kExpBias);
 
   uint8_t* kb = a.kc + b.bh * (kBlock * D);
   uint8_t* vb = a.vc + b.bh * (kBlock * D);
+  const float s = pow2(-e);
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int c = u * 256 + tid, side = c / (kBlock * CH);
-    const int o = c / CH % kBlock, part = c % CH;
-    if (o < b.off0 || o >= b.off1) continue;
-    const float s = pow2(-(side ? e[1] : e[0]));
-    const u32x2 q = {codes_of(x[u][0], x[u][1], x[u][2], x[u][3], s),
-                     codes_of(x[u][4], x[u][5], x[u][6], x[u][7], s)};
-    if (side) *reinterpret_cast<u32x2*>(&vt[o][8 * part]) = q;
-    else *reinterpret_cast<u32x2*>(kb + part / 8 * 1024 + o * 64 + part % 8 * 8) = q;
-  }
-  if (grow[0] > 0) {  // earlier tokens' keys
-    const float s = pow2(-grow[0]);
-    for (int c = tid; c < b.off0 * (D / 16); c += 256) {
-      uint8_t* p = kb + c % (D / 64) * 1024 + c / (D / 16) * 64 + c / (D / 64) % 4 * 16;
+  for (int u = 0; u < NI; ++u)
+    if (has(u)) {
+      float y[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float v = x[u].at(k);
+        y[k] = fabsf(v) < __builtin_huge_valf() ? v : __builtin_nanf("");
+      }
+      const u32x2 q = {codes_of(y[0], y[1], y[2], y[3], s), codes_of(y[4], y[5], y[6], y[7], s)};
+      const int o = u * TI + sub;
+      *reinterpret_cast<u32x2*>(side ? &vt[o][8 * c] : kb + c / 8 * 1024 + o * 64 + c % 8 * 8) = q;
+    }
+  const int grow_k = __builtin_amdgcn_readlane(grow, 0), grow_v = __builtin_amdgcn_readlane(grow, LR);
+  if (grow_k > 0) {  // earlier tokens' keys
+    const float f = pow2(-grow_k);
+    for (int j = lane; j < b.off0 * (D / 16); j += 64) {
+      uint8_t* p = kb + j % (D / 64) * 1024 + j / (D / 16) * 64 + j / (D / 64) % 4 * 16;
       u32x4 v = ld16(p);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = codes_again(v[i], s);
+      for (int k = 0; k < 4; ++k) v[k] = codes_again(v[k], f);
       st16(p, v);
     }
   }
-  __syncthreads();
+  wave_lds_order();
   const bool whole = b.off0 == 0 && b.off1 == kBlock;
-  if (whole || grow[1] > 0) {
-    const float s = pow2(-grow[1]);
-    for (int d = tid; d < D; d += 256) {
-      u32x4 v = zero16();
-      if (!whole) v = ld16(vb + d * kBlock);
+  if (whole || grow_v > 0) {
+    const float f = pow2(-grow_v);
+    const int dq = 4 * (lane % (D / 4)), o0 = 4 * SQ * (lane / (D / 4));
+    uint32_t q[SQ][4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint32_t q = 0;
+    for (int sq = 0; sq < SQ; ++sq) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) q |= uint32_t(vt[4 * i + k][d]) << (8 * k);
-        // earlier tokens, new ones, and slots behind them as they were
-        if (!whole)
-          q = first_bytes(codes_again(v[i], s), first_bytes(q, v[i], b.off1 - 4 * i), b.off0 - 4 * i);
-        v[i] = q;
+      for (int k = 0; k < 4; ++k) q[sq][k] = *reinterpret_cast<const uint32_t*>(&vt[o0 + 4 * sq + k][dq]);
+      transpose4(q[sq]);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      uint32_t* p = reinterpret_cast<uint32_t*>(vb + (dq + k) * kBlock + o0);
+      uint32_t r[SQ];
+#pragma unroll
+      for (int sq = 0; sq < SQ; ++sq) {
+        r[sq] = q[sq][k];
+        if (!whole) {
+          // earlier tokens, new ones, and slots behind them as they were
+          const uint32_t was = p[sq];
+          const int o = o0 + 4 * sq;
+          r[sq] = first_bytes(codes_again(was, f), first_bytes(r[sq], was, b.off1 - o), b.off0 - o);
+        }
       }
-      st16(vb + d * kBlock, v);
+      if constexpr (SQ == 2) *reinterpret_cast<u32x2*>(p) = u32x2{r[0], r[1]};
+      else p[0] = r[0];
     }
   } else {
-    for (int c = tid; c < D * (b.off1 - b.off0); c += 256) {
-      const int d = c % D, o = b.off0 + c / D;
+    for (int j = lane; j < D * (b.off1 - b.off0); j += 64) {
+      const int d = j % D, o = b.off0 + j / D;
       vb[d * kBlock + o] = vt[o][d];
     }
   }
 }
 
-// Eight e4m3 codes times a power of two, stored as T.
+// Four e4m3 codes times a power of two, stored as T.
 template <typename T>
-__device__ __forceinline__ void store8(T* p, u32x2 c, float s);
-template <>
-__device__ __forceinline__ void store8<float>(float* p, u32x2 c, float s) {
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(c[i], false);
-    const f32x2 b = __builtin_amdgcn_cvt_pk_f32_fp8(c[i], true);
-    *reinterpret_cast<f32x4*>(p + 4 * i) = f32x4{a[0] * s, a[1] * s, b[0] * s, b[1] * s};
+__device__ __forceinline__ void store4(T* p, uint32_t c, float s) {
+  if constexpr (sizeof(T) == 2) {
+    *reinterpret_cast<u32x2*>(p) = u32x2{
+        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, s, false)),
+        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, s, true))};
+  } else {
+    const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(c, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(c, true);
+    *reinterpret_cast<f32x4*>(p) = f32x4{a[0] * s, a[1] * s, b[0] * s, b[1] * s};
   }
-}
-template <>
-__device__ __forceinline__ void store8<__bf16>(__bf16* p, u32x2 c, float s) {
-  u32x4 r;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    r[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[i], s, false));
-    r[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[i], s, true));
-  }
-  st16(p, r);
 }
 
+// One wavefront per (block, kv-head), all loads issued before the first store.  Keys:
+// four dims of a token a lane.  Values: squares of 4 dims x 4 tokens, transposed in
+// registers; the 16 lanes of a square's four tokens store 128 contiguous bytes (bf16)
+// of a row.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void kv8_read_kernel(T* __restrict__ k_out, T* __restrict__ v_out,
                                                        Kv8Args a) {
-  constexpr int CH = D / 8;
-  __shared__ uint8_t vt[kBlock][D + 8];
-  const int tid = threadIdx.x;
-  const int h = blockIdx.x % a.hkv;
-  const BlockRows b = find_rows(a, blockIdx.x / a.hkv, h);
+  constexpr int LT = D / 4;          // lanes of a token's keys
+  constexpr int NK = kBlock * LT / 64;
+  constexpr int SQ = D / 64;         // squares of a lane
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t i = (int64_t)blockIdx.x * 4 + w;
+  const int64_t slot = i / a.hkv;
+  if (slot >= a.slots) return;
+  const int h = int(i - slot * a.hkv);
+  const BlockRows b = find_rows(a, int(slot), h);
   if (b.bh < 0) return;
   const uint8_t* kb = a.kc + b.bh * (kBlock * D);
   const uint8_t* vb = a.vc + b.bh * (kBlock * D);
   const float sk = pow2(int(a.scales[2 * b.bh]) - kExpBias);
   const float sv = pow2(int(a.scales[2 * b.bh + 1]) - kExpBias);
-  for (int d = tid; d < D; d += 256) {
-    const u32x4 v = ld16(vb + d * kBlock);
+  auto has = [&](int o) { return o >= b.off0 && o < b.off1; };
+  const int kd = 4 * (lane % LT), ko = lane / LT;      // of load 0; 64 / LT tokens a load
+  const int vd = 4 * (lane / 4), vo = 4 * (lane % 4);  // of square 0; 64 dims a square
+
+  uint32_t k[NK], v[SQ][4];
 #pragma unroll
-    for (int o = 0; o < kBlock; ++o) vt[o][d] = uint8_t(v[o / 4] >> (8 * (o % 4)));
+  for (int u = 0; u < NK; ++u)
+    k[u] = *reinterpret_cast<const uint32_t*>(kb + kd / 64 * 1024 + (u * (64 / LT) + ko) * 64 + kd % 64);
+#pragma unroll
+  for (int sq = 0; sq < SQ; ++sq)
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      v[sq][x] = *reinterpret_cast<const uint32_t*>(vb + (64 * sq + vd + x) * kBlock + vo);
+#pragma unroll
+  for (int u = 0; u < NK; ++u) {
+    const int o = u * (64 / LT) + ko;
+    if (has(o)) store4(k_out + (int64_t)(b.row0 + o - b.off0) * a.k_stride + (int64_t)h * D + kd, k[u], sk);
   }
-  for (int c = tid; c < kBlock * CH; c += 256) {
-    const int o = c / CH, part = c % CH;
-    if (o < b.off0 || o >= b.off1) continue;
-    const u32x2 q = *reinterpret_cast<const u32x2*>(kb + part / 8 * 1024 + o * 64 + part % 8 * 8);
-    store8(k_out + (int64_t)(b.row0 + o - b.off0) * a.k_stride + (int64_t)h * D + 8 * part, q, sk);
-  }
-  __syncthreads();
-  for (int c = tid; c < kBlock * CH; c += 256) {
-    const int o = c / CH, part = c % CH;
-    if (o < b.off0 || o >= b.off1) continue;
-    const u32x2 q = *reinterpret_cast<const u32x2*>(&vt[o][8 * part]);
-    store8(v_out + (int64_t)(b.row0 + o - b.off0) * a.v_stride + (int64_t)h * D + 8 * part, q, sv);
+#pragma unroll
+  for (int sq = 0; sq < SQ; ++sq) {
+    transpose4(v[sq]);
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      if (has(vo + x))
+        store4(v_out + (int64_t)(b.row0 + vo + x - b.off0) * a.v_stride + (int64_t)h * D + 64 * sq + vd, v[sq][x], sv);
   }
 }
 
-// Workgroups of n rows of n_seqs sequences.
-int64_t kv8_grid(int32_t n, int32_t n_seqs, int32_t hkv) {
-  return (int64_t(n) / kBlock + 2 * int64_t(n_seqs)) * hkv;
+// Slots of n rows of n_seqs sequences: one per row where that is fewer than two per
+// sequence and one per 16 rows (decode and verification steps).
+Kv8Args with_slots(Kv8Args a) {
+  a.slots = int64_t(a.n_tokens) / kBlock + 2 * int64_t(a.n_seqs);
+  a.by_token = a.n_tokens <= a.slots;
+  if (a.by_token) a.slots = a.n_tokens;
+  return a;
 }
 
 }  // namespace
@@ -286,9 +337,9 @@ int launch_kv8_append(const void* kn, int64_t k_stride, const void* vn, int64_t 
                       const int32_t* cu, int32_t n_seqs, int32_t n, void* kc, void* vc,
                       uint8_t* scales, int32_t nb, int32_t hkv, int32_t d, int32_t dtype,
                       hipStream_t stream) {
-  const Kv8Args a{bt, seq_lens, cu, static_cast<uint8_t*>(kc), static_cast<uint8_t*>(vc), scales,
-                  k_stride, v_stride, max_blocks, n_seqs, n, nb, hkv};
-  const int64_t grid = kv8_grid(n, n_seqs, hkv);
+  const Kv8Args a = with_slots({bt, seq_lens, cu, static_cast<uint8_t*>(kc), static_cast<uint8_t*>(vc), scales,
+                  k_stride, v_stride, max_blocks, n_seqs, n, nb, hkv, 0, false});
+  const int64_t grid = (a.slots * hkv + 3) / 4;  // a wavefront per (block, kv-head)
   if (grid > INT32_MAX) return static_cast<int>(hipErrorInvalidValue);
 #define PA_KV8(T, DD)                                                                            \
   hipLaunchKernelGGL((kv8_append_kernel<T, DD>), dim3(unsigned(grid)), dim3(256), 0, stream,     \
@@ -309,10 +360,10 @@ int launch_kv8_read(void* k_out, int64_t k_stride, void* v_out, int64_t v_stride
                     const int32_t* cu, int32_t n_seqs, int32_t n, const void* kc, const void* vc,
                     const uint8_t* scales, int32_t nb, int32_t hkv, int32_t d, int32_t dtype,
                     hipStream_t stream) {
-  const Kv8Args a{bt, seq_lens, cu, static_cast<uint8_t*>(const_cast<void*>(kc)),
+  const Kv8Args a = with_slots({bt, seq_lens, cu, static_cast<uint8_t*>(const_cast<void*>(kc)),
                   static_cast<uint8_t*>(const_cast<void*>(vc)), const_cast<uint8_t*>(scales),
-                  k_stride, v_stride, max_blocks, n_seqs, n, nb, hkv};
-  const int64_t grid = kv8_grid(n, n_seqs, hkv);
+                  k_stride, v_stride, max_blocks, n_seqs, n, nb, hkv, 0, false});
+  const int64_t grid = (a.slots * hkv + 3) / 4;
   if (grid > INT32_MAX) return static_cast<int>(hipErrorInvalidValue);
 #define PA_KV8(T, DD)                                                                            \
   hipLaunchKernelGGL((kv8_read_kernel<T, DD>), dim3(unsigned(grid)), dim3(256), 0, stream,       \
