@@ -259,16 +259,17 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(const T* __restrict__ k
   }
 }
 
-// Four e4m3 codes times a power of two, stored as T.
+// Four e4m3 codes times a power of two, stored as T.  Non-temporal: the rows leave the
+// caches to what is read again (163000 tokens 146 us, 156 with plain stores).
 template <typename T>
 __device__ __forceinline__ void store4(T* p, uint32_t c, float s) {
   if constexpr (sizeof(T) == 2) {
-    *reinterpret_cast<u32x2*>(p) = u32x2{
+    __builtin_nontemporal_store(u32x2{
         __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, s, false)),
-        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, s, true))};
+        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, s, true))}, reinterpret_cast<u32x2*>(p));
   } else {
     const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(c, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(c, true);
-    *reinterpret_cast<f32x4*>(p) = f32x4{a[0] * s, a[1] * s, b[0] * s, b[1] * s};
+    __builtin_nontemporal_store(f32x4{a[0] * s, a[1] * s, b[0] * s, b[1] * s}, reinterpret_cast<f32x4*>(p));
   }
 }
 
