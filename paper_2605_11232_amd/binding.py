@@ -69,6 +69,7 @@ _lib = None
 _torch = None  # the torch module, once a call needed it
 _attn = {}     # attention entry point of each launch kind
 _kv8_attn = {}  # and over the 8-bit cache
+_ROW_DTYPES = {}  # dtype codes of rows, once torch is there
 _P = C.c_void_p
 _I32P = C.POINTER(C.c_int32)
 _I64P = C.POINTER(C.c_int64)
@@ -460,6 +461,7 @@ def _torch_module():
     if _torch is None:
         import torch
         _torch = torch
+        _ROW_DTYPES.update({torch.bfloat16: PA_BF16, torch.float32: PA_F32})
     return _torch
 
 
@@ -668,34 +670,31 @@ def _refuse_device(*tensors):
 def _stream_on(device: int, stream) -> int:
     """The stream's handle, or the current one's; -1 where the current device is
     not ``device``."""
-    t = _torch
-    if device < 0 or t.cuda.current_device() != device:
+    c = _torch._C
+    if device < 0 or c._cuda_getDevice() != device:
         return -1
     if stream is None:
-        return t._C._cuda_getCurrentRawStream(device)
+        return c._cuda_getCurrentRawStream(device)
     return int(getattr(stream, "cuda_stream", stream))
 
 
-def _packed_rows(t, T: int, heads: int, d: int):
-    """Elements between the rows of [T, heads, d] tensor t if each row's heads are
-    packed (a column slice of a larger matrix, too), else None."""
-    if t.dim() != 3 or t.shape != (T, heads, d):
-        return None
-    s0, s1, s2 = t.stride()
-    if T and heads and not (s2 == 1 and (s1 == d or heads == 1)):
-        return None
-    return s0 if T > 1 else heads * d
+def _packed(x, heads: int, d: int) -> bool:
+    """Whether each row's heads of x [T, heads, d] lie side by side (in a column
+    slice of a larger matrix they do)."""
+    s = x.stride()
+    return s[2] == 1 and (s[1] == d or heads == 1) or x.numel() == 0
 
 
 def _kv8_rows(fn, k, v, block_table, seq_lens, cu_seqlens, k_cache, v_cache, scales, stream):
     t = _torch or _torch_module()
     nb, hkv, d, bs = v_cache.shape
-    T, n, i32, e4m3 = k.shape[0], seq_lens.numel(), t.int32, t.float8_e4m3fn
-    ks, vs = _packed_rows(k, T, hkv, d), _packed_rows(v, T, hkv, d)
+    shape, dt, n, i32, e4m3 = k.shape, k.dtype, seq_lens.numel(), t.int32, t.float8_e4m3fn
+    T, code = shape[0], _ROW_DTYPES.get(dt)
     rows, width = block_table.shape if block_table.dim() == 2 else (-1, 0)
     dev = v_cache.get_device()
     st = _stream_on(dev, stream)
-    if not (ks is not None and vs is not None and k.dtype == v.dtype
+    if not (shape == (T, hkv, d) and v.shape == shape and _packed(k, hkv, d)
+            and _packed(v, hkv, d) and code is not None and v.dtype == dt
             and k_cache.dtype == e4m3 and v_cache.dtype == e4m3 and scales.dtype == t.uint8
             and k_cache.shape == (nb, hkv, d // 64, bs, 64) and scales.shape == (nb, hkv, 2)
             and k_cache.is_contiguous() and v_cache.is_contiguous() and scales.is_contiguous()
@@ -708,16 +707,21 @@ def _kv8_rows(fn, k, v, block_table, seq_lens, cu_seqlens, k_cache, v_cache, sca
             == cu_seqlens.get_device() == dev):
         _refuse_cache(t, k_cache, v_cache, scales)
         _refuse(PA_ERR_ARG, [
-            (ks is not None and vs is not None,
+            (shape == (T, hkv, d) and v.shape == shape and _packed(k, hkv, d)
+             and _packed(v, hkv, d),
              f"rows {tuple(k.shape)} of strides {k.stride()} and {tuple(v.shape)} of "
              f"{v.stride()}, expected [T, {hkv}, {d}] with a row's heads packed"),
-            (k.dtype == v.dtype, "keys and values differ in dtype")])
+            (dt == v.dtype, "keys and values differ in dtype")])
         _refuse_metadata(t, block_table, seq_lens, cu_seqlens)
         _dtype_code(k)
         _refuse_device(k, v, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlens)
-    _check(fn(k.data_ptr(), ks, v.data_ptr(), vs, block_table.data_ptr(), width,
-              seq_lens.data_ptr(), cu_seqlens.data_ptr(), n, T, k_cache.data_ptr(),
-              v_cache.data_ptr(), scales.data_ptr(), nb, hkv, d, bs, _dtype_code(k), st))
+    # a single row's stride means nothing
+    ks, vs = (k.stride(0), v.stride(0)) if T > 1 else (hkv * d, hkv * d)
+    rc = fn(k.data_ptr(), ks, v.data_ptr(), vs, block_table.data_ptr(), width,
+            seq_lens.data_ptr(), cu_seqlens.data_ptr(), n, T, k_cache.data_ptr(),
+            v_cache.data_ptr(), scales.data_ptr(), nb, hkv, d, bs, code, st)
+    if rc:
+        _check(rc)
 
 
 def kv8_append(k_new, v_new, block_table, seq_lens, cu_seqlens, k_cache, v_cache, scales,
@@ -797,7 +801,9 @@ def kv8_attention(kind: int, q, k_cache, v_cache, scales, block_table, seq_lens,
     args, st = _kv8_attn_args(q, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlens_q,
                               plan_dev, info, out, lse, scale, stream, workspace)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(_kv8_attn[kind](*args, _dptr(workspace), ws_bytes, out.data_ptr(), _dptr(lse), st))
+    rc = _kv8_attn[kind](*args, _dptr(workspace), ws_bytes, out.data_ptr(), _dptr(lse), st)
+    if rc:
+        _check(rc)
 
 
 def kv8_attention_decode_noalloc(q, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlens_q,
@@ -819,22 +825,24 @@ def qk_norm_rope(q, k, positions, cos_sin, q_out, k_out, q_weight=None, k_weight
     fn = (_lib or lib()).pa_qk_norm_rope
     T, hq, d = q.shape
     hkv = k.shape[1]
-    qs, ks = _packed_rows(q, T, hq, d), _packed_rows(k, T, hkv, d)
     dt, dev = q.dtype, q_out.get_device()
-    st = _stream_on(dev, stream)
+    st, code = _stream_on(dev, stream), _ROW_DTYPES.get(dt)
     n_pos, rot = cos_sin.shape if cos_sin.dim() == 2 else (-1, 0)
-    if not (qs is not None and ks is not None and k.dtype == dt
+    if not (k.shape == (T, hkv, d) and _packed(q, hq, d) and _packed(k, hkv, d)
+            and code is not None and k.dtype == dt
             and q_out.dtype == dt and q_out.shape == (T, hq, d) and q_out.is_contiguous()
             and k_out.dtype == dt and k_out.shape == (T, hkv, d) and k_out.is_contiguous()
             and positions.dtype == t.int32 and positions.numel() == T
             and positions.is_contiguous() and n_pos >= 0 and cos_sin.dtype == t.float32
             and cos_sin.is_contiguous()
-            and all([w is None or (w.dtype == dt and w.numel() == d and w.is_contiguous()
-                                   and w.get_device() == dev) for w in (q_weight, k_weight)])
+            and (q_weight is None or (q_weight.dtype == dt and q_weight.numel() == d
+                 and q_weight.is_contiguous() and q_weight.get_device() == dev))
+            and (k_weight is None or (k_weight.dtype == dt and k_weight.numel() == d
+                 and k_weight.is_contiguous() and k_weight.get_device() == dev))
             and st >= 0 and q.get_device() == k.get_device() == k_out.get_device()
             == positions.get_device() == cos_sin.get_device() == dev):
         _refuse(PA_ERR_ARG, [
-            (qs is not None and ks is not None,
+            (k.shape == (T, hkv, d) and _packed(q, hq, d) and _packed(k, hkv, d),
              f"q {tuple(q.shape)} of strides {q.stride()} and k {tuple(k.shape)} of "
              f"{k.stride()}: expected [T, Hq, D] and [T, Hkv, D] with a row's heads packed"),
             (k.dtype == dt, "q and k differ in dtype")]
@@ -848,8 +856,12 @@ def qk_norm_rope(q, k, positions, cos_sin, q_out, k_out, q_weight=None, k_weight
                 and positions.is_contiguous(), "one contiguous int32 position per token"),
                (n_pos >= 0 and cos_sin.dtype == t.float32 and cos_sin.is_contiguous(),
                 "cos_sin must be contiguous float32 [n_positions, rot_dim]")])
+        _dtype_code(q)
         _refuse_device(q, k, q_out, k_out, positions, cos_sin, q_weight, k_weight)
-    _check(fn(q.data_ptr(), qs, k.data_ptr(), ks, positions.data_ptr(), T, cos_sin.data_ptr(),
-              n_pos, rot, _dptr(q_weight), _dptr(k_weight), eps,
-              (QK_NORM if norm else 0) | (ROPE_INTERLEAVED if interleaved else 0),
-              q_out.data_ptr(), k_out.data_ptr(), hq, hkv, d, _dtype_code(q), st))
+    qs, ks = (q.stride(0), k.stride(0)) if T > 1 else (hq * d, hkv * d)
+    rc = fn(q.data_ptr(), qs, k.data_ptr(), ks, positions.data_ptr(), T, cos_sin.data_ptr(),
+            n_pos, rot, _dptr(q_weight), _dptr(k_weight), eps,
+            (QK_NORM if norm else 0) | (ROPE_INTERLEAVED if interleaved else 0),
+            q_out.data_ptr(), k_out.data_ptr(), hq, hkv, d, code, st)
+    if rc:
+        _check(rc)
