@@ -919,8 +919,20 @@ __device__ __forceinline__ void store_row(const AttnArgs& a, const f32x4 (&acc)[
 // elements are keys 4 tt + e of block g4, the block whose values the lane holds as
 // A operand of the PV product (16 keys of dimension 16 dt + j: two k-steps).  The
 // score's k-steps take dims 64 c + 16 g4 + 8 u .. + 7, the halves u of a lane's load.
+// With kItemJoin the workgroup's four wavefronts hold the same rows over adjacent
+// keys: they leave their accumulators, references and sums in LDS, and each combines a
+// quarter of the output dims and writes them.
 template <int D, int NC>
-__device__ __forceinline__ void row_item8(const int32_t* it, int g, int poff, const AttnArgs& a) {
+struct JoinSmem {
+  f32x4 acc[4][NC][D / 16][64];  // [wavefront][column tile][16 dims][lane]
+};
+struct JoinStat {
+  float mc, l;  // reference (scaled; minus infinity without a key) and sum of a row
+};
+
+template <int D, int NC>
+__device__ __forceinline__ void row_item8(const int32_t* it, int g, int poff, const AttnArgs& a,
+                                          JoinSmem<D, NC>& sm, JoinStat (&stat)[4][2][16]) {
   constexpr int KC = D / 64;  // 64-dim groups of a key
   constexpr int DT = D / 16;  // 16-row tiles of O^T
   constexpr int kStep = kKeyStep8;
@@ -1085,6 +1097,63 @@ __device__ __forceinline__ void row_item8(const int32_t* it, int g, int poff, co
     l[c] += wave_xor(l[c], 16);
     l[c] += wave_xor(l[c], 32);
   }
+  if (it[I_FLAGS] & kItemJoin) {
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      if (g4 == 0) stat[w][c][j] = {m[c] == kNegInf ? kNegInf : mc[c], l[c]};
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) sm.acc[w][c][dt][lane] = acc[c][dt];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      JoinStat st[4];
+      float top = kNegInf;
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        st[v] = stat[v][c][j];
+        top = fmaxf(top, st[v].mc);
+      }
+      float sum = 0.f, f[4];
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        // a wavefront without a visible key counts for nothing, one without a number
+        // (its sum is NaN) stays
+        f[v] = st[v].mc == kNegInf ? (st[v].l == 0.f ? 0.f : 1.f) : fast_exp2(st[v].mc - top);
+        sum += f[v] == 0.f ? 0.f : f[v] * st[v].l;
+      }
+      const float inv = sum > 0.f ? 1.f / sum : 0.f;
+      const float lse_v = sum > 0.f ? kLn2 * (top + __log2f(sum)) : kNegInf;
+      const int64_t row = (int64_t)(qs + qi[c]) * a.hq + hq[c];
+      const int64_t prow = part + 16 * c + j;
+#pragma unroll
+      for (int i = 0; i < DT / 4; ++i) {
+        const int dt = 4 * i + w;
+        f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const f32x4 x = sm.acc[v][c][dt][lane];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[e] += f[v] == 0.f ? 0.f : f[v] * x[e];
+        }
+        if (!valid[c]) continue;
+        if (part < 0) {
+          __bf16 o4[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o4[e] = (__bf16)(o[e] * inv);
+          *reinterpret_cast<u32x2*>(a.out + row * D + 16 * dt + 4 * g4) = __builtin_bit_cast(u32x2, o4);
+        } else {
+          *reinterpret_cast<f32x4*>(a.ws_o + prow * D + 16 * dt + 4 * g4) = o * inv;
+        }
+      }
+      if (valid[c] && g4 == 0 && w == 0) {
+        if (part >= 0) a.ws_lse[prow] = sum == sum ? lse_v : sum;
+        else if (a.lse) a.lse[row] = lse_v;
+      }
+    }
+    return;
+  }
 #pragma unroll
   for (int c = 0; c < NC; ++c)
     if (valid[c]) store_row<D>(a, acc[c], l[c], mc[c], qs + qi[c], hq[c], part < 0 ? -1 : part + 16 * c + j, g4);
@@ -1113,8 +1182,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(waves_per_e
   const int n_shared = plan[H_N_SHARED_TMPL];
   const int n_tile = n_shared + plan[H_N_TILE_TMPL];  // templates before the row templates
   const int poff = g * plan[H_HEAD_PARTIAL];  // the kv-head's partial rows
+  // KV8: tiles and joined row items use the same LDS
+  constexpr size_t kTileBytes = (MIX & 1) ? sizeof(TileSmem<D, kTileSub>) : 0;
+  constexpr size_t kJoinBytes = (MIX & 4) ? sizeof(JoinSmem<D, 2>) : (MIX & 2) ? sizeof(JoinSmem<D, 1>) : 0;
+  __shared__ __align__(16) char lds8[KV8 ? (kTileBytes > kJoinBytes ? kTileBytes : kJoinBytes) : 16];
   if constexpr (MIX & 1) {
-    __shared__ TileSmem<D, kTileSub> sm;
+    __shared__ TileSmem<D, kTileSub> tile_lds;
+    TileSmem<D, kTileSub>* const tile_sm =
+        KV8 ? reinterpret_cast<TileSmem<D, kTileSub>*>(lds8) : &tile_lds;
+    TileSmem<D, kTileSub>& sm = *tile_sm;
     if constexpr ((MIX & 8) != 0) {
       if (ti == kWildcard) {
         // Take tail items (full tiles) from this XCD queue's list, then from
@@ -1203,18 +1279,19 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(waves_per_e
     }
   }
   if constexpr ((MIX & 6) != 0) {
+    __shared__ JoinStat stat8[4][2][16];
     if (ti >= n_tile) {
       // a quad of row templates, one per wavefront
       const int32_t* it =
           plan + plan[H_ROW_OFF] + (ti - n_tile + (threadIdx.x >> 6)) * kItemWords;
       if constexpr ((MIX & 4) != 0) {
         if (it[I_NROWS] > 16) {
-          if constexpr (KV8) row_item8<D, 2>(it, g, poff, a);
+          if constexpr (KV8) row_item8<D, 2>(it, g, poff, a, *reinterpret_cast<JoinSmem<D, 2>*>(lds8), stat8);
           else row_item<D, 2>(it, g, poff, a);
           return;
         }
       }
-      if constexpr (KV8) row_item8<D, 1>(it, g, poff, a);
+      if constexpr (KV8) row_item8<D, 1>(it, g, poff, a, *reinterpret_cast<JoinSmem<D, 1>*>(lds8), stat8);
       else row_item<D, 1>(it, g, poff, a);
     }
   }

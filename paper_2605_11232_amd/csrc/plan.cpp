@@ -494,12 +494,19 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
     // private parts of a sequence, within the workspace bound's part count; n_private
     // holds those of the few-row sequences
     std::vector<int32_t> n_private(n_seqs, 0);
+    // Over the 8-bit cache sequences whose keys give a workgroup's four wavefronts a row
+    // item's length each run as such: they join their results in LDS, a quarter of the
+    // parts that the merge would read.
+    auto row_waves = [&](int32_t r) -> int64_t {
+      const int64_t quarter = cdiv(cdiv(seq_lens[r] - kstart[r], 4), row_step) * row_step;
+      return kv8 && !on_tiles(r) && quarter > row_step && quarter >= row_chunk[r] ? 4 : 1;
+    };
     auto count_private = [&](int32_t r) {
       const int64_t L = seq_lens[r], len = L - kstart[r];
       const int64_t most = cdiv(L, kMinRowKeys) + (L > pa::kSharedMinKeys ? cdiv(L, pa::kSharedChunk) : 0) -
                            (cgroup[r] >= 0 ? cg_chunks[cgroup[r]] : 0);
       n_private[r] =
-          int32_t(std::max<int64_t>(1, std::min(cdiv(len, on_tiles(r) ? tile_keys : row_chunk[r]), most)));
+          int32_t(std::max<int64_t>(1, std::min(cdiv(len, on_tiles(r) ? tile_keys : row_waves(r) * row_chunk[r]), most)));
     };
     auto count_all_private = [&] {
       for (int32_t r = 0; r < n_seqs; ++r)
@@ -536,10 +543,12 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
         if (is_row(r)) {
           rest += double(keys) * num_kv_heads * key_bytes / kStepBytes;
           int64_t per = cdiv(keys, n_private[r]);
+          per = cdiv(per, row_waves(r));
           // without long sequences' tiles, rows of the usual length as of the small
           // launches' (992 shared keys in two chunks beside them: 64 requests of 240-800
           // keys, 32/8 heads, 29 us and 34)
-          if (!on_tiles(r)) per = 2 * (!long_seqs && per <= kMinRowKeys ? std::min(per, kSmallRowKeys) : per);
+          // (a 64-key step over the 8-bit cache as long as a tile's)
+          if (!on_tiles(r)) per = (kv8 ? 1 : 2) * (!long_seqs && per <= kMinRowKeys ? std::min(per, kSmallRowKeys) : per);
           longest = std::max(longest, per);
         } else {
           rest += 4.0 * head_dim * qlen(r) * num_q_heads * double(keys) / kStepFlops;
@@ -591,7 +600,8 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
         const int64_t keys = seq_lens[r] - kstart[r];
         launch_steps += double(keys) * num_kv_heads * key_bytes / kStepBytes;
         if (is_row(r))
-          other_steps = std::max(other_steps, cdiv(cdiv(keys, n_private[r]), pa::kTileStep));
+          other_steps = std::max(other_steps, cdiv(cdiv(keys, n_private[r] * row_waves(r)),
+                                                   pa::kTileStep));
       }
     }
     const int64_t split_keys = tile_split_keys(
@@ -619,6 +629,8 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
       row_cost.reserve(nr);
       t_groups.reserve(ng);
     }
+    std::vector<std::array<Rec, 4>> joined;  // row items of four wavefronts, and their keys
+    std::vector<int64_t> joined_cost;
     for (int32_t r = 0; r < n_seqs; ++r) {
       const int32_t n = qlen(r);
       const int32_t L = seq_lens[r];
@@ -631,6 +643,7 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
         // parts 0 .. first-1 are the shared prefix's key chunks
         const int32_t first = cgroup[r] >= 0 ? cg_chunks[cgroup[r]] : 0;
         const int32_t nsplit = n_private[r];
+        const int64_t waves = row_waves(r);
         // equal private key ranges, multiples of the key step, covering [k0s, L)
         const int64_t per = cdiv(cdiv(L - k0s, nsplit), kstep) * kstep;
         int32_t used = 0;
@@ -655,9 +668,20 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
             tile_cost.push_back((k1 - k0) * rows);
           } else {
             for (int32_t row0 = 0; row0 < rows; row0 += pa::kRowItemRows) {
-              t_rows.push_back({r, 0, row0, std::min(pa::kRowItemRows, rows - row0), int32_t(k0),
-                                int32_t(k1), part < 0 ? -1 : part + row0, 0});
-              row_cost.push_back(k1 - k0);
+              const Rec item = {r, 0, row0, std::min(pa::kRowItemRows, rows - row0), int32_t(k0),
+                                int32_t(k1), part < 0 ? -1 : part + row0, waves > 1 ? pa::kItemJoin : 0};
+              if (waves == 1) {
+                t_rows.push_back(item);
+                row_cost.push_back(k1 - k0);
+                continue;
+              }
+              const int64_t wave_keys = cdiv(cdiv(k1 - k0, waves), row_step) * row_step;
+              joined.push_back({item, item, item, item});
+              for (int64_t w = 0; w < waves; ++w) {
+                joined.back()[w][pa::I_KV0] = int32_t(std::min(k0 + w * wave_keys, k1));
+                joined.back()[w][pa::I_KV1] = int32_t(std::min(k0 + (w + 1) * wave_keys, k1));
+              }
+              joined_cost.push_back(wave_keys);
             }
           }
         }
@@ -773,7 +797,10 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
     // empty items) so a workgroup's waves share one kv-head.
     {
       const auto ord = order_longest_first(row_cost);
-      sorted_rows.reserve(cdiv(int64_t(ord.size()), 4) * 4);
+      sorted_rows.reserve(cdiv(int64_t(ord.size()), 4) * 4 + 4 * joined.size());
+      // joined items come first, being the longer ones
+      for (int32_t i : order_longest_first(joined_cost))
+        sorted_rows.insert(sorted_rows.end(), joined[i].begin(), joined[i].end());
       for (int32_t i : ord) sorted_rows.push_back(t_rows[i]);
       while (sorted_rows.size() % 4) sorted_rows.push_back({-1, 0, 0, 0, 0, 0, -1, 0});
     }
@@ -893,7 +920,7 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
   for (const auto& g : t_groups) info->n_merge_rows += int64_t(g[pa::G_NROWS]) * num_kv_heads;
   info->grid = int32_t(grid);
   bool wide = false;
-  for (const auto& it : t_rows) wide = wide || it[pa::I_NROWS] > 16;
+  for (const auto& it : sorted_rows) wide = wide || it[pa::I_NROWS] > 16;
   info->variant = dtype == PA_F32 ? (by_row ? pa::kVariantF32ByRow : 0)
                                   : (pa::kVariantBf16 | (wide ? pa::kVariantWideRows : 0) |
                                      (n_tail ? pa::kVariantTail : 0) |

@@ -88,7 +88,11 @@ enum : int32_t {
   kItemWords = 8
 };
 
+// kItemJoin (8-bit cache): the workgroup's four row items hold the same rows over
+// adjacent key ranges, any of them empty; they combine their results in LDS and write
+// one: the same part in all four.
 constexpr int32_t kItemStream = 1;
+constexpr int32_t kItemJoin = 2;
 
 // Shared-prefix item: gathered rows [row0, row0 + nrows) of a cascade group's
 // members (member m owns gathered rows m * rpm .. m * rpm + rpm - 1, its own

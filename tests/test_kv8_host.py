@@ -243,11 +243,67 @@ def test_binding_refusals():
     bad("arg", B.qk_norm_rope, q, rows.float(), pos, tab, q, rows)
 
 
+def check_plan8(plan, info, L, q, G, hkv, D):
+    """Every (sequence, kv-head, row) is produced exactly once, by one item or by
+    parts whose key ranges tile its keys and whose partial rows are its merge
+    group's; the four items of a joined workgroup hold the same rows over adjacent
+    keys, at most 64 blocks each, and count as one."""
+    from tests.test_capi_host import parse_plan
+    h, shared, tiles, rows, groups = parse_plan(plan)
+    assert h[0] == 0x31304150 and len(rows) % 4 == 0
+    assert info.grid == len(shared) + h[3] + len(rows) // 4
+    assert bool(info.variant & 2) == any(t[3] > 16 for t in rows if t[0] >= 0)
+    items = list(tiles)
+    for i in range(0, len(rows), 4):
+        quad = rows[i:i + 4]
+        assert all(t[5] - t[4] <= 1024 and t[3] <= 32 for t in quad if t[0] >= 0)
+        if quad[0][7] & 2:
+            assert all(t[:4] + t[6:] == quad[0][:4] + quad[0][6:] and t[0] >= 0 for t in quad)
+            assert all(a[5] == b[4] and b[4] <= b[5] for a, b in zip(quad, quad[1:]))
+            assert quad[0][4] < quad[0][5] <= quad[3][5] and quad[0][4] % 16 == 0
+            assert all(t[4] % 16 == 0 for t in quad if t[4] < t[5])
+            items.append(quad[0][:5] + [quad[3][5]] + quad[0][6:])
+        else:
+            items += [t for t in quad if t[0] >= 0]
+            assert not any(t[7] & 2 for t in quad)
+    cover, writes = {}, []
+    for seq, kvh, row0, nrows, kv0, kv1, part, _ in items:
+        assert kv0 % 16 == 0 and 0 <= kv0 < kv1 <= L[seq]
+        for lr in range(nrows):
+            cover.setdefault((seq, kvh, row0 + lr), []).append((kv0, kv1, part + lr if part >= 0 else -1))
+    for moff, kvh, row0, nrows, kv0, kv1, rpm, bseq, poff in shared:
+        assert kv0 % 64 == 0 and kv1 % 64 == 0
+        for rg in range(row0, row0 + nrows):
+            m, rl = divmod(rg, rpm)
+            seq, base = plan[moff + 2 * m], plan[moff + 2 * m + 1] + poff
+            assert kv1 <= L[seq] - q[seq]
+            cover.setdefault((seq, kvh, rl), []).append((kv0, kv1, base + rl))
+    expected = {}
+    for seq, kvh, row0, nrows, nsplit, part, stride, _ in groups:
+        for lr in range(nrows):
+            expected[(seq, kvh, row0 + lr)] = {part + sp * stride + lr for sp in range(nsplit)}
+    assert len(cover) == int(q.sum()) * G * hkv
+    for (seq, kvh, rho), ranges in cover.items():
+        ranges.sort()
+        if len(ranges) == 1 and ranges[0][2] < 0:
+            assert (seq, kvh, rho) not in expected and ranges[0][0] == 0
+            assert ranges[0][1] >= L[seq] - q[seq] + rho // G + 1
+        else:
+            parts = [p for _, _, p in ranges]
+            assert set(parts) == expected[(seq, kvh, rho)] and len(set(parts)) == len(parts)
+            assert ranges[0][0] == 0 and ranges[-1][1] == L[seq]
+            assert all(a[1] == b[0] for a, b in zip(ranges, ranges[1:]))
+            writes += parts
+    assert sorted(writes) == list(range(int(info.partial_rows)))
+    assert int(info.workspace_bytes) == int(info.partial_rows) * (D + 1) * 4
+    assert B.workspace_size(int(q.sum()), hkv * G, D, int(max(L))) >= int(info.workspace_bytes)
+    return tiles, rows
+
+
 @pytest.mark.parametrize("seed", range(30))
 def test_plans_cover_every_row_once(seed):
     """Random launches over the 8-bit cache, prefixes shared, rows of every item
     kind (sequences of 33 to 64 rows run as two row items)."""
-    from tests.test_capi_host import check_plan, parse_plan
     r = np.random.default_rng(seed)
     n, hkv, G = int(r.integers(1, 40)), int(r.choice([1, 2, 8])), int(r.choice([1, 4, 7, 8, 40, 64]))
     L = r.integers(1, 4000, size=n)
@@ -270,8 +326,7 @@ def test_plans_cover_every_row_once(seed):
         nxt += nb - pb
     D = int(r.choice([64, 128]))
     plan, info = B.plan(kind, n_q, L, cu, hkv * G, hkv, D, 16, B.PA_BF16_KV8, block_table=bt)
-    check_plan(plan, info, L, cu, G, hkv, D)
-    _, _, tiles, rows, _ = parse_plan(plan)
+    tiles, rows = check_plan8(plan, info, L, q, G, hkv, D)
     assert all(q[t[0]] * G <= 64 for t in rows if t[0] >= 0)
     if kind != B.KIND_DECODE:
         assert all(q[t[0]] * G > 64 for t in tiles)
