@@ -49,6 +49,19 @@ namespace {
 
 constexpr int kXcds = 8;
 constexpr int64_t kRowWavesPerCu = 10;      // row-item split target
+// Over the 8-bit cache: half the bytes leave an item's start and its parts a larger
+// share, so they are longer.  Verifications (more than 16 rows, two workgroups per CU)
+// take the least with all workgroups resident.  us at 10, 5 and 4 wavefronts per CU, no
+// shared prefix, 24 sequences of 1024-4096 keys, 64/8 heads: one token 34.4, 32.2, 34.0,
+// two 37.3, 33.6, 35.0, five 54, 44.7, 47.5, and on 4096 shared keys 76, 71, 64.6; 64
+// decode requests of 32/8 heads on 2048 shared keys 31.4, 27.1, 27.0, 84 at head_dim 64
+// 21.7, 18.4, 20.5.
+constexpr int64_t kRowWavesPerCu8 = 5, kWideRowWavesPerCu8 = 4;
+// Fewest keys of a shared prefix's chunk there, unless the launch leaves every other CU
+// without a workgroup: 64 decode requests 26.9 us, 29.1 with 256 (768: 33.3), 4
+// verifications on 4096 shared keys 22.0 and 24.7 (27.2); 4 decode requests (104
+// workgroups) 12.0 with 256, 15.2 with 384.
+constexpr int64_t kSharedMinKeys8 = 512;
 constexpr int64_t kPrivateTileKeys = 4160;  // most private keys a few-row tile item covers
 constexpr int64_t kMinTileKeys = 256;       // fewest, in launches that leave compute units idle
 constexpr int64_t kMinRowKeys = 256;        // split target floor of row items
@@ -440,13 +453,16 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
     // aim for enough single-wave items to keep kRowWavesPerCu wavefronts per
     // CU busy, a split target of at least kMinRowKeys and at most 1024 keys
     // per item (halved for the tail below).
-    int64_t row_keys = 0, item_keys = 0, long_tiles = 0, longest_row = 0;
+    bool wide_rows = false;
+    int64_t row_keys = 0, item_keys = 0, row_quads = 0, long_tiles = 0, longest_row = 0;
     std::vector<FewTile> few;  // sequences on_tiles: private keys, rows
     for (int32_t r = 0; r < n_seqs; ++r) {
       const int64_t keys = seq_lens[r] - kstart[r];
       if (!is_row(r)) long_tiles += cdiv(int64_t(qlen(r)) * G, pa::kTileRows) * num_kv_heads;
       else if (on_tiles(r)) few.push_back({keys, int64_t(qlen(r)) * G, cgroup[r] >= 0});
       else {
+        row_quads += num_kv_heads * row_pieces(r);
+        wide_rows = wide_rows || qlen(r) * G > 16;
         row_keys += keys * num_kv_heads;
         item_keys += keys * num_kv_heads * row_pieces(r);
         longest_row = std::max(longest_row, keys);
@@ -466,7 +482,7 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
             ? kPrivateTileKeys
             : few_tile_keys(few, num_kv_heads, head_dim, num_cus, num_cus - long_tiles, row_steps,
                             !cg_keys.empty() || longest_row > kMinRowKeys);
-    const int64_t target_waves = int64_t(num_cus) * kRowWavesPerCu;
+    const int64_t target_waves = int64_t(num_cus) * (!kv8 ? kRowWavesPerCu : wide_rows ? kWideRowWavesPerCu8 : kRowWavesPerCu8);
     // The sequences with the fewest private keys, up to kTailWork of the row
     // work, get half-length items: ordered longest first, those run last, so
     // the launch drains sooner.  A sequence keeps at most cdiv(L, kMinRowKeys)
@@ -496,10 +512,14 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
     std::vector<int32_t> n_private(n_seqs, 0);
     // Over the 8-bit cache sequences whose keys give a workgroup's four wavefronts a row
     // item's length each run as such: they join their results in LDS, a quarter of the
-    // parts that the merge would read.
+    // parts that the merge would read.  So do shorter ones, down to two steps a wavefront,
+    // while there are no more of them than workgroups run at once (24 verifications of 5
+    // tokens 45 us, 51 with separate items; 256 decode requests of 256-1152 keys 79, 74
+    // with separate ones).
     auto row_waves = [&](int32_t r) -> int64_t {
       const int64_t quarter = cdiv(cdiv(seq_lens[r] - kstart[r], 4), row_step) * row_step;
-      return kv8 && !on_tiles(r) && quarter > row_step && quarter >= row_chunk[r] ? 4 : 1;
+      return kv8 && !on_tiles(r) && quarter >= 2 * row_step &&
+                     (quarter >= row_chunk[r] || row_quads <= 2 * num_cus) ? 4 : 1;
     };
     auto count_private = [&](int32_t r) {
       const int64_t L = seq_lens[r], len = L - kstart[r];
@@ -537,10 +557,12 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
     if (!cg_keys.empty()) {
       double rest = 0;      // steps
       int64_t longest = 0;  // keys, in tile steps
+      int64_t row_wgs = 0;
       for (int32_t r = 0; r < n_seqs; ++r) {
         if (qlen(r) == 0) continue;
         const int64_t keys = seq_lens[r] - kstart[r];
         if (is_row(r)) {
+          row_wgs += cdiv(row_pieces(r) * n_private[r] * num_kv_heads * row_waves(r), 4);
           rest += double(keys) * num_kv_heads * key_bytes / kStepBytes;
           int64_t per = cdiv(keys, n_private[r]);
           per = cdiv(per, row_waves(r));
@@ -554,16 +576,23 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
           rest += 4.0 * head_dim * qlen(r) * num_q_heads * double(keys) / kStepFlops;
         }
       }
-      int64_t row_tiles = 0;
+      int64_t row_tiles = 0, chunk_wgs = 0;
       for (size_t c = 0; c < cg_keys.size(); ++c) {
         const int64_t members = cg_begin[c + 1] - cg_begin[c];
         row_tiles += cdiv(members * qlen(cg_seqs[cg_begin[c]]) * G, pa::kTileRows);
+        chunk_wgs += cdiv(members * qlen(cg_seqs[cg_begin[c]]) * G, pa::kTileRows) * num_kv_heads *
+                     (cg_keys[c] / std::max<int64_t>(longest, pa::kSharedMinKeys));
       }
-      longest = std::max<int64_t>(longest, pa::kSharedMinKeys);
+      const bool few_wgs = 2 * (row_wgs + chunk_wgs) <= num_cus;
+      longest = std::max<int64_t>(longest, kv8 && !few_wgs ? kSharedMinKeys8 : pa::kSharedMinKeys);
       const int64_t share = 1 + int64_t(std::min(rest, 1e6) * 0.4 * pa::kTileStep);
+      // beside verifications' row items, whose workgroups need the room, three on four CUs
+      // (24 of 5 tokens on 4096 shared keys 64.6 us; one per CU 70; one on two 60.4, where
+      // 16 on 8192 keys take 71 us against 59)
+      const int64_t most_wgs = kv8 && wide_rows ? int64_t(num_cus) * 3 / 4 : num_cus;
       for (size_t c = 0; c < cg_keys.size(); ++c) {
         const int64_t n = std::min<int64_t>({cg_keys[c] / longest, (cg_keys[c] + share / 2) / share,
-                                             num_cus / (row_tiles * num_kv_heads)});
+                                             most_wgs / (row_tiles * num_kv_heads)});
         if (n <= cg_chunks[c]) continue;
         cg_chunks[c] = int32_t(n);
         for (int32_t m = cg_begin[c]; m < cg_begin[c + 1]; ++m) count_private(cg_seqs[m]);
