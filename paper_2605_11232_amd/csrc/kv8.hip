@@ -116,13 +116,15 @@ __device__ __forceinline__ uint32_t first_bytes(uint32_t old, uint32_t x, int ke
   return (old & m) | (x & ~m);
 }
 
-// Eight values of T as loaded, and as float32.
+// Eight values of T as loaded, and as float32.  Non-temporal: the rows are read once (64
+// prompts whose rows are in no cache 49 us, 55 with plain loads; 46 where the last-level
+// cache holds them all).
 template <typename T>
 struct Raw8 {
   u32x4 x[sizeof(T) / 2];
   __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-    for (size_t i = 0; i < sizeof(T) / 2; ++i) x[i] = ld16(p + 16 / sizeof(T) * i);
+    for (size_t i = 0; i < sizeof(T) / 2; ++i) x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + 16 / sizeof(T) * i));
   }
   __device__ __forceinline__ float at(int i) const {
     if constexpr (sizeof(T) == 2) return __uint_as_float(i % 2 ? x[0][i / 2] & 0xFFFF0000u : x[0][i / 2] << 16);
