@@ -760,15 +760,16 @@ def _kv8_attn_args(q, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlen
             and block_table.dtype == i32 and seq_lens.dtype == i32 and cu_seqlens_q.dtype == i32
             and block_table.is_contiguous() and seq_lens.is_contiguous()
             and cu_seqlens_q.is_contiguous()
-            and plan_dev.dtype == i32 and plan_dev.numel() >= info.plan_words
-            and plan_dev.is_contiguous()
+            and (plan_dev is None or (plan_dev.dtype == i32 and plan_dev.is_contiguous()
+                                      and plan_dev.numel() >= info.plan_words
+                                      and plan_dev.get_device() == dev))
             and (lse is None or (lse.dtype == t.float32 and lse.shape == (total_q, hq)
                                  and lse.is_contiguous() and lse.get_device() == dev))
             and (workspace is None or (workspace.is_contiguous()
                                        and workspace.get_device() == dev))
             and st >= 0 and q.get_device() == out.get_device() == k_cache.get_device()
             == scales.get_device() == block_table.get_device() == seq_lens.get_device()
-            == cu_seqlens_q.get_device() == plan_dev.get_device() == dev):
+            == cu_seqlens_q.get_device() == dev):
         _refuse_cache(t, k_cache, v_cache, scales)
         _refuse(PA_ERR_UNSUPPORTED, [
             (q.dtype == out.dtype == t.bfloat16,
@@ -778,17 +779,16 @@ def _kv8_attn_args(q, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlen
              "q and out must be contiguous [T, Hq, D] of the cache's head_dim"),
             (lse is None or (lse.dtype == t.float32 and lse.shape == (total_q, hq)
                              and lse.is_contiguous()), "lse must be contiguous float32 [T, Hq]"),
-            (plan_dev.dtype == i32 and plan_dev.is_contiguous()
-             and plan_dev.numel() >= info.plan_words,
-             f"plan: {plan_dev.numel()} words of {plan_dev.dtype}, its info says "
-             f"{info.plan_words} of int32"),
+            (plan_dev is None or (plan_dev.dtype == i32 and plan_dev.is_contiguous()
+                                  and plan_dev.numel() >= info.plan_words),
+             f"plan: contiguous int32 of at least its info's {info.plan_words} words"),
             (workspace is None or workspace.is_contiguous(), "workspace must be contiguous")])
         _refuse_metadata(t, block_table, seq_lens, cu_seqlens_q)
         _refuse_device(q, out, lse, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlens_q,
                        plan_dev, workspace)
     return (q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), scales.data_ptr(), nb,
             block_table.data_ptr(), width, seq_lens.data_ptr(), cu_seqlens_q.data_ptr(), n,
-            total_q, hq, hkv, d, bs, d ** -0.5 if scale is None else scale, plan_dev.data_ptr(),
+            total_q, hq, hkv, d, bs, d ** -0.5 if scale is None else scale, _dptr(plan_dev),
             C.byref(info)), st
 
 

@@ -90,8 +90,9 @@ int check_kv8_rows(const char* fn, const void* k_rows, int64_t k_stride, const v
     return fail(PA_ERR_ARG, "%s: row strides %lld and %lld, a token's heads take %lld", fn,
                 (long long)k_stride, (long long)v_stride, (long long)row);
   if (!aligned16(k_rows, k_stride, dtype) || !aligned16(v_rows, v_stride, dtype) ||
-      !aligned16(k_cache, 0, dtype) || !aligned16(v_cache, 0, dtype))
-    return fail(PA_ERR_ARG, "%s: rows and caches must be 16-byte aligned", fn);
+      !aligned16(k_cache, 0, dtype) || !aligned16(v_cache, 0, dtype) ||
+      (reinterpret_cast<uintptr_t>(scales) & 3))
+    return fail(PA_ERR_ARG, "%s: rows and caches must be 16-byte aligned, scales 4-byte", fn);
   return PA_OK;
 }
 
@@ -172,10 +173,10 @@ int attn_common(const char* fn, int32_t want_kind, const void* q, const void* k_
   if (!q || !k_cache || !v_cache || !block_table || !seq_lens || !cu_seqlens_q || !out ||
       (kv8 && !scales))
     return fail(PA_ERR_ARG, "%s: NULL device pointer", fn);
-  // the 8-bit calls are new, so they can ask for what the kernels' 16-byte accesses need
-  if (kv8 && ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k_cache) |
-               reinterpret_cast<uintptr_t>(v_cache) | reinterpret_cast<uintptr_t>(out)) & 15))
-    return fail(PA_ERR_ARG, "%s: q, out and caches must be 16-byte aligned", fn);
+  if (kv8 && (((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k_cache) |
+                reinterpret_cast<uintptr_t>(v_cache) | reinterpret_cast<uintptr_t>(out)) & 15) ||
+              (reinterpret_cast<uintptr_t>(scales) & 3)))
+    return fail(PA_ERR_ARG, "%s: q, out and caches must be 16-byte aligned, scales 4-byte", fn);
   if (dtype == PA_F32) {
     rc = dev::launch_attn_f32(q, k_cache, v_cache, num_blocks, block_table, max_blocks_per_seq,
                               seq_lens, cu_seqlens_q, n_seqs, total_q, num_q_heads, num_kv_heads,
@@ -200,9 +201,10 @@ int attn_common(const char* fn, int32_t want_kind, const void* q, const void* k_
       // the workspace is the library's per-device array
       if (static_cast<uint64_t>(info->workspace_bytes) > PA_NOALLOC_WORKSPACE_BYTES)
         return fail(PA_ERR_ARG, "%s: the plan needs %lld bytes of workspace, more than the "
-                    "%zu bytes this call holds per device; call pa_attn_decode with a "
+                    "%zu bytes this call holds per device; call %s with a "
                     "workspace of that size", fn, (long long)info->workspace_bytes,
-                    (size_t)PA_NOALLOC_WORKSPACE_BYTES);
+                    (size_t)PA_NOALLOC_WORKSPACE_BYTES,
+                    kv8 ? "pa_kv8_attn_decode" : "pa_attn_decode");
       workspace = nullptr;
       workspace_bytes = 0;
       if (info->workspace_bytes > 0) {

@@ -343,7 +343,7 @@ int launch_kv8_append(const void* kn, int64_t k_stride, const void* vn, int64_t 
   const Kv8Args a = with_slots({bt, seq_lens, cu, static_cast<uint8_t*>(kc), static_cast<uint8_t*>(vc), scales,
                   k_stride, v_stride, max_blocks, n_seqs, n, nb, hkv, 0, false});
   const int64_t grid = (a.slots * hkv + 3) / 4;  // a wavefront per (block, kv-head)
-  if (grid > INT32_MAX) return static_cast<int>(hipErrorInvalidValue);
+  if (grid > INT32_MAX || a.slots > INT32_MAX) return static_cast<int>(hipErrorInvalidValue);
 #define PA_KV8(T, DD)                                                                            \
   hipLaunchKernelGGL((kv8_append_kernel<T, DD>), dim3(unsigned(grid)), dim3(256), 0, stream,     \
                      static_cast<const T*>(kn), static_cast<const T*>(vn), a)
@@ -367,7 +367,7 @@ int launch_kv8_read(void* k_out, int64_t k_stride, void* v_out, int64_t v_stride
                   static_cast<uint8_t*>(const_cast<void*>(vc)), const_cast<uint8_t*>(scales),
                   k_stride, v_stride, max_blocks, n_seqs, n, nb, hkv, 0, false});
   const int64_t grid = (a.slots * hkv + 3) / 4;
-  if (grid > INT32_MAX) return static_cast<int>(hipErrorInvalidValue);
+  if (grid > INT32_MAX || a.slots > INT32_MAX) return static_cast<int>(hipErrorInvalidValue);
 #define PA_KV8(T, DD)                                                                            \
   hipLaunchKernelGGL((kv8_read_kernel<T, DD>), dim3(unsigned(grid)), dim3(256), 0, stream,       \
                      static_cast<T*>(k_out), static_cast<T*>(v_out), a)

@@ -379,6 +379,137 @@ def test_attention_scale(scale):
                   <= ds + 2.0 ** -16 * np.maximum(1, np.abs(lse)))
 
 
+# rows merged from key-split tiles and from row items, joined ones, a shared
+# prefix's chunks, whole tiles, two row items of one sequence
+NAN = {
+    "tiles": (8, 2, 128, [100], [2100], 0),
+    "tiles-whole": (8, 2, 128, [100], [120], 0),
+    "two-items": (16, 2, 64, [5] * 2, [1000, 2053], 0),
+    "decode": (32, 8, 128, [1, 1], [1000, 257], 0),
+    "decode-joined": (8, 2, 128, [1], [700], 0),
+    "decode-short": (8, 2, 64, [1] * 5, [30, 1, 64, 65, 17], 0),
+    "decode-shared": (8, 2, 128, [1] * 3, [2100, 2049, 2563], 2048),
+}
+
+
+@pytest.mark.parametrize("where", ["query", "key", "value"])
+@pytest.mark.parametrize("name", list(NAN))
+def test_rows_without_a_number_stay_visible(name, where):
+    """A row whose query, or a key it sees, is NaN comes out NaN (its log-sum-exp
+    minus infinity) however its keys are split, one that sees a NaN value in that
+    dim; no other row changes."""
+    hq, hkv, d, q_lens, lens, prefix = NAN[name]
+    cfg = synth.AttnConfig(f"kv8-nan-{name}", "bf16", hq, hkv, d, 16, 7300 + len(name))
+    wl, dv, orc = replay(cfg, q_lens, lens, 53, prefix)
+    ro = orc.launch(wl.launches[0])
+    p = dv.prepare(wl.launches[0])
+    dv.append(p)
+    dv.attend(p)
+    torch.cuda.synchronize()
+    plain, plain_lse = p.out.clone(), p.lse.clone()
+    last = q_lens[0] - 1  # of the first sequence
+    slot = int(p.slots[last])
+    bad = torch.zeros(plain.shape, dtype=torch.bool, device="cuda")
+    if where == "query":
+        p.q[last, 1, 3] = float("nan")
+        bad[last, 1] = True
+    elif where == "key":
+        dv.k_cache.view(torch.uint8)[slot // 16, 0, 0, slot % 16, 3] = 0x7F
+        bad[last, :hq // hkv] = True
+    else:
+        dv.v_cache.view(torch.uint8)[slot // 16, 0, 5, slot % 16] = 0xFF
+        bad[last, :hq // hkv, 5] = True
+    dv.attend(p)
+    torch.cuda.synchronize()
+    keep = ~bad
+    if where == "value":
+        keep[:q_lens[0], :hq // hkv, 5] = False  # earlier tokens of the launch: either
+        assert torch.equal(p.lse, plain_lse)
+    else:
+        assert torch.equal(p.lse == -float("inf"), bad.all(2))
+        # a wavefront's reference moves for all its rows: each result is within 2^-16 of
+        # itself (the head of this file), so two are within 2^-15
+        ok = ~bad.all(2)
+        assert torch.all((p.lse - plain_lse).abs()[ok] <= 2.0 ** -15 * plain_lse.abs().clamp(min=1)[ok])
+    assert torch.isnan(p.out[bad]).all()
+    # and the outputs are within the bound of the same exact ones
+    md = ro["meta"]
+    bo, _ = bounds(wl.launches[0].q.get().astype(np.float64), orc.k_cache, orc.v_cache,
+                   md["block_table"], md["seq_lens"], md["cu_seqlens_q"], hkv, ro["out"], ro["lse"])
+    diff = (p.out.double() - plain.double()).abs().cpu().numpy()
+    assert np.all(diff[keep.cpu().numpy()] <= 2 * bo[keep.cpu().numpy()])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("q_len", [1, 130])
+def test_values_near_the_largest_stay_finite(d, q_len):
+    """One key's probability lies 2^11 above the others', its values are 3e35:
+    every sum stays in range."""
+    L, at = 500, 300
+    cfg = synth.AttnConfig(f"kv8-large-{d}", "bf16", 4, 2, d, 16, 7400 + d)
+    wl, dv, _ = replay(cfg, [q_len], [L], 54)
+    p = dv.prepare(wl.launches[0])
+    table = p.meta["block_table"]
+    k = np.zeros((L, 2, d), np.float32)
+    v = np.zeros((L, 2, d), np.float32)
+    k[at, :, 0] = 11 * 0.6931 * d ** 0.5 / 8
+    v[at] = 3e35
+    m = [dev(x) for x in meta(table, [L], [L])]
+    B.kv8_append(dev(k), dev(v), *m, dv.k_cache, dv.v_cache, dv.scales)
+    p.q.zero_()
+    p.q[:, :, 0] = 8.0
+    dv.attend(p)
+    ko, vo = (torch.empty((L, 2, d), device="cuda") for _ in range(2))
+    B.kv8_read(ko, vo, *m, dv.k_cache, dv.v_cache, dv.scales)
+    torch.cuda.synchronize()
+    w = np.exp(float(ko[at, 0, 0].double()) * 8 * d ** -0.5)
+    val = float(vo[at, 0, 0].double())
+    seen = np.arange(L - q_len + 1, L + 1).astype(float)
+    ref = np.where(seen > at, w / (w + seen - 1), 0.0)[:, None, None]
+    got = p.out.double().cpu().numpy() / val
+    assert np.all(np.abs(got - ref) <= (2 * 2.0 ** -8 + 2.0 ** -12) * ref)
+
+
+def test_decode_of_many_heads_without_workspace():
+    """More than 32 heads per kv-head in a launch whose split row items would not
+    fit the array of the call without workspace: tile items, streamed."""
+    n, hq, hkv, d = 243, 128, 2, 128
+    r = np.random.default_rng(8)
+    lens = [513 + i % 11 for i in range(n)]
+    table, nb = tables(lens, 8)
+    c = Cache(nb, hkv, d, 8)
+    # finite codes of ordinary scales everywhere
+    for t in (c.k, c.v):
+        u = t.view(torch.uint8)
+        u.copy_(torch.where((u & 0x7F) == 0x7F, u & 0x87, u))
+    c.scales.copy_(dev(r.integers(117, 120, c.scales.shape).astype(np.uint8)))
+    m = meta(table, lens, [1] * n)
+    plan, info = B.plan(B.KIND_DECODE, 1, m[1], m[2], hq, hkv, d, 16, B.PA_BF16_KV8,
+                        block_table=m[0])
+    assert info.n_tile_items > 0 and info.workspace_bytes <= B.NOALLOC_WORKSPACE_BYTES
+    q = torch.randn((n, hq, d), device="cuda").to(torch.bfloat16)
+    out = torch.empty_like(q)
+    dm = [dev(x) for x in m]
+    B.kv8_attention_decode_noalloc(q, *c.args, *dm, dev(plan), info, out)
+    torch.cuda.synchronize()
+    s = torch.exp2(c.scales.double() - 127)
+    k = (c.k.double() * s[:, :, 0, None, None, None]).transpose(2, 3).reshape(nb, hkv, 16, d)
+    v = (c.v.double() * s[:, :, 1, None, None]).transpose(2, 3)
+    for i in range(0, n, 37):
+        b = torch.from_numpy(table[i][table[i] >= 0]).cuda().long()
+        kk = k[b].transpose(0, 1).reshape(hkv, -1, d)[:, :lens[i]]
+        vv = v[b].transpose(0, 1).reshape(hkv, -1, d)[:, :lens[i]].contiguous()
+        qq = q[i].double().view(hkv, hq // hkv, d)
+        sc = torch.bmm(qq, kk.transpose(1, 2).contiguous()) * d ** -0.5
+        pr = torch.softmax(sc, 2)
+        ref = torch.bmm(pr, vv).view(hq, d)
+        A = torch.bmm(pr, vv.abs()).view(hq, d)
+        # scores' sums: (D + 4) 2^-24 scale |q| |k|, |q| of 128 normal values below 16
+        ds = (d + 4) * 2.0 ** -24 * 16 * float(kk.norm(dim=2).max()) * d ** -0.5
+        assert torch.all((out[i].double() - ref).abs()
+                         <= 2.0 ** -8 * ref.abs() + (2.0 ** -8 + 2 * ds + 2.0 ** -16) * A)
+
+
 # ---- norms and rotation -----------------------------------------------------------------------
 
 ROPE = [
@@ -466,7 +597,7 @@ def test_norm_rope(case):
 
 class Chain:
     """A decode step of one layer, as a serving program runs it: norms and rotation
-    of the projection's rows, append, attention, all on 8-bit cache."""
+    of the projection's rows, append, attention, and the new tokens read back."""
 
     def __init__(self, lens, n_new, hq=8, hkv=2, d=128, seed=0):
         r = np.random.default_rng([seed, 4])
@@ -492,6 +623,7 @@ class Chain:
         self.qkv = torch.empty((self.T, hq + 2 * hkv, d), dtype=torch.bfloat16, device="cuda")
         self.q = torch.empty((self.T, hq, d), dtype=torch.bfloat16, device="cuda")
         self.k = torch.empty((self.T, hkv, d), dtype=torch.bfloat16, device="cuda")
+        self.k_back, self.v_back = torch.empty_like(self.k), torch.empty_like(self.k)
         self.out = torch.empty_like(self.q)
         self.lse = torch.empty((self.T, hq), dtype=torch.float32, device="cuda")
         self.kind = B.KIND_DECODE if n_new == 1 else B.KIND_VERIFY
@@ -512,6 +644,7 @@ class Chain:
         B.kv8_append(self.k, self.qkv[:, hq + hkv:], *self.dm, *self.cache.args, stream=stream)
         B.kv8_attention(self.kind, self.q, *self.cache.args, *self.dm, self.plan, self.info, self.ws,
                         self.out, self.lse, stream=stream)
+        B.kv8_read(self.k_back, self.v_back, *self.dm, *self.cache.args, stream=stream)
 
     def check(self, label):
         """The rotated rows against the oracle's, then everything after them from the
@@ -523,6 +656,10 @@ class Chain:
             assert np.all(np.abs(got.double().cpu().numpy() - y) <= b), label
         kv8.append(self.kc, self.vc, self.ex, *self.m, self.k.double().cpu().numpy(),
                    self.x[:, hq + hkv:])
+        seq = np.repeat(np.arange(len(self.lens)), self.n_new)
+        blk, off = self.table[seq, self.pos // 16], self.pos % 16
+        assert np.array_equal(self.k_back.double().cpu().numpy(), self.kc[blk, :, off]), label
+        assert np.array_equal(self.v_back.double().cpu().numpy(), self.vc[blk, :, :, off]), label
         q = self.q.double().cpu().numpy()
         ro, rl = paged_attention(q, self.kc, self.vc, *self.m, hkv)
         bo, bl = bounds(q, self.kc, self.vc, *self.m, hkv, ro, rl)
@@ -592,7 +729,7 @@ def test_workload_steps():
         wl = synth.workload(name, scale=scale, steps=2)
         cfg = wl.cfg
         dv, orc = DeviceReplay(wl, kv8=True).setup(), OracleReplay(wl, kv8=True).setup()
-        launches = list(wl.launches[:2])
+        launches = list(wl.launches[:2]) + ([wl.step(1)] if wl.step else [])
         n, T = max(len(x.seq_ids) for x in launches), max(x.total_q for x in launches)
         st = [Staging(dv.device, n, wl.max_blocks_per_seq, T,
                       plan_words_bound(cfg, n, T, wl.max_blocks_per_seq)) for _ in range(2)]

@@ -8,7 +8,8 @@ import pytest
 import torch
 
 from oracle import kv8
-from paper_2605_11232_amd import binding as B
+from paper_2605_11232_amd import binding as B, synth
+from paper_2605_11232_amd.runtime import plan_words_bound
 
 
 def e4m3_values():
@@ -104,7 +105,7 @@ def test_rows_refusals(name):
                      ({"ks": 255}, B.PA_ERR_ARG), ({"vs": 128}, B.PA_ERR_ARG),
                      ({"ks": 260}, B.PA_ERR_ARG), ({"k": 264}, B.PA_ERR_ARG),
                      ({"v": 520}, B.PA_ERR_ARG), ({"kc": 1032}, B.PA_ERR_ARG),
-                     ({"vc": 2052}, B.PA_ERR_ARG)):
+                     ({"vc": 2052}, B.PA_ERR_ARG), ({"sc": 66}, B.PA_ERR_ARG)):
         assert fn(*rows_args(**kw)) == code, kw
         assert name.encode() in B.lib().pa_last_error()
     for p in ("k", "v", "bt", "sl", "cu", "kc", "vc", "sc"):
@@ -139,7 +140,8 @@ def test_attention_refusals():
                          ({"scale": float("inf")}, B.PA_ERR_ARG), ({"nb": 0}, B.PA_ERR_ARG),
                          ({"info": None}, B.PA_ERR_ARG), ({"mb": 0}, B.PA_ERR_ARG),
                          ({"q": 264}, B.PA_ERR_ARG), ({"kc": 1028}, B.PA_ERR_ARG),
-                         ({"vc": 2056}, B.PA_ERR_ARG), ({"out": 514}, B.PA_ERR_ARG)):
+                         ({"vc": 2056}, B.PA_ERR_ARG), ({"out": 514}, B.PA_ERR_ARG),
+                         ({"sc": 66}, B.PA_ERR_ARG)):
             assert call(fn, **kw) == code, (fn, kw)
         for p in ("q", "kc", "vc", "sc", "bt", "sl", "cu", "plan", "out"):
             assert call(fn, **{p: None}) == B.PA_ERR_ARG, p
@@ -232,6 +234,20 @@ def test_binding_refusals():
         a.update(kw)
         bad(code, B.kv8_attention, B.KIND_PREFILL, a["q"], k, v, sc, *meta, bt, info, None,
             a["out"], a["lse"])
+    # a plan shorter than its info says, one of another type
+    info.plan_words = 100
+    for plan in (torch.zeros(99, dtype=torch.int32), torch.zeros(200, dtype=torch.int64)):
+        bad("arg", B.kv8_attention, B.KIND_PREFILL, q, k, v, sc, *meta, plan, info, None, q)
+    # everything in order but for the device: a host tensor is refused
+    info.plan_words = 1
+    for call in (lambda: B.kv8_append(rows, rows, *meta, k, v, sc),
+                 lambda: B.kv8_attention(B.KIND_PREFILL, q, k, v, sc, *meta, bt, info, None, q),
+                 lambda: B.kv8_attention_decode_noalloc(q, k, v, sc, *meta, bt, info, q),
+                 lambda: B.qk_norm_rope(q, rows, torch.zeros(3, dtype=torch.int32),
+                                        torch.zeros((8, d)), q, rows)):
+        with pytest.raises(B.PaError) as e:
+            call()
+        assert e.value.code == "arg" and "GPU" in str(e.value)
     pos, tab = torch.zeros(3, dtype=torch.int32), torch.zeros((8, d))
     bad("arg", B.qk_norm_rope, q, rows[:2], pos, tab, q, rows)
     bad("arg", B.qk_norm_rope, q, rows, pos.long(), tab, q, rows)
@@ -327,6 +343,8 @@ def test_plans_cover_every_row_once(seed):
     D = int(r.choice([64, 128]))
     plan, info = B.plan(kind, n_q, L, cu, hkv * G, hkv, D, 16, B.PA_BF16_KV8, block_table=bt)
     tiles, rows = check_plan8(plan, info, L, q, G, hkv, D)
+    cfg = synth.AttnConfig("", "bf16", hkv * G, hkv, D, 16, 0)
+    assert info.plan_words <= plan_words_bound(cfg, n, int(cu[-1]), mb)
     assert all(q[t[0]] * G <= 64 for t in rows if t[0] >= 0)
     if kind != B.KIND_DECODE:
         assert all(q[t[0]] * G > 64 for t in tiles)
