@@ -931,7 +931,7 @@ struct JoinStat {
   float mc, l;  // reference (scaled; minus infinity without a key) and sum of a row
 };
 
-template <int D, int NC>
+template <int D, int NC, bool AHEAD>
 __device__ __forceinline__ void row_item8(const int32_t* it, int g, int poff, const AttnArgs& a,
                                           JoinSmem<D, NC>& sm, JoinStat (&stat)[4][2][16]) {
   constexpr int KC = D / 64;  // 64-dim groups of a key
@@ -978,8 +978,15 @@ __device__ __forceinline__ void row_item8(const int32_t* it, int g, int poff, co
 #pragma unroll
   for (int c = 0; c < NC; ++c) m[c] = kNegInf, mc[c] = 0.f, l[c] = 0.f;
 
-  // One register set for K and one for V^T, reloaded as in row_item.  Blocks at
-  // or past kv1 read the item's last block again.
+  // AHEAD: two register sets of K and V^T; a step loads the next one's before it uses its
+  // own, so a whole step hides the memory's latency (24 sequences of 8192-20480 keys 121
+  // us, 5.9 TB/s, against 145 with one set and three wavefronts per SIMD instead of two).
+  // Beside tiles or two-tile items, which leave two wavefronts anyway, one set, reloaded
+  // as in row_item, is as good or better: 128 decode requests on 4096 shared keys 48.6 us,
+  // 51.1 with two, 32 verifications on 16384 158 and 170 (an item ahead of the other that
+  // reads its keys finds them in no cache).  Blocks at or past kv1 read the item's last
+  // block again.
+  constexpr int NB = AHEAD ? 2 : 1;
   const uint8_t* kc = reinterpret_cast<const uint8_t*>(a.kc);
   const uint8_t* vc = reinterpret_cast<const uint8_t*>(a.vc);
   const int last = kv1 > kv0 ? (kv1 - 1) / kBlock : kv0 / kBlock;
@@ -989,48 +996,54 @@ __device__ __forceinline__ void row_item8(const int32_t* it, int g, int poff, co
     const int id = __shfl(win.ids, (min(jb, last) - win.base) & 63, 64);
     return (int64_t)clamp_block(id, a.num_blocks) * a.hkv + g;
   };
-  u32x4 kreg[4][KC], vreg[DT];
-  uint32_t ek = 0, ev = 0;
-  auto load_k = [&](int t0) {
+  u32x4 kreg[NB][4][KC], vreg[NB][DT];
+  uint32_t ek[NB] = {}, ev[NB] = {};
+  auto load_k = [&](int t0, int s) {
     const int64_t b = block_of(t0 / kBlock + (j >> 2));
     const uint8_t* p = kc + b * (kBlock * D) + (j & 3) * 64 + 16 * g4;
 #pragma unroll
     for (int tt = 0; tt < 4; ++tt)
 #pragma unroll
       for (int c = 0; c < KC; ++c)
-        kreg[tt][c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + 1024 * c + 256 * tt));
-    ek = a.scales[2 * b];
+        kreg[s][tt][c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + 1024 * c + 256 * tt));
+    ek[s] = a.scales[2 * b];
   };
-  auto load_v = [&](int t0) {
+  auto load_v = [&](int t0, int s) {
     const int64_t b = block_of(t0 / kBlock + g4);
     const uint8_t* p = vc + b * (kBlock * D) + j * kBlock;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
-      vreg[dt] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + 256 * dt));
-    ev = a.scales[2 * b + 1];
+      vreg[s][dt] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + 256 * dt));
+    ev[s] = a.scales[2 * b + 1];
   };
 
   if (kv0 < kv1) {
-    load_k(kv0);
-    load_v(kv0);
+    load_k(kv0, 0);
+    load_v(kv0, 0);
   }
-  for (int t0 = kv0; t0 < kv1; t0 += kStep) {
+  // the step at t0, its K and V^T in register set b
+  auto step = [&](int t0, auto b) {
+    constexpr int cur = decltype(b)::value, next = AHEAD ? 1 - cur : 0;
     const bool more = t0 + kStep < kv1;
+    if (AHEAD && more) {
+      load_k(t0 + kStep, next);
+      load_v(t0 + kStep, next);
+    }
     f32x4 s[NC][4];
-    const float sk = scale8(ek);
+    const float sk = scale8(ek[cur]);
 #pragma unroll
     for (int tt = 0; tt < 4; ++tt) {
 #pragma unroll
       for (int c = 0; c < NC; ++c) s[c][tt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int ks = 0; ks < 2 * KC; ++ks) {
-        const u32x4 x = kreg[tt][ks / 2];
+        const u32x4 x = kreg[cur][tt][ks / 2];
         const bf16x8 k = as_bf16x8(bf16_of_e4m3(x[2 * (ks % 2)], x[2 * (ks % 2) + 1], sk));
 #pragma unroll
         for (int c = 0; c < NC; ++c) s[c][tt] = mfma16(k, qf[c][ks], s[c][tt]);
       }
     }
-    if (more) load_k(t0 + kStep);
+    if (!AHEAD && more) load_k(t0 + kStep, next);
     // Lane (j, g4), element e of score tile tt holds key t0 + 16 g4 + 4 tt + e.
     const bool masked = t0 + kStep - 1 > amin || !more;  // wave-uniform
     if (masked) {
@@ -1050,7 +1063,7 @@ __device__ __forceinline__ void row_item8(const int32_t* it, int g, int poff, co
         const int b = min(max(keep - 4 * k, 0), 4);
         const uint32_t mask = b == 4 ? ~0u : (1u << (8 * b)) - 1u;
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) vreg[dt][k] &= mask;
+        for (int dt = 0; dt < DT; ++dt) vreg[cur][dt][k] &= mask;
       }
     }
     bf16x8 pb[NC][2];
@@ -1081,16 +1094,26 @@ __device__ __forceinline__ void row_item8(const int32_t* it, int g, int poff, co
           pb[c][tt >> 1][4 * (tt & 1) + e] = (__bf16)p;
         }
     }
-    const float sv = scale8(ev);
+    const float sv = scale8(ev[cur]);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const bf16x8 v = as_bf16x8(bf16_of_e4m3(vreg[dt][2 * u], vreg[dt][2 * u + 1], sv));
+        const bf16x8 v = as_bf16x8(bf16_of_e4m3(vreg[cur][dt][2 * u], vreg[cur][dt][2 * u + 1], sv));
 #pragma unroll
         for (int c = 0; c < NC; ++c) acc[c][dt] = mfma16(v, pb[c][u], acc[c][dt]);
       }
-    if (more) load_v(t0 + kStep);
+    if (!AHEAD && more) load_v(t0 + kStep, next);
+  };
+  using B0 = std::integral_constant<int, 0>;
+  if constexpr (AHEAD) {
+    using B1 = std::integral_constant<int, 1>;
+    for (int t0 = kv0; t0 < kv1; t0 += 2 * kStep) {
+      step(t0, B0{});
+      if (t0 + kStep < kv1) step(t0 + kStep, B1{});
+    }
+  } else {
+    for (int t0 = kv0; t0 < kv1; t0 += kStep) step(t0, B0{});
   }
 
 #pragma unroll
@@ -1167,13 +1190,14 @@ __device__ __forceinline__ void row_item8(const int32_t* it, int g, int poff, co
 // from paying for the wildcard loop; a launch with only 16-row row items
 // runs at three waves per SIMD, and so does every launch at head_dim 64, whose
 // tiles fit 168 registers (24 requests' prefill 123 us against 138 with two).
-template <int D, int MIX>
+// Over the 8-bit cache 16-row items at head_dim 128 take two sets of loads and two waves.
+template <int D, int MIX, bool KV8>
 constexpr int waves_per_eu() {
-  return MIX == 2 || D == 64 ? 3 : kTileWavesPerEu;
+  return (MIX == 2 && !KV8) || D == 64 ? 3 : kTileWavesPerEu;
 }
 
 template <int D, int MIX, bool KV8 = false>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(waves_per_eu<D, MIX>()))) void attn_bf16_kernel(AttnArgs a) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(waves_per_eu<D, MIX, KV8>()))) void attn_bf16_kernel(AttnArgs a) {
   const int32_t* plan = a.plan;
   // this workgroup's kv-head and template (the dispatch list follows the
   // header, so its word loads together with the header words); template
@@ -1287,12 +1311,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(waves_per_e
           plan + plan[H_ROW_OFF] + (ti - n_tile + (threadIdx.x >> 6)) * kItemWords;
       if constexpr ((MIX & 4) != 0) {
         if (it[I_NROWS] > 16) {
-          if constexpr (KV8) row_item8<D, 2>(it, g, poff, a, *reinterpret_cast<JoinSmem<D, 2>*>(lds8), stat8);
+          if constexpr (KV8) row_item8<D, 2, false>(it, g, poff, a, *reinterpret_cast<JoinSmem<D, 2>*>(lds8), stat8);
           else row_item<D, 2>(it, g, poff, a);
           return;
         }
       }
-      if constexpr (KV8) row_item8<D, 1>(it, g, poff, a, *reinterpret_cast<JoinSmem<D, 1>*>(lds8), stat8);
+      if constexpr (KV8) row_item8<D, 1, MIX == 2>(it, g, poff, a, *reinterpret_cast<JoinSmem<D, 1>*>(lds8), stat8);
       else row_item<D, 1>(it, g, poff, a);
     }
   }
