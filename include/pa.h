@@ -291,7 +291,8 @@ typedef struct pa_plan_info {
  * is too small the call fails with PA_ERR_ARG and *info holds the size.
  * kind PA_KIND_DECODE requires every q_len == 1, PA_KIND_VERIFY every q_len ==
  * n_q (1..8); PA_KIND_PREFILL takes any q_len >= 0 (prefill chunks and decode
- * tokens may be mixed).  num_cus = compute units to fill (0: 256).
+ * tokens may be mixed).  dtype: PA_BF16, PA_F32, or PA_BF16_KV8 for the
+ * pa_kv8_attn_* calls.  num_cus = compute units to fill (0: 256).
  * Errors: PA_ERR_ARG, PA_ERR_UNSUPPORTED. */
 int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int32_t* seq_lens,
                  const int32_t* cu_seqlens_q, const int32_t* block_table,

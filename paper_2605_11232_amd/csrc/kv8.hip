@@ -35,8 +35,8 @@ struct Kv8Args {
 
 // One block of the launch and its rows.
 struct BlockRows {
-  int64_t bh;      // block * hkv + kv-head; -1: nothing to do
-  int off0, off1;  // token offsets [off0, off1) of the block have rows
+  int id;          // block, as the table has it
+  int off0, off1;  // token offsets [off0, off1) of the block have rows; none: nothing to do
   int row0;        // row of offset off0
 };
 
@@ -57,8 +57,8 @@ __device__ __forceinline__ int find_seq(const int32_t* cu, int n, int x, Key key
   return lo;
 }
 
-__device__ __forceinline__ BlockRows find_rows(const Kv8Args& a, int slot, int h) {
-  BlockRows b{-1, 0, 0, 0};
+__device__ __forceinline__ BlockRows find_rows(const Kv8Args& a, int slot) {
+  const BlockRows none{-1, 0, 0, 0};
   int r, c0, n, L;
   int64_t j;  // logical block
   if (a.by_token) {
@@ -69,7 +69,7 @@ __device__ __forceinline__ BlockRows find_rows(const Kv8Args& a, int slot, int h
       r = find_seq(a.cu, a.n_seqs, slot, [](int c, int) { return c; });
     c0 = a.cu[r], n = a.cu[r + 1] - c0, L = a.seq_lens[r];
     const int row = slot - c0, pos = L - n + row;
-    if (row < 0 || row >= n || pos < 0 || (row > 0 && pos % kBlock)) return b;
+    if (row < 0 || row >= n || pos < 0 || (row > 0 && pos % kBlock)) return none;
     j = pos / kBlock;
   } else {
     r = find_seq(a.cu, a.n_seqs, slot, [](int c, int i) { return c / kBlock + 2 * i; });
@@ -77,16 +77,12 @@ __device__ __forceinline__ BlockRows find_rows(const Kv8Args& a, int slot, int h
     j = (L - n) / kBlock + (int64_t)slot - (c0 / kBlock + 2 * r);
   }
   const int first = L - n;  // first row's position
-  if (n <= 0 || first < 0 || c0 < 0 || j < 0 || j * kBlock >= L || j >= a.max_blocks) return b;
-  const int p0 = int(j) * kBlock;
-  b.off0 = max(first - p0, 0);
-  b.off1 = min(L - p0, kBlock);
-  b.row0 = c0 + p0 + b.off0 - first;
-  const int id = a.bt[(int64_t)r * a.max_blocks + j];
+  if (n <= 0 || first < 0 || c0 < 0 || j < 0 || j * kBlock >= L || j >= a.max_blocks) return none;
+  const int p0 = int(j) * kBlock, off0 = max(first - p0, 0), off1 = min(L - p0, kBlock);
+  const int row0 = c0 + p0 + off0 - first;
   // rows past the caller's: cu does not end at n_tokens
-  if (id >= 0 && id < a.num_blocks && (int64_t)b.row0 + (b.off1 - b.off0) <= a.n_tokens)
-    b.bh = (int64_t)id * a.hkv + h;
-  return b;
+  if ((int64_t)row0 + (off1 - off0) > a.n_tokens) return none;
+  return {a.bt[(int64_t)r * a.max_blocks + j], off0, off1, row0};
 }
 
 // Smallest e of [kExpMin, kExpMax] with amax <= 448 * 2^e; 448 = 1.75 * 2^8.
@@ -165,12 +161,10 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(const T* __restrict__ k
   const int64_t slot = i / a.hkv;
   if (slot >= a.slots) return;
   const int h = int(i - slot * a.hkv);
-  const BlockRows b = find_rows(a, int(slot), h);
-  if (b.bh < 0) return;
+  const BlockRows b = find_rows(a, int(slot));
+  if (b.off0 == b.off1) return;
   uint8_t (*vt)[D + 8] = vt_sh[w];
   const int c = lane % LR, side = lane / LR % 2, sub = lane / (2 * LR);
-  const int e_old = min(max(int(a.scales[2 * b.bh + side]) - kExpBias, kExpMin), kExpMax);
-
   Raw8<T> x[NI];
   const T* src = (side ? v_new + (int64_t)b.row0 * a.v_stride : k_new + (int64_t)b.row0 * a.k_stride) + (int64_t)h * D + 8 * c;
   const int64_t stride = side ? a.v_stride : a.k_stride;
@@ -178,6 +172,10 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(const T* __restrict__ k
 #pragma unroll
   for (int u = 0; u < NI; ++u)
     if (has(u)) x[u].load(src + (u * TI + sub - b.off0) * stride);
+  // the rows are on their way while the block's id arrives
+  if (b.id < 0 || b.id >= a.num_blocks) return;
+  const int64_t bh = (int64_t)b.id * a.hkv + h;
+  const int e_old = min(max(int(a.scales[2 * bh + side]) - kExpBias, kExpMin), kExpMax);
   float mx = 0.f;
 #pragma unroll
   for (int u = 0; u < NI; ++u)
@@ -195,10 +193,10 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(const T* __restrict__ k
     grow = min(max(e - e_old, 0), 126);
     e = max(e, e_old);
   }
-  if (sub == 0 && c == 0) a.scales[2 * b.bh + side] = uint8_t(e + kExpBias);
+  if (sub == 0 && c == 0) a.scales[2 * bh + side] = uint8_t(e + kExpBias);
 
-  uint8_t* kb = a.kc + b.bh * (kBlock * D);
-  uint8_t* vb = a.vc + b.bh * (kBlock * D);
+  uint8_t* kb = a.kc + bh * (kBlock * D);
+  uint8_t* vb = a.vc + bh * (kBlock * D);
   const float s = pow2(-e);
 #pragma unroll
   for (int u = 0; u < NI; ++u)
@@ -290,12 +288,13 @@ __global__ __launch_bounds__(256) void kv8_read_kernel(T* __restrict__ k_out, T*
   const int64_t slot = i / a.hkv;
   if (slot >= a.slots) return;
   const int h = int(i - slot * a.hkv);
-  const BlockRows b = find_rows(a, int(slot), h);
-  if (b.bh < 0) return;
-  const uint8_t* kb = a.kc + b.bh * (kBlock * D);
-  const uint8_t* vb = a.vc + b.bh * (kBlock * D);
-  const float sk = pow2(int(a.scales[2 * b.bh]) - kExpBias);
-  const float sv = pow2(int(a.scales[2 * b.bh + 1]) - kExpBias);
+  const BlockRows b = find_rows(a, int(slot));
+  if (b.off0 == b.off1 || b.id < 0 || b.id >= a.num_blocks) return;
+  const int64_t bh = (int64_t)b.id * a.hkv + h;
+  const uint8_t* kb = a.kc + bh * (kBlock * D);
+  const uint8_t* vb = a.vc + bh * (kBlock * D);
+  const float sk = pow2(int(a.scales[2 * bh]) - kExpBias);
+  const float sv = pow2(int(a.scales[2 * bh + 1]) - kExpBias);
   auto has = [&](int o) { return o >= b.off0 && o < b.off1; };
   const int kd = 4 * (lane % LT), ko = lane / LT;      // of load 0; 64 / LT tokens a load
   const int vd = 4 * (lane / 4), vo = 4 * (lane % 4);  // of square 0; 64 dims a square

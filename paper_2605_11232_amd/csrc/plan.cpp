@@ -10,7 +10,8 @@
 // whose key range is split so the launch has enough wavefronts in flight to
 // stream the cache at HBM bandwidth; sequences with 33..64 rows run their
 // split key ranges as tile items.  Split partial results are combined by
-// log-sum-exp in a merge pass.
+// log-sum-exp in a merge pass.  Over the 8-bit cache sequences of 33..64 rows run as two
+// row items, and the four row items of a workgroup may be one sequence's, joined in LDS.
 //
 // Shared prefixes (cascade): few-row sequences whose block tables start
 // with the same blocks read the same prefix keys (Section 2, Automatic Prefix

@@ -510,6 +510,43 @@ def test_decode_of_many_heads_without_workspace():
                          <= 2.0 ** -8 * ref.abs() + (2.0 ** -8 + 2 * ds + 2.0 ** -16) * A)
 
 
+@pytest.mark.parametrize("q_lens", [[1, 1, 1], [5, 5, 5], [40, 3, 100]])
+def test_blocks_past_4_gib(q_lens):
+    """The same launch on a small cache and on the last blocks of one whose keys and
+    whose values pass 2^32 bytes: equal bit for bit."""
+    hq, hkv, d = 16, 8, 128
+    lens = [300, 77, 1100]
+    far_nb = (1 << 32) // (hkv * 16 * d) + 2000
+    table, nb = tables(lens, 11)
+    r = np.random.default_rng(11)
+    k, v = (dev(rows_of(r, sum(lens), hkv, d, "bf16"), torch.bfloat16) for _ in range(2))
+    q = torch.randn((sum(q_lens), hq, d), device="cuda", generator=torch.Generator(
+        "cuda").manual_seed(1)).to(torch.bfloat16)
+    kind = {1: B.KIND_DECODE, 5: B.KIND_VERIFY}.get(q_lens[1], B.KIND_PREFILL)
+    results = []
+    for blocks, t in ((nb, table), (far_nb, np.where(table >= 0, table + far_nb - nb, -1))):
+        ks, vs, ss = B.kv8_cache_shapes(blocks, hkv, d)
+        cache = [torch.empty(ks, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn),
+                 torch.empty(vs, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn),
+                 torch.empty(ss, dtype=torch.uint8, device="cuda")]
+        m = [dev(x) for x in meta(t, lens, lens)]
+        B.kv8_append(k, v, *m, *cache)
+        ko, vo = torch.empty_like(k), torch.empty_like(v)
+        B.kv8_read(ko, vo, *m, *cache)
+        mq = meta(t, lens, q_lens)
+        plan, info = B.plan(kind, q_lens[0], mq[1], mq[2], hq, hkv, d, 16, B.PA_BF16_KV8,
+                            block_table=mq[0])
+        ws = torch.empty(max(16, int(info.workspace_bytes)), dtype=torch.uint8, device="cuda")
+        out, lse = torch.empty_like(q), torch.empty((sum(q_lens), hq), device="cuda")
+        B.kv8_attention(kind, q, *cache, *[dev(x) for x in mq], dev(plan), info, ws, out, lse)
+        torch.cuda.synchronize()
+        results.append((ko, vo, out, lse))
+        del cache
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+    assert torch.isfinite(results[0][2].float()).all()
+
+
 # ---- norms and rotation -----------------------------------------------------------------------
 
 ROPE = [
