@@ -699,7 +699,8 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
           } else {
             for (int32_t row0 = 0; row0 < rows; row0 += pa::kRowItemRows) {
               const Rec item = {r, 0, row0, std::min(pa::kRowItemRows, rows - row0), int32_t(k0),
-                                int32_t(k1), part < 0 ? -1 : part + row0, waves > 1 ? pa::kItemJoin : 0};
+                                int32_t(k1), part < 0 ? -1 : part + row0,
+                                (waves > 1 ? pa::kItemJoin : 0) | (row_pieces(r) > 1 ? pa::kItemTwice : 0)};
               if (waves == 1) {
                 t_rows.push_back(item);
                 row_cost.push_back(k1 - k0);

@@ -92,7 +92,10 @@ enum : int32_t {
 // adjacent key ranges, any of them empty; they combine their results in LDS and write
 // one: the same part in all four.
 constexpr int32_t kItemStream = 1;
+// kItemTwice (8-bit cache): a second row item, with the sequence's other rows, reads the
+// same keys.
 constexpr int32_t kItemJoin = 2;
+constexpr int32_t kItemTwice = 4;
 
 // Shared-prefix item: gathered rows [row0, row0 + nrows) of a cascade group's
 // members (member m owns gathered rows m * rpm .. m * rpm + rpm - 1, its own

@@ -282,6 +282,8 @@ def check_plan8(plan, info, L, q, G, hkv, D):
         else:
             items += [t for t in quad if t[0] >= 0]
             assert not any(t[7] & 2 for t in quad)
+        # items of sequences with more rows than one holds say so
+        assert all(bool(t[7] & 4) == (q[t[0]] * G > 32) for t in quad if t[0] >= 0)
     cover, writes = {}, []
     for seq, kvh, row0, nrows, kv0, kv1, part, _ in items:
         assert kv0 % 16 == 0 and 0 <= kv0 < kv1 <= L[seq]
