@@ -349,18 +349,19 @@ __device__ __forceinline__ void tile_item(const int32_t* it, int g, int poff, co
     }
   };
   // The wave-uniform address in scalar registers, the lane's offset in a vector one.
-  auto raw16 = [](const char* base, uint32_t off) {
-    const __amdgpu_buffer_rsrc_t r =
-        __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), (short)0, 16 * D, 0x00020000);
+  // Steps past the last are loads of nothing: no branch splits the code around them.
+  auto raw16 = [](const char* base, uint32_t off, bool load) {
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<char*>(base), (short)0, load ? 16 * D : 0, 0x00020000);
     return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, STREAM ? kCachePolicyNonTemporal : 0));
   };
-  auto load_k8 = [&](int s) {
+  auto load_k8 = [&](int s, bool load) {
 #pragma unroll
-    for (int i = 0; i < NR; ++i) rk[i] = raw16(kbase + blk8[s][i], koff8);
+    for (int i = 0; i < NR; ++i) rk[i] = raw16(kbase + blk8[s][i], koff8, load);
   };
-  auto load_v8 = [&](int s) {
+  auto load_v8 = [&](int s, bool load) {
 #pragma unroll
-    for (int i = 0; i < NR; ++i) rv[i] = raw16(vbase + blk8[s][i], piece_off + 16 * lane);
+    for (int i = 0; i < NR; ++i) rv[i] = raw16(vbase + blk8[s][i], piece_off + 16 * lane, load);
   };
   auto store_k8 = [&](int s) {
 #pragma unroll
@@ -372,10 +373,11 @@ __device__ __forceinline__ void tile_item(const int32_t* it, int g, int poff, co
       st16(p + 8 * (kdst8 ^ 1), bf16_of_e4m3(rk[i][2], rk[i][3], sc));
     }
   };
+  uint32_t scv[NR];  // scales of the V^T to store
   auto store_v8 = [&](int s) {
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
-      const float sc = scale8(sc8[s][i] >> 8 & 255);
+      const float sc = scale8(scv[i] >> 8 & 255);
       const int sw = vswz(lane);  // vswz(64 + d) == vswz(d)
       __bf16* p = &sm.v[s][8 * (128 * (4 * i + w) + 2 * lane)];
       st16(p + 8 * sw, bf16_of_e4m3(rv[i][0], rv[i][1], sc));
@@ -527,19 +529,19 @@ __device__ __forceinline__ void tile_item(const int32_t* it, int g, int poff, co
     int64_t blk[2][NB] = {};
     if constexpr (KV8) {
       step_blocks8(kv0, 0);
-      load_k8(0);
-      load_v8(0);
+      load_k8(0, true);
+      load_v8(0, true);
+#pragma unroll
+      for (int i = 0; i < NR; ++i) scv[i] = sc8[0][i];
       store_k8(0);
       store_v8(0);
       if (ntiles > 1) {
         step_blocks8(kv0 + KT, 1);
-        load_k8(1);
-        load_v8(1);  // stored in step 0
+        load_k8(1, true);
+        load_v8(1, true);  // stored in step 0
         store_k8(1);
-        if (ntiles > 2) {
-          step_blocks8(kv0 + 2 * KT, 0);
-          load_k8(0);
-        }
+        step_blocks8(kv0 + KT * min(2, ntiles - 1), 0);
+        load_k8(0, ntiles > 2);
       }
     } else {
       step_blocks(kv0, blk[0]);
@@ -565,18 +567,20 @@ __device__ __forceinline__ void tile_item(const int32_t* it, int g, int poff, co
     }
     __syncthreads();  // K buffer 0 is refilled next
 
-    // KV8: K of step t + 2 and V^T of step t + 1 into LDS, the next on their way
+    // KV8: blocks8 finds step t + 3's blocks, stage8 puts K of step t + 2 and V^T of step
+    // t + 1 into LDS (past the last step: unused buffers) and the next on their way
+    auto blocks8 = [&](int t, auto buf_c) {
+      constexpr int buf = decltype(buf_c)::value;
+#pragma unroll
+      for (int i = 0; i < NR; ++i) scv[i] = sc8[1 - buf][i];  // of step t + 1
+      step_blocks8(kv0 + KT * min(t + 3, ntiles - 1), 1 - buf);
+    };
     auto stage8 = [&](int t, auto buf_c) {
       constexpr int buf = decltype(buf_c)::value;
       store_v8(1 - buf);
-      if (t + 2 < ntiles) {
-        store_k8(buf);
-        load_v8(buf);  // of step t + 2, whose blocks were found one step earlier
-        if (t + 3 < ntiles) {
-          step_blocks8(kv0 + KT * (t + 3), 1 - buf);
-          load_k8(1 - buf);
-        }
-      }
+      store_k8(buf);
+      load_v8(buf, t + 2 < ntiles);  // whose blocks were found one step earlier
+      load_k8(1 - buf, t + 3 < ntiles);
     };
     // One pipelined step: softmax + PV of step t, scores of step t + 1.
     // buf_c = t % 2, the LDS buffer pair of step t (a compile-time constant).
@@ -590,6 +594,7 @@ __device__ __forceinline__ void tile_item(const int32_t* it, int g, int poff, co
         }
         issue_v(blk[1 - buf], 1 - buf);  // blocks of step t + 1, found one step earlier
       }
+      if constexpr (KV8) blocks8(t, buf_c);
       bf16x8 p[NSUB][2];
       f32x16 sn[NSUB];
       probs(s, p);
@@ -614,6 +619,7 @@ __device__ __forceinline__ void tile_item(const int32_t* it, int g, int poff, co
     };
     auto idle_step = [&](int t, auto buf_c) {
       if constexpr (KV8) {
+        blocks8(t, buf_c);
         stage8(t, buf_c);
       } else {
         constexpr int buf = decltype(buf_c)::value;

@@ -58,10 +58,11 @@ constexpr int64_t kRowWavesPerCu = 10;      // row-item split target
 // decode requests of 32/8 heads on 2048 shared keys 31.4, 27.1, 27.0, 84 at head_dim 64
 // 21.7, 18.4, 20.5.
 constexpr int64_t kRowWavesPerCu8 = 5, kWideRowWavesPerCu8 = 4;
-// Fewest keys of a shared prefix's chunk there, unless the launch leaves every other CU
-// without a workgroup: 64 decode requests 26.9 us, 29.1 with 256 (768: 33.3), 4
-// verifications on 4096 shared keys 22.0 and 24.7 (27.2); 4 decode requests (104
-// workgroups) 12.0 with 256, 15.2 with 384.
+// Up to so many keys a shared prefix's chunk there takes twice what the longest row item
+// does, unless the launch leaves every other CU without a workgroup: 64 decode requests
+// 26.9 us with chunks of 512, 29.1 with 256 (768: 33.3), 4 verifications on 4096 shared
+// keys 22.0 and 24.7 (27.2); 4 decode requests (104 workgroups) 12.0 with 256, 15.2 with
+// 384; 44 requests of 3-6 keys on 1303 shared ones, 64/8 heads, 19.1 with 256, 23.3 with 512.
 constexpr int64_t kSharedMinKeys8 = 512;
 constexpr int64_t kPrivateTileKeys = 4160;  // most private keys a few-row tile item covers
 constexpr int64_t kMinTileKeys = 256;       // fewest, in launches that leave compute units idle
@@ -585,7 +586,8 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
                      (cg_keys[c] / std::max<int64_t>(longest, pa::kSharedMinKeys));
       }
       const bool few_wgs = 2 * (row_wgs + chunk_wgs) <= num_cus;
-      longest = std::max<int64_t>(longest, kv8 && !few_wgs ? kSharedMinKeys8 : pa::kSharedMinKeys);
+      if (kv8 && !few_wgs) longest = std::max(longest, std::min(2 * longest, kSharedMinKeys8));
+      longest = std::max<int64_t>(longest, pa::kSharedMinKeys);
       const int64_t share = 1 + int64_t(std::min(rest, 1e6) * 0.4 * pa::kTileStep);
       // beside verifications' row items, whose workgroups need the room, three on four CUs
       // (24 of 5 tokens on 4096 shared keys 64.6 us; one per CU 70; one on two 60.4, where
