@@ -510,8 +510,8 @@ int pa_attn_decode_noalloc(const void* q, const void* k_cache, const void* v_cac
  * allocates nothing.  The result depends on the order of appends to a block (as
  * said above), not on the launch.  Errors: PA_ERR_ARG (NULL pointer with rows to
  * store, negative size, a row stride below num_kv_heads * head_dim, rows or
- * caches not 16-byte, scales not 4-byte aligned), PA_ERR_UNSUPPORTED (head_dim, block_size, dtype),
- * PA_ERR_LAUNCH. */
+ * caches not 16-byte, scales not 4-byte aligned), PA_ERR_UNSUPPORTED (head_dim,
+ * block_size, dtype), PA_ERR_LAUNCH. */
 int pa_kv8_append(const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
                   const int32_t* block_table, int32_t max_blocks_per_seq, const int32_t* seq_lens,
                   const int32_t* cu_seqlens, int32_t n_seqs, int32_t n_tokens, void* k_cache,
@@ -537,11 +537,10 @@ int pa_kv8_read(void* k_out, int64_t k_stride, void* v_out, int64_t v_stride,
  * PA_BF16_KV8 (pa_attn_plan, pa_prepare_launch; the workspace bounds hold for
  * them too).  Arguments, layouts, ownership and errors as for those calls; q,
  * out and the caches must be 16-byte aligned, the scales 4-byte (PA_ERR_ARG).
- * Slots behind a
- * sequence's last token may hold any bytes.  A key that is NaN makes the rows that
- * see it NaN, a value that is NaN those rows' element of its dim; in a launch of
- * several tokens per sequence it may make that element of the sequence's other
- * rows NaN, too, as with the bf16 cache. */
+ * Slots behind a sequence's last token may hold any bytes.  A key that is NaN
+ * makes the rows that see it NaN, a value that is NaN those rows' element of its
+ * dim; in a launch of several tokens per sequence it may make that element of the
+ * sequence's other rows NaN, too, as with the bf16 cache. */
 int pa_kv8_attn_prefill(const void* q, const void* k_cache, const void* v_cache,
                         const uint8_t* scales, int32_t num_blocks, const int32_t* block_table,
                         int32_t max_blocks_per_seq, const int32_t* seq_lens,
