@@ -61,9 +61,21 @@ constexpr int64_t kRowWavesPerCu8 = 5, kWideRowWavesPerCu8 = 4;
 // Up to so many keys a shared prefix's chunk there takes twice what the longest row item
 // does, unless the launch leaves every other CU without a workgroup: 64 decode requests
 // 26.9 us with chunks of 512, 29.1 with 256 (768: 33.3), 4 verifications on 4096 shared
-// keys 22.0 and 24.7 (27.2); 4 decode requests (104 workgroups) 12.0 with 256, 15.2 with
-// 384; 44 requests of 3-6 keys on 1303 shared ones, 64/8 heads, 19.1 with 256, 23.3 with 512.
+// keys 22.0 and 24.7 (27.2); 44 requests of 3-6 keys on 1303 shared ones, 64/8 heads, 19.1
+// with 256, 23.3 with 512.
 constexpr int64_t kSharedMinKeys8 = 512;
+// A launch whose sequences all run on row items and come to at most so many keys (of all
+// sequences and kv-heads) per CU does not split shared prefixes off: its row items all
+// start at once and read them from the caches, and the prefix's tiles, which copy every
+// key through LDS, and their parts are what it would wait for.  us with and without tiles:
+// 4 decode requests on 2048 shared and 200-400 own keys, 64/8 heads, 12.2 and 11.0, 16 on
+// 320 15.5 and 8.6 (32/8 heads of 64 dims 11.0 and 6.5), 8 on 1024 and 1500-2500 (760 keys
+// per CU) 17.1 and 14.5; 2 verifications of 6 tokens on 320, 28/4 heads, 14.1 and 10.1,
+// 64/8 heads 16 on 1024 and 200-400 (660) 25.7 and 15.1, 8 on 1024 and 1500-2500 (760)
+// 23.4 and 24.9; at 32/8 heads of 64 dims and 200-400 own keys the verifications lose up to
+// 1.5 us from 512 shared keys on (4 on 1024: 11.1 and 12.3).  Past it: 8 decode requests on
+// 2048 and 1500-2500 (1010) 17.0 and 17.1, 16 (2020) 21.8 and 27.6.
+constexpr int64_t kUnsharedKeysPerCu8 = 768;
 constexpr int64_t kPrivateTileKeys = 4160;  // most private keys a few-row tile item covers
 constexpr int64_t kMinTileKeys = 256;       // fewest, in launches that leave compute units idle
 constexpr int64_t kMinRowKeys = 256;        // split target floor of row items
@@ -416,7 +428,17 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
     std::vector<int32_t> cg_seqs;             // members of all groups, group by group
     std::vector<int32_t> cg_begin{0};         // group c's members start at cg_seqs[cg_begin[c]]
     std::vector<int32_t> cg_keys, cg_chunks;  // shared keys, key chunks (one merge part each)
-    if (block_table) {
+    bool share = block_table != nullptr;
+    if (share && kv8) {
+      int64_t keys = 0;
+      bool rows_only = true;
+      for (int32_t r = 0; r < n_seqs; ++r) {
+        rows_only = rows_only && (qlen(r) == 0 || is_row(r));
+        keys += int64_t(seq_lens[r]) * num_kv_heads * (qlen(r) > 0);
+      }
+      share = !rows_only || keys > kUnsharedKeysPerCu8 * num_cus;
+    }
+    if (share) {
       std::vector<std::pair<int64_t, int32_t>> cand;
       cand.reserve(n_seqs);
       for (int32_t r = 0; r < n_seqs; ++r)

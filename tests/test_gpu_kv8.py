@@ -292,10 +292,21 @@ ATTN = {
 
 @pytest.mark.parametrize("name", list(ATTN))
 def test_attention(name):
+    attention_case(name)
+
+
+@pytest.mark.parametrize("name", ["shared", "shared-64", "verify-shared"])
+def test_attention_on_a_split_off_prefix(name):
+    """The same launches planned for a chip so small that the shared keys are worth
+    tiles of their own."""
+    assert attention_case(name, num_cus=8).n_shared_items > 0
+
+
+def attention_case(name, num_cus=0):
     hq, hkv, d, q_lens, lens, prefix = ATTN[name]
     say("[kv8] attention", name)
     cfg = synth.AttnConfig(f"kv8-{name}", "bf16", hq, hkv, d, 16, 7000 + len(name))
-    wl, dv, orc = replay(cfg, q_lens, lens, 50, prefix)
+    wl, dv, orc = replay(cfg, q_lens, lens, 50, prefix, num_cus=num_cus)
     ro = orc.launch(wl.launches[0])
     p = dv.run(wl.launches[0])
     torch.cuda.synchronize()
@@ -312,6 +323,7 @@ def test_attention(name):
                                        p.seq_lens, p.cu, p.plan, p.info, out, lse)
         torch.cuda.synchronize()
         assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
+    return p.info
 
 
 def test_attention_with_tail_lists():
@@ -389,6 +401,7 @@ NAN = {
     "decode-joined": (8, 2, 128, [1], [700], 0),
     "decode-short": (8, 2, 64, [1] * 5, [30, 1, 64, 65, 17], 0),
     "decode-shared": (8, 2, 128, [1] * 3, [2100, 2049, 2563], 2048),
+    "decode-shared-tiles": (8, 2, 128, [1] * 3, [2100, 2049, 2563], 2048),
 }
 
 
@@ -400,9 +413,12 @@ def test_rows_without_a_number_stay_visible(name, where):
     dim; no other row changes."""
     hq, hkv, d, q_lens, lens, prefix = NAN[name]
     cfg = synth.AttnConfig(f"kv8-nan-{name}", "bf16", hq, hkv, d, 16, 7300 + len(name))
-    wl, dv, orc = replay(cfg, q_lens, lens, 53, prefix)
+    # a chip of 8 CUs: the shared keys are worth tiles of their own
+    wl, dv, orc = replay(cfg, q_lens, lens, 53, prefix,
+                         num_cus=8 if name == "decode-shared-tiles" else 0)
     ro = orc.launch(wl.launches[0])
     p = dv.prepare(wl.launches[0])
+    assert name != "decode-shared-tiles" or p.info.n_shared_items > 0
     dv.append(p)
     dv.attend(p)
     torch.cuda.synchronize()

@@ -352,3 +352,25 @@ def test_plans_cover_every_row_once(seed):
         assert all(q[t[0]] * G > 64 for t in tiles)
     else:  # tiles only where the array of the call without workspace asks for them
         assert info.workspace_bytes <= B.NOALLOC_WORKSPACE_BYTES
+
+
+@pytest.mark.parametrize("q", [1, 5])
+@pytest.mark.parametrize("num_cus, shared", [(256, False), (23, False), (22, True)])
+def test_small_launches_leave_shared_prefixes_to_their_row_items(q, num_cus, shared):
+    """Up to 768 keys per CU: 4 sequences of 8580 keys together are 17160 for 2 kv-heads."""
+    L = np.array([2100, 2130, 2160, 2190])
+    bt = np.full((4, 137), -1, np.int32)
+    for s in range(4):
+        bt[s, :128] = np.arange(128)
+        bt[s, 128:] = 128 + 9 * s + np.arange(9)
+    kind = B.KIND_DECODE if q == 1 else B.KIND_VERIFY
+    plan, info = B.plan(kind, q, L, np.arange(5) * q, 16, 2, 128, 16, B.PA_BF16_KV8,
+                        num_cus=num_cus, block_table=bt)
+    assert (info.n_shared_items > 0) == shared
+    check_plan8(plan, info, L, np.full(4, q), 8, 2, 128)
+    # beside a prefill chunk they are split off
+    n = np.array([q, q, q, 300])
+    plan, info = B.plan(B.KIND_PREFILL, 0, L, np.concatenate([[0], np.cumsum(n)]), 16, 2, 128, 16,
+                        B.PA_BF16_KV8, num_cus=num_cus, block_table=bt)
+    assert info.n_shared_items > 0
+    check_plan8(plan, info, L, n, 8, 2, 128)
