@@ -3,7 +3,8 @@
 // y = x / sqrt(mean(x^2) + eps) * w over a head's D dims, then the first rot dims
 // turned in pairs (a, b) by the position's angles: (a cos - b sin, b cos + a sin),
 // which for a dim with partner `o` is x * cos + o * sin with the sine's sign
-// folded in; dims behind rot have cosine 1 and sine 0.
+// folded in; dims behind rot stay: they are selected, as a product with a sine of zero
+// would turn an infinity, or a finite dim beside one, into NaN.
 //
 // One pass over the rows, bound by memory.  D / 8 lanes hold a row, 16 bytes of
 // bf16 (32 of float32) each: dims 8 c .. 8 c + 7 of lane c.  A wavefront keeps one
@@ -79,7 +80,8 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(const T* q, const T* 
                   : k + t * a.k_stride + (int64_t)(h - a.hq) * D + 8 * c, x[u]);
   }
   if (pos < 0 || pos >= a.n_positions) return;
-  float cs[8], sn[8];
+  float cs[8], sn[8];  // of the dims that are turned
+  auto turned = [&](int e) { return WHERE == kHalfLanes ? 8 * c < a.rot : 8 * c + e < a.rot; };
   const float* tab = a.cos_sin + (int64_t)pos * a.rot;
   const int half = a.rot / 2;
   if (WHERE == kHalfLanes || (WHERE == kPairs && a.rot % 8 == 0)) {
@@ -107,9 +109,8 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(const T* q, const T* 
       const int d = 8 * c + e;
       const bool first = WHERE == kPairs ? d % 2 == 0 : d < half;
       const int p = WHERE == kPairs ? d / 2 : first ? d : d - half;
-      const bool turned = d < a.rot;
-      cs[e] = turned ? tab[p] : 1.f;
-      sn[e] = turned ? tab[half + p] : 0.f;
+      cs[e] = turned(e) ? tab[p] : 1.f;
+      sn[e] = turned(e) ? tab[half + p] : 0.f;
       sn[e] = first ? -sn[e] : sn[e];
     }
   }
@@ -157,7 +158,7 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(const T* q, const T* 
     }
     float y[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = x[u][e] * cs[e] + o[e] * sn[e];
+    for (int e = 0; e < 8; ++e) y[e] = turned(e) ? x[u][e] * cs[e] + o[e] * sn[e] : x[u][e];
     if (h < heads)
       put8(key ? k_out + (t * a.hkv + h - a.hq) * D + 8 * c : q_out + (t * a.hq + h) * D + 8 * c, y);
   }

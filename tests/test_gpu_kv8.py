@@ -646,6 +646,43 @@ def test_norm_rope(case):
         assert torch.equal(qd[~keep], dev(q, t)[~keep])
 
 
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("d, rot, inter, dtype", [
+    (128, 64, True, "bf16"), (128, 64, False, "bf16"), (64, 6, True, "f32"), (64, 6, False, "f32"),
+    (64, 48, False, "f32"), (128, 126, True, "bf16"), (128, 0, False, "bf16"), (64, 0, True, "f32")])
+def test_dims_that_are_not_turned_stay(d, rot, inter, dtype, norm):
+    """Infinities, NaN and zeros of either sign behind rot_dim change no dim beside
+    them; without norms those dims come out bit for bit."""
+    T, hq, hkv, n_pos = 14, 5, 2, 50
+    r = np.random.default_rng(d + rot)
+    table, pos = rope_table(n_pos, rot), r.integers(1, n_pos, T).astype(np.int32)
+    x = synth.round_to_dtype(r.standard_normal((T, hq + hkv, d)).astype(np.float32), dtype)
+    special = [np.inf, -np.inf, np.nan, -0.0, 0.0]
+    for t in range(T - 2):  # one or two of them in a head, beside ordinary values
+        for h in range(hq + hkv):
+            for _ in range(1 + (t + h) % 2):
+                x[t, h, r.integers(rot, d)] = special[r.integers(5)]
+    x[T - 2, :, rot:] = np.inf
+    dt = DTYPE[dtype]
+    q, k = dev(x[:, :hq], dt), dev(x[:, hq:], dt)
+    qo, ko = torch.empty_like(q), torch.empty_like(k)
+    B.qk_norm_rope(q, k, dev(pos), dev(table), qo, ko, norm=norm, interleaved=inter)
+    torch.cuda.synchronize()
+    with np.errstate(invalid="ignore"):
+        y = kv8.norm_rope(x, pos, table, norm=norm, interleaved=inter)
+        b = rope_bound(x.astype(np.float64), y, table, None, norm, inter, dtype)
+    got = np.concatenate([qo.double().cpu().numpy(), ko.double().cpu().numpy()], 1)
+    fin = np.isfinite(y)
+    assert np.array_equal(got[~fin], y[~fin], equal_nan=True)
+    assert np.all(np.abs(got - y)[fin] <= b[fin])
+    if not norm:
+        bits = torch.int16 if dtype == "bf16" else torch.int32
+        for a, o in ((q, qo), (k, ko)):
+            a, o = a[..., rot:].contiguous(), o[..., rot:].contiguous()
+            same = (a.view(bits) == o.view(bits)) | (a.isnan() & o.isnan())
+            assert same.all()
+
+
 # ---- together ---------------------------------------------------------------------------------
 
 class Chain:
