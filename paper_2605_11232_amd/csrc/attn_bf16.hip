@@ -1137,6 +1137,9 @@ __device__ __forceinline__ void row_item8(const int32_t* it, int g, int poff, co
   }
   if (it[I_FLAGS] & kItemJoin) {
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int first[4];  // the wavefronts' first keys
+#pragma unroll
+    for (int v = 0; v < 4; ++v) first[v] = (it + (v - w) * kItemWords)[I_KV0];
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       if (g4 == 0) stat[w][c][j] = {m[c] == kNegInf ? kNegInf : mc[c], l[c]};
@@ -1147,6 +1150,7 @@ __device__ __forceinline__ void row_item8(const int32_t* it, int g, int poff, co
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       JoinStat st[4];
+      bool seen[4];
       float top = kNegInf;
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
@@ -1156,10 +1160,12 @@ __device__ __forceinline__ void row_item8(const int32_t* it, int g, int poff, co
       float sum = 0.f, f[4];
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
-        // a wavefront without a visible key counts for nothing, one without a number
-        // (its sum is NaN) stays
-        f[v] = st[v].mc == kNegInf ? (st[v].l == 0.f ? 0.f : 1.f) : fast_exp2(st[v].mc - top);
-        sum += f[v] == 0.f ? 0.f : f[v] * st[v].l;
+        // A wavefront whose keys the row does not see counts for nothing.  The others' sums
+        // and outputs are multiplied by their weights where those are zero, too: one that is
+        // not a number makes the row none, however low the wavefront's other scores lie.
+        seen[v] = apos[c] >= first[v];
+        f[v] = !seen[v] ? 0.f : st[v].mc == kNegInf ? 1.f : fast_exp2(st[v].mc - top);
+        sum += seen[v] ? f[v] * st[v].l : 0.f;
       }
       const float inv = sum > 0.f ? 1.f / sum : 0.f;
       const float lse_v = sum > 0.f ? kLn2 * (top + __log2f(sum)) : kNegInf;
@@ -1173,7 +1179,7 @@ __device__ __forceinline__ void row_item8(const int32_t* it, int g, int poff, co
         for (int v = 0; v < 4; ++v) {
           const f32x4 x = sm.acc[v][c][dt][lane];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[e] += f[v] == 0.f ? 0.f : f[v] * x[e];
+          for (int e = 0; e < 4; ++e) o[e] += seen[v] ? f[v] * x[e] : 0.f;
         }
         if (!valid[c]) continue;
         if (part < 0) {

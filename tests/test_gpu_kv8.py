@@ -456,6 +456,49 @@ def test_rows_without_a_number_stay_visible(name, where):
     assert np.all(diff[keep.cpu().numpy()] <= 2 * bo[keep.cpu().numpy()])
 
 
+@pytest.mark.parametrize("where", ["key", "value"])
+@pytest.mark.parametrize("hq, d, n, L", [(8, 128, 1, 700), (8, 64, 1, 9001), (16, 128, 5, 900),
+                                         (16, 64, 5, 5000)])
+def test_joined_wavefronts_keep_what_is_not_a_number(hq, d, n, L, where):
+    """A NaN among keys whose weight underflows beside another wavefront's: the row is
+    NaN, or its element is, as it is where one item holds all keys."""
+    hkv = 2
+    table, nb = tables([L], 12)
+    c = Cache(nb, hkv, d, 12)
+    mq = meta(table, [L], [n])
+    kind = B.KIND_DECODE if n == 1 else B.KIND_VERIFY
+    plan, info = B.plan(kind, n, mq[1], mq[2], hq, hkv, d, 16, B.PA_BF16_KV8, block_table=mq[0])
+    from tests.test_capi_host import parse_plan
+    rows = parse_plan(plan)[3]
+    assert rows and all(t[7] & 2 for t in rows)  # every row item is one of a joined four
+    ws = torch.empty(max(16, int(info.workspace_bytes)), dtype=torch.uint8, device="cuda")
+    dm, dplan = [dev(x) for x in mq], dev(plan)
+    q = torch.zeros((n, hq, d), dtype=torch.bfloat16, device="cuda")
+    q[:, :, 0] = 16.0
+    out, lse = torch.empty_like(q), torch.empty((n, hq), device="cuda")
+    r = np.random.default_rng(12)
+    v = rows_of(r, L, hkv, d, "bf16")
+    # a step's, a wavefront's and the item's ends; the last n tokens are not seen by all rows
+    spots = sorted({0, 63, 191, 200, L // 3, L // 2, 3 * L // 4, L - n})
+    for i, at in enumerate(spots):
+        top = spots[(i + 1 + i % (len(spots) - 1)) % len(spots)]
+        k = np.zeros((L, hkv, d), np.float32)
+        k[top, :, 0] = 448.0  # its score lies above 600: 2^-900 for all others
+        B.kv8_append(dev(k), dev(v), *[dev(x) for x in meta(table, [L], [L])], *c.args)
+        blk, off = int(table[0, at // 16]), at % 16
+        if where == "key":
+            c.k.view(torch.uint8)[blk, 1, d // 64 - 1, off, 7] = 0x7F
+        else:
+            c.v.view(torch.uint8)[blk, 1, 9, off] = 0x7F
+        B.kv8_attention(kind, q, *c.args, *dm, dplan, info, ws, out, lse)
+        torch.cuda.synchronize()
+        g = hq // hkv
+        bad = torch.zeros(out.shape, dtype=torch.bool, device="cuda")
+        bad[:, g:, slice(None) if where == "key" else 9] = True
+        assert torch.equal(out.isnan(), bad), (at, top)
+        assert torch.equal(lse == -float("inf"), bad.all(2)), (at, top)
+
+
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("q_len", [1, 130])
 def test_values_near_the_largest_stay_finite(d, q_len):
