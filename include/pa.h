@@ -484,14 +484,16 @@ int pa_attn_decode_noalloc(const void* q, const void* k_cache, const void* v_cac
  * bits, largest finite value 448, no infinities).  scales[block][h][0] is the
  * keys' scale, [1] the values': the power of two 2^e as the byte e + 127, e of
  * -100 .. 120.  A code c stands for c * 2^e, which bf16 and float32 hold exactly
- * (beyond bf16's largest value: infinity).
+ * (256 * 2^120 and more, which no append stores: infinity).
  *
  * Storing: a block's e is the smallest with amax <= 448 * 2^e, amax the largest
  * finite magnitude among its new tokens' keys (values) of that kv-head; where
  * the block holds earlier tokens of the sequence, the larger of that and the
  * block's e, and where e grew the earlier tokens' codes are rounded again (the
  * shift is by a power of two, so a code only loses bits below 2^(e-9)).  A code
- * is x / 2^e rounded to nearest even; infinities and NaN are stored as NaN.
+ * is x / 2^e rounded to nearest even; infinities and NaN are stored as NaN, finite
+ * magnitudes above 240 * 2^120 = 3.19e38, whose nearest code may stand for 2^128,
+ * as that.
  * e does not shrink while a block fills: tokens rolled back (pa_seq_truncate)
  * may leave it larger than the rest needs.
  *

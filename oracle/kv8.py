@@ -6,7 +6,8 @@ m * 2^-9, m of 0 .. 7, below.  A (block, kv-head) of keys, and of values, is
 such numbers times 2^e.  Storing tokens: e is the smallest of -100 .. 120 with
 amax <= 448 * 2^e over the new tokens' finite values; where the block holds
 earlier tokens, no less than its e, and those are rounded again to the new one.
-Rounding is to nearest, ties to even m; what is not finite becomes NaN.
+Rounding is to nearest, ties to even m; what is not finite becomes NaN, and finite
+magnitudes above 240 * 2^120 (the number below 2^128) become that.
 
 The store holds the values (code * 2^e) in the layout of oracle.attention
 (K [NB, Hkv, bs, D], V [NB, Hkv, D, bs]) and the exponents [NB, Hkv, 2].
@@ -16,6 +17,7 @@ from __future__ import annotations
 import numpy as np
 
 EXP_MIN, EXP_MAX = -100, 120
+MOST = 240 * 2.0 ** 120
 
 
 def round_e4m3(x):
@@ -51,7 +53,7 @@ def _store(values, exps, off, x):
             if e > old:
                 values[h, :off] = np.ldexp(round_e4m3(np.ldexp(
                     values[h, :off].astype(np.float64), -e)), e)
-        rows = np.where(np.isfinite(rows), rows, np.nan)
+        rows = np.where(np.isfinite(rows), np.clip(rows, -MOST, MOST), np.nan)
         values[h, off:off + len(rows)] = np.ldexp(round_e4m3(np.ldexp(rows, -e)), e)
         exps[h] = e
 

@@ -100,6 +100,12 @@ __device__ __forceinline__ uint32_t codes_of(float x0, float x1, float x2, float
   int r = __builtin_amdgcn_cvt_pk_fp8_f32(x0 * s, x1 * s, 0, false);
   return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(x2 * s, x3 * s, r, true));
 }
+// Codes of the largest scale: finite values from 248 * 2^120 on were rounded to 256, which
+// would stand for 2^128; the code below does instead.  Byte by byte, without carries.
+__device__ __forceinline__ uint32_t below_256(uint32_t c) {
+  const uint32_t other = ((c & 0x7F7F7F7F) ^ 0x78787878) + 0x7F7F7F7F;  // bit 7: not +-256
+  return c - ((~other & 0x80808080) >> 7);
+}
 // Codes rounded again for a scale 1 / s times as large.
 __device__ __forceinline__ uint32_t codes_again(uint32_t c, float s) {
   const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(c, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(c, true);
@@ -207,7 +213,8 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(const T* __restrict__ k
         const float v = x[u].at(k);
         y[k] = fabsf(v) < __builtin_huge_valf() ? v : __builtin_nanf("");
       }
-      const u32x2 q = {codes_of(y[0], y[1], y[2], y[3], s), codes_of(y[4], y[5], y[6], y[7], s)};
+      u32x2 q = {codes_of(y[0], y[1], y[2], y[3], s), codes_of(y[4], y[5], y[6], y[7], s)};
+      if (e == kExpMax) q = u32x2{below_256(q[0]), below_256(q[1])};
       const int o = u * TI + sub;
       *reinterpret_cast<u32x2*>(side ? &vt[o][8 * c] : kb + c / 8 * 1024 + o * 64 + c % 8 * 8) = q;
     }

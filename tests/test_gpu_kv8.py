@@ -191,6 +191,43 @@ def test_append_of_values_at_the_ends_of_the_range(d):
     assert np.isnan(kc[table[7, 0], 0, :3]).all() and np.isfinite(kc[table[4, 0]]).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_largest_finite_values_stay_finite(dtype):
+    """Values whose nearest code would stand for 2^128 are stored as the largest below
+    it, 240 * 2^120: read back finite, and a value of no weight adds nothing."""
+    hkv, hq, d, L = 2, 4, 128, 20
+    largest = float(torch.finfo(DTYPE[dtype]).max)
+    table, nb = tables([L], 13)
+    c = Cache(nb, hkv, d, 13)
+    kc, vc = np.zeros((nb, hkv, 16, d)), np.zeros((nb, hkv, d, 16))
+    ex = kv8.new_exponents(nb, hkv)
+    k, v = np.zeros((L, hkv, d), np.float32), np.ones((L, hkv, d), np.float32)
+    v[3, :, 0], v[3, :, 1], v[3, :, 2], v[3, :, 3] = largest, -largest, 244 * 2.0 ** 120, 236 * 2.0 ** 120
+    v[17, 0], k[9, 1, 5] = 248 * 2.0 ** 120, -largest
+    k[18, :, 0] = 448.0
+    m = meta(table, [L], [L])
+    kv8.append(kc, vc, ex, *m, k, v)
+    B.kv8_append(dev(k, DTYPE[dtype]), dev(v, DTYPE[dtype]), *map(dev, m), *c.args)
+    ko, vo = (torch.empty((L, hkv, d), dtype=DTYPE[dtype], device="cuda") for _ in range(2))
+    B.kv8_read(ko, vo, *map(dev, m), *c.args)
+    q = torch.zeros((1, hq, d), dtype=torch.bfloat16, device="cuda")
+    q[:, :, 0] = 16.0
+    mq = meta(table, [L], [1])
+    plan, info = B.plan(B.KIND_DECODE, 1, mq[1], mq[2], hq, hkv, d, 16, B.PA_BF16_KV8)
+    out = torch.empty_like(q)
+    B.kv8_attention(B.KIND_DECODE, q, *c.args, *map(dev, mq), dev(plan), info, None, out)
+    torch.cuda.synchronize()
+    seq, pos = table[0, np.arange(L) // 16], np.arange(L) % 16
+    assert np.array_equal(ko.double().cpu().numpy(), kc[seq, :, pos])
+    assert np.array_equal(vo.double().cpu().numpy(), vc[seq, :, :, pos])
+    most = 240 * 2.0 ** 120
+    assert vc[seq[3], 0, :4, 3].tolist() == [most, -most, most, 240 * 2.0 ** 120]
+    assert np.abs(vc[np.isfinite(vc)]).max() == most and np.isfinite(vc).all()
+    # all weight is on key 18: ones, but for kv-head 0, where they are below its block's steps
+    assert np.array_equal(out.double().cpu().numpy()[0],
+                          np.repeat([np.zeros(d), np.ones(d)], hq // hkv, 0))
+
+
 def test_append_skips_what_it_cannot_place():
     """Block ids outside the cache, positions past the table and rows past the
     caller's write nothing; the other sequences are stored."""
