@@ -159,7 +159,7 @@ def run_workload(name, W, K, C, cpu_budget, profile=False, settle_ms=0.0):
     out = torch.empty((T, cfg.num_q_heads, cfg.head_dim), dtype=tdt, device="cuda")
     lse = torch.empty((T, cfg.num_q_heads), dtype=torch.float32, device="cuda")
     n = len(L0.seq_ids)
-    plan_words = plan_words_bound(cfg, n, T, wl.max_blocks_per_seq)
+    plan_words = plan_words_bound(cfg, n, T, wl.max_blocks_per_seq, kv8=False)
     stagings = [Staging("cuda", n, wl.max_blocks_per_seq, T, plan_words) for _ in range(2)]
     stream = torch.cuda.current_stream()
 

@@ -59,14 +59,16 @@ def marshal_launch(launch):
     return d["_batched"], d["_inputs"]
 
 
-def plan_words_bound(cfg, n_seqs: int, total_q: int, max_blocks_per_seq: int) -> int:
+def plan_words_bound(cfg, n_seqs: int, total_q: int, max_blocks_per_seq: int,
+                     kv8: bool = True) -> int:
     """Upper bound on the plan size of a launch of n_seqs sequences and
     total_q query tokens (tile items, key-split items of at least 256 keys,
     merge groups, cascade member tables, per-XCD padding; in a small launch
-    the key-split tiles and shared-prefix chunks that fill the chip; over the
-    8-bit cache two row items per sequence of four records each)."""
+    the key-split tiles and shared-prefix chunks that fill the chip; with
+    ``kv8`` the plan may be one over the 8-bit cache: two row items per
+    sequence of four records each)."""
     max_keys = max_blocks_per_seq * cfg.block_size
-    few = 8 * (total_q * cfg.group // 4 + n_seqs * (2 * (max_keys // 128 + 4) + 1))
+    few = kv8 * 8 * (total_q * cfg.group // 4 + n_seqs * (2 * (max_keys // 128 + 4) + 1))
     return few + 16384 + 32 + 8 * (cfg.num_kv_heads * (total_q * cfg.group // 128 + n_seqs)
                      + 2 * cfg.num_kv_heads * n_seqs * (max_keys // 256 + 2) + 64)
 

@@ -354,6 +354,29 @@ def test_plans_cover_every_row_once(seed):
         assert info.workspace_bytes <= B.NOALLOC_WORKSPACE_BYTES
 
 
+@pytest.mark.parametrize("seed", range(12))
+def test_plan_bound_without_the_8_bit_cache(seed):
+    """Callers that plan for bf16 and float32 caches only need not hold its row items."""
+    r = np.random.default_rng([seed, 3])
+    n, hkv, G = int(r.integers(1, 60)), int(r.choice([1, 2, 8])), int(r.choice([1, 4, 8, 40]))
+    L = r.integers(1, 5000, size=n)
+    q = np.minimum(L, r.choice([1, 2, 5, 33, 300], size=n))
+    kind = B.KIND_PREFILL
+    if seed % 2:
+        q[:], kind = 1, B.KIND_DECODE
+    cu = np.concatenate([[0], np.cumsum(q)])
+    mb = int((L.max() + 15) // 16)
+    cfg = synth.AttnConfig("", "bf16", hkv * G, hkv, 128, 16, 0)
+    least = plan_words_bound(cfg, n, int(cu[-1]), mb, kv8=False)
+    # tiles, key-split items and merge groups, 8 words each, and what does not grow
+    assert least == 16416 + 8 * (hkv * (int(cu[-1]) * G // 128 + n)
+                                 + 2 * hkv * n * (mb * 16 // 256 + 2) + 64)
+    assert least < plan_words_bound(cfg, n, int(cu[-1]), mb)
+    for dtype in (B.PA_BF16, B.PA_F32):
+        _, info = B.plan(kind, 1, L, cu, hkv * G, hkv, 128, 16, dtype)
+        assert info.plan_words <= least
+
+
 @pytest.mark.parametrize("q", [1, 5])
 @pytest.mark.parametrize("num_cus, shared", [(256, False), (23, False), (22, True)])
 def test_small_launches_leave_shared_prefixes_to_their_row_items(q, num_cus, shared):
