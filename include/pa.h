@@ -479,6 +479,9 @@ int pa_attn_decode_noalloc(const void* q, const void* k_cache, const void* v_cac
  *   k_cache[num_blocks][num_kv_heads][head_dim/64][16][64]   bytes
  *   v_cache[num_blocks][num_kv_heads][head_dim][16]          bytes
  *   scales[num_blocks][num_kv_heads][2]                      bytes
+ * (the memory of the scales a multiple of 4 bytes: where num_blocks * num_kv_heads is
+ * odd, attention reads the last pair with the two bytes behind it, which may hold
+ * anything and are not written).
  * Key dim d of the token at offset o is k_cache[block][h][d/64][o][d%64], value
  * dim d v_cache[block][h][d][o]: e4m3 codes (1 sign, 4 exponent, 3 mantissa
  * bits, largest finite value 448, no infinities).  scales[block][h][0] is the

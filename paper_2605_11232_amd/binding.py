@@ -617,7 +617,8 @@ def attention_decode_noalloc(q, k_cache, v_cache, block_table, seq_lens, cu_seql
 def kv8_cache_shapes(num_blocks: int, num_kv_heads: int, head_dim: int, block_size: int = 16):
     """Shapes of an 8-bit cache's (k_cache, v_cache, scales); the caches are
     torch.float8_e4m3fn, the scales torch.uint8 (exponent + 127 of keys and of
-    values).  Contents need no initialisation."""
+    values), in memory of a multiple of 4 bytes, as torch allocates it.  Contents need
+    no initialisation."""
     return ((num_blocks, num_kv_heads, head_dim // 64, block_size, 64),
             (num_blocks, num_kv_heads, head_dim, block_size), (num_blocks, num_kv_heads, 2))
 

@@ -334,8 +334,9 @@ __device__ __forceinline__ void tile_item(const int32_t* it, int g, int poff, co
   const uint32_t koff8 = piece_off + slot8 * 64 + 32 * hh + 16 * (lane & 1);
   const uint32_t kdst8 = hh * 64 + 4 * pos8 + ((2 * (lane & 1)) ^ ((pos8 >> 2) & 3));
   // Blocks and scales of a step's pieces.  A block is 16 D hkv bytes, its scales are 2
-  // hkv; a pair lies in one aligned word (the array is 4-byte aligned), which a scalar
-  // load takes.
+  // hkv; a pair lies in one aligned word (the array's memory is whole words), which a
+  // scalar load takes (16-bit vector loads: 32 prompts 816 us against 805, 256 decode
+  // requests 77.6 against 75.7).
   auto step_blocks8 = [&](int t0, int s) {
     const int jb = t0 / kBlock;
     win.seek(jb);

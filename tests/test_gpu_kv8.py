@@ -643,6 +643,36 @@ def test_blocks_past_4_gib(q_lens):
     assert torch.isfinite(results[0][2].float()).all()
 
 
+@pytest.mark.parametrize("q_lens", [[40, 3], [1, 1]])
+def test_odd_scales_array(q_lens):
+    """One kv-head and an odd number of blocks: the last pair of scales shares its word
+    with two bytes behind the array, which change nothing and stay as they are."""
+    hq, hkv, d, lens = 4, 1, 128, [300, 77]
+    table, nb = tables(lens, 14, spare=0)
+    nb += 1 - nb % 2
+    table[0, 3] = nb - 1  # the last block is in use
+    r = np.random.default_rng(14)
+    k, v = (dev(rows_of(r, sum(lens), hkv, d, "bf16"), torch.bfloat16) for _ in range(2))
+    q = dev(rows_of(r, sum(q_lens), hq, d, "bf16"), torch.bfloat16)
+    kind = B.KIND_DECODE if q_lens == [1, 1] else B.KIND_PREFILL
+    m, mq = meta(table, lens, lens), meta(table, lens, q_lens)
+    plan, info = B.plan(kind, 1, mq[1], mq[2], hq, hkv, d, 16, B.PA_BF16_KV8, block_table=mq[0])
+    ws = torch.empty(max(16, int(info.workspace_bytes)), dtype=torch.uint8, device="cuda")
+    results = []
+    for behind in (0, 255):
+        memory = torch.full((2 * nb + 2,), behind, dtype=torch.uint8, device="cuda")
+        c = Cache(nb, hkv, d, 14)
+        cache = c.k, c.v, memory[:2 * nb].view(nb, hkv, 2)
+        B.kv8_append(k, v, *map(dev, m), *cache)
+        out, lse = torch.empty_like(q), torch.empty((sum(q_lens), hq), device="cuda")
+        B.kv8_attention(kind, q, *cache, *map(dev, mq), dev(plan), info, ws, out, lse)
+        torch.cuda.synchronize()
+        assert memory[2 * nb:].tolist() == [behind] * 2
+        results.append((out, lse))
+    assert torch.isfinite(results[0][0]).all()
+    assert torch.equal(results[0][0], results[1][0]) and torch.equal(results[0][1], results[1][1])
+
+
 # ---- norms and rotation -----------------------------------------------------------------------
 
 ROPE = [
