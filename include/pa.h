@@ -545,7 +545,12 @@ int pa_kv8_read(void* k_out, int64_t k_stride, void* v_out, int64_t v_stride,
  * Slots behind a sequence's last token may hold any bytes.  A key that is NaN
  * makes the rows that see it NaN, a value that is NaN those rows' element of its
  * dim; in a launch of several tokens per sequence it may make that element of the
- * sequence's other rows NaN, too, as with the bf16 cache. */
+ * sequence's other rows NaN, too, as with the bf16 cache.  A row whose sum is NaN
+ * (its query, or a key that it sees) has the log-sum-exp minus infinity, the bf16
+ * cache's, too: a caller that combines parts of rows by it must look at the outputs.
+ * Scores, exponentials, sums and the log-sum-exp are float32; each probability is
+ * rounded to bf16 for its product with the value, which with the output's own
+ * rounding puts an output within 2^-8 (|out| + sum_t p_t |v_t|) of the exact one. */
 int pa_kv8_attn_prefill(const void* q, const void* k_cache, const void* v_cache,
                         const uint8_t* scales, int32_t num_blocks, const int32_t* block_table,
                         int32_t max_blocks_per_seq, const int32_t* seq_lens,
