@@ -71,10 +71,16 @@ constexpr int64_t kSharedMinKeys8 = 512;
 // 4 decode requests on 2048 shared and 200-400 own keys, 64/8 heads, 12.2 and 11.0, 16 on
 // 320 15.5 and 8.6 (32/8 heads of 64 dims 11.0 and 6.5), 8 on 1024 and 1500-2500 (760 keys
 // per CU) 17.1 and 14.5; 2 verifications of 6 tokens on 320, 28/4 heads, 14.1 and 10.1,
-// 64/8 heads 16 on 1024 and 200-400 (660) 25.7 and 15.1, 8 on 1024 and 1500-2500 (760)
-// 23.4 and 24.9; at 32/8 heads of 64 dims and 200-400 own keys the verifications lose up to
-// 1.5 us from 512 shared keys on (4 on 1024: 11.1 and 12.3).  Past it: 8 decode requests on
+// 64/8 heads 16 on 1024 and 200-400 (660) 25.7 and 15.1.  Past it: 8 decode requests on
 // 2048 and 1500-2500 (1010) 17.0 and 17.1, 16 (2020) 21.8 and 27.6.
+// Verifications (more than 16 rows) that would be merged, on more row workgroups than CUs,
+// so that most CUs wait for those with two: at head_dim 64 they split it off below the
+// line, too (207 random launches take 4.5 % less so, from 24 % more to 23 % less; 32/8 heads,
+// 5 tokens, 8 on 2048 and 800-1200 14.1 and 16.0); at 128 they are even (195 launches of up
+// to 1.25 row workgroups per CU, 1 % more, from 28 % more to 15 % less; 64/8 heads, 5 tokens,
+// 8 on 1024 and 1500-2500 23.4 and 24.9, 8 tokens, 4 on 2048 and 1500-2500, 23.8 and 21.0).
+// On fewer workgroups some lose a microsecond without (32/8 heads of 64 dims, 5 tokens, 4
+// on 1024 and 200-400 11.1 and 12.3), as many gain one (4 on 4096 and 20-60 12.9 and 12.3).
 constexpr int64_t kUnsharedKeysPerCu8 = 768;
 constexpr int64_t kPrivateTileKeys = 4160;  // most private keys a few-row tile item covers
 constexpr int64_t kMinTileKeys = 256;       // fewest, in launches that leave compute units idle
@@ -418,6 +424,15 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
     auto row_pieces = [&](int32_t r) { return cdiv(qlen(r) * G, pa::kRowItemRows); };
     const int64_t row_step = kv8 ? pa::kKeyStep8 : pa::kKeyStep;
     const double key_bytes = head_dim * (kv8 ? 2 : 4);  // a key and its value
+    // Keys of a row item where all items hold `keys` and `waves` wavefronts are wanted; a
+    // row item's block ids fit one wavefront (64 lanes): at most 1024 keys.
+    auto item_chunk = [&](int64_t keys, int64_t least, int64_t waves) {
+      const int64_t chunk = std::max<int64_t>(least, cdiv(keys, std::max<int64_t>(1, waves)));
+      return std::min<int64_t>(cdiv(chunk, row_step) * row_step, int64_t(pa::kRowItemBlocks) * block_size);
+    };
+    auto small_rows = [&](int64_t keys) {
+      return cdiv(keys, kSmallRowKeys) <= (head_dim == 64 ? 6 : 3) * int64_t(num_cus);
+    };
 
     // Cascade groups: few-row sequences with the same first block and
     // q_len whose leading blocks coincide share those keys; attention over
@@ -430,13 +445,29 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
     std::vector<int32_t> cg_keys, cg_chunks;  // shared keys, key chunks (one merge part each)
     bool share = block_table != nullptr;
     if (share && kv8) {
-      int64_t keys = 0;
-      bool rows_only = true;
+      int64_t keys = 0, items = 0;
+      bool rows_only = true, wide = false;
       for (int32_t r = 0; r < n_seqs; ++r) {
-        rows_only = rows_only && (qlen(r) == 0 || is_row(r));
-        keys += int64_t(seq_lens[r]) * num_kv_heads * (qlen(r) > 0);
+        if (qlen(r) == 0) continue;
+        rows_only = rows_only && is_row(r);
+        wide = wide || qlen(r) * G > 16;
+        keys += int64_t(seq_lens[r]) * num_kv_heads;
+        items += int64_t(seq_lens[r]) * num_kv_heads * row_pieces(r);
       }
       share = !rows_only || keys > kUnsharedKeysPerCu8 * num_cus;
+      if (!share && wide && head_dim == 64) {
+        // the row workgroups (joined items) that the launch has without tiles
+        const int64_t reach = 4 * item_chunk(items, small_rows(items) ? kSmallRowKeys : kMinRowKeys,
+                                             kWideRowWavesPerCu8 * num_cus);
+        int64_t quads = 0;
+        bool merged = false;
+        for (int32_t r = 0; r < n_seqs; ++r) {
+          if (qlen(r) == 0) continue;
+          quads += num_kv_heads * row_pieces(r) * cdiv(seq_lens[r], reach);
+          merged = merged || seq_lens[r] > reach;
+        }
+        share = merged && quads > num_cus;
+      }
     }
     if (share) {
       std::vector<std::pair<int64_t, int32_t>> cand;
@@ -513,10 +544,7 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
     // private parts (the workspace bound).
     std::vector<int64_t> row_chunk;
     auto split_rows = [&](int64_t least) {
-      int64_t chunk = std::max<int64_t>(least, cdiv(item_keys, std::max<int64_t>(1, target_waves)));
-      chunk = cdiv(chunk, row_step) * row_step;
-      // a row item's block ids fit one wavefront (64 lanes): at most 1024 keys
-      chunk = std::min<int64_t>(chunk, int64_t(pa::kRowItemBlocks) * block_size);
+      const int64_t chunk = item_chunk(item_keys, least, target_waves);
       row_chunk.assign(n_seqs, chunk);
       if (row_keys == 0) return;
       std::vector<std::pair<int64_t, int32_t>> by_len;
@@ -537,9 +565,11 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
     // Over the 8-bit cache sequences whose keys give a workgroup's four wavefronts a row
     // item's length each run as such: they join their results in LDS, a quarter of the
     // parts that the merge would read.  So do shorter ones, down to two steps a wavefront,
-    // while there are no more of them than workgroups run at once (24 verifications of 5
-    // tokens 45 us, 51 with separate items; 256 decode requests of 256-1152 keys 79, 74
-    // with separate ones).
+    // while one workgroup for each kv-head and 32 rows comes to no more than run at once (24
+    // verifications of 5 tokens 45 us, 51 with separate items; 256 decode requests of
+    // 256-1152 keys 79, 74 with separate ones).  Neither a sequence's several parts nor the
+    // shared prefixes' workgroups count: with them more may be launched than run at once (24
+    // verifications on 4096 shared keys: 576 where 512 do).
     auto row_waves = [&](int32_t r) -> int64_t {
       const int64_t quarter = cdiv(cdiv(seq_lens[r] - kstart[r], 4), row_step) * row_step;
       return kv8 && !on_tiles(r) && quarter >= 2 * row_step &&
@@ -557,9 +587,7 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
         if (is_row(r)) count_private(r);
     };
     for (int32_t S : cg_keys) cg_chunks.push_back(int32_t(cdiv(S, pa::kSharedChunk)));
-    const bool small_rows =
-        !long_seqs && cdiv(item_keys, kSmallRowKeys) <= (head_dim == 64 ? 6 : 3) * int64_t(num_cus);
-    split_rows(small_rows ? kSmallRowKeys : kMinRowKeys);
+    split_rows(!long_seqs && small_rows(item_keys) ? kSmallRowKeys : kMinRowKeys);
     count_all_private();
 
     // Key chunks of the shared prefixes.  A shared item is a serial walk over

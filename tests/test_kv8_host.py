@@ -397,3 +397,21 @@ def test_small_launches_leave_shared_prefixes_to_their_row_items(q, num_cus, sha
                         B.PA_BF16_KV8, num_cus=num_cus, block_table=bt)
     assert info.n_shared_items > 0
     check_plan8(plan, info, L, n, 8, 2, 128)
+
+
+@pytest.mark.parametrize("d, q, num_cus, shared", [(64, 5, 256, True), (64, 5, 304, False),
+                                                   (64, 1, 256, False), (128, 5, 256, False)])
+def test_small_verifications_split_shared_prefixes_off(d, q, num_cus, shared):
+    """At head_dim 64, where their row workgroups (joined fours of up to 384 keys each) are
+    more than the CUs: 8 sequences of 3000 keys and 8 kv-heads come to more than 256."""
+    L = np.array([2848 + 40 * i for i in range(8)])
+    bt = np.full((8, 200), -1, np.int32)
+    for s in range(8):
+        bt[s, :128] = np.arange(128)
+        n = (int(L[s]) + 15) // 16 - 128
+        bt[s, 128:128 + n] = 128 + 80 * s + np.arange(n)
+    kind = B.KIND_DECODE if q == 1 else B.KIND_VERIFY
+    plan, info = B.plan(kind, q, L, np.arange(9) * q, 32, 8, d, 16, B.PA_BF16_KV8,
+                        num_cus=num_cus, block_table=bt)
+    assert (info.n_shared_items > 0) == shared
+    check_plan8(plan, info, L, np.full(8, q), 4, 8, d)
