@@ -78,10 +78,11 @@ __device__ __forceinline__ BlockRows find_rows(const Kv8Args& a, int slot) {
   }
   const int first = L - n;  // first row's position
   if (n <= 0 || first < 0 || c0 < 0 || j < 0 || j * kBlock >= L || j >= a.max_blocks) return none;
-  const int p0 = int(j) * kBlock, off0 = max(first - p0, 0), off1 = min(L - p0, kBlock);
+  const int p0 = int(j) * kBlock, off0 = max(first - p0, 0);
   const int row0 = c0 + p0 + off0 - first;
-  // rows past the caller's: cu does not end at n_tokens
-  if ((int64_t)row0 + (off1 - off0) > a.n_tokens) return none;
+  // cu may run past the caller's rows
+  const int off1 = min(min(L - p0, kBlock), off0 + max(a.n_tokens - row0, 0));
+  if (off1 <= off0) return none;
   return {a.bt[(int64_t)r * a.max_blocks + j], off0, off1, row0};
 }
 

@@ -258,6 +258,34 @@ def test_append_skips_what_it_cannot_place():
     assert all(np.array_equal(x, y) for x, y in zip(a, b))
 
 
+@pytest.mark.parametrize("lens, q, n", [([20, 40, 18], [20, 4, 2], 22), ([3, 21, 9], [1, 2, 1], 2),
+                                        ([40], [40], 21)])
+def test_rows_past_the_callers_are_skipped(lens, q, n):
+    """cu_seqlens that run past n_tokens, in the middle of a block: the rows before are
+    stored, and read back, those behind are not touched."""
+    hkv, d = 2, 64
+    table, nb = tables(lens, 15)
+    c, want = Cache(nb, hkv, d, 15), Cache(nb, hkv, d, 15)
+    r = np.random.default_rng(15)
+    k, v = (dev(rows_of(r, sum(q), hkv, d, "bf16"), torch.bfloat16) for _ in range(2))
+    m = meta(table, lens, q)
+    at = np.minimum(m[2], n)
+    cut = [table, np.array(lens, np.int32) - np.diff(m[2] - at).astype(np.int32), at]
+    for x in (c, want):  # what lies before the new tokens
+        before = np.array(lens) - np.array(q)
+        old = dev(rows_of(np.random.default_rng(16), int(before.sum()), hkv, d, "bf16"), torch.bfloat16)
+        B.kv8_append(old, old, *map(dev, meta(table, before, before)), *x.args)
+    B.kv8_append(k[:n], v[:n], *map(dev, cut), *want.args)
+    B.kv8_append(k[:n], v[:n], *map(dev, m), *c.args)
+    torch.cuda.synchronize()
+    assert all(np.array_equal(a, b) for a, b in zip(c.raw(), want.raw()))
+    out = torch.full((4, n + 3, hkv, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    B.kv8_read(out[0, :n], out[1, :n], *map(dev, cut), *c.args)
+    B.kv8_read(out[2, :n], out[3, :n], *map(dev, m), *c.args)
+    torch.cuda.synchronize()
+    assert torch.equal(out[:2], out[2:]) and (out[:, n:] == 7).all() and (out[:, :n] != 7).any()
+
+
 # ---- attention --------------------------------------------------------------------------------
 
 def bounds(q, kc, vc, table, lens, cu, hkv, out, lse):
