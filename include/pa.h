@@ -540,7 +540,8 @@ int pa_kv8_read(void* k_out, int64_t k_stride, void* v_out, int64_t v_stride,
  * pa_attn_verify and pa_attn_decode_noalloc with bf16 queries and outputs, k_t
  * and v_t the values that the codes stand for.  Plans are built with dtype
  * PA_BF16_KV8 (pa_attn_plan, pa_prepare_launch; the workspace bounds hold for
- * them too).  Arguments, layouts, ownership and errors as for those calls; q,
+ * them too; the call without a workspace shares pa_attn_decode_noalloc's array
+ * with it).  Arguments, layouts, ownership and errors as for those calls; q,
  * out and the caches must be 16-byte aligned, the scales 4-byte (PA_ERR_ARG).
  * Slots behind a sequence's last token may hold any bytes.  A key that is NaN
  * makes the rows that see it NaN, a value that is NaN those rows' element of its
@@ -614,9 +615,9 @@ int pa_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_st
 
 /* Timing hook, for callers that time attention calls on the device
  * (benchmarks, profilers) without event packets between kernels: the next
- * pa_attn_* call on this thread attaches start_event to the dispatch of its
- * first kernel (recorded when that kernel starts) and stop_event to the
- * dispatch of its last (recorded when it ends), through hipExtLaunchKernel,
+ * pa_attn_* or pa_kv8_attn_* call on this thread attaches start_event to the
+ * dispatch of its first kernel (recorded when that kernel starts) and stop_event
+ * to the dispatch of its last (recorded when it ends), through hipExtLaunchKernel,
  * instead of separate event records, each of which idles the device for a
  * few microseconds between back-to-back kernels.  Either may be NULL.  The
  * events are hipEvent_t handles the caller created (with timing, for

@@ -190,8 +190,9 @@ __device__ __forceinline__ float max_halves(float x) {
 // the same LDS tiles: step t stores K of step t + 2 and V^T of step t + 1, loaded
 // during step t - 1, and loads the next.  Each value is converted once per
 // workgroup, not once per wavefront that reads it: 32 prompts on 2048 cached tokens
-// take 795 us against 752 over a bf16 cache, of which the conversions are 32 VALU
-// instructions in about 160 a step and the float32 sums 16.
+// take 792 to 825 us on different cards, on one of them 811 against 741 over a bf16 cache
+// of the same values; the conversions are 32 VALU instructions in about 160 a step, the
+// float32 sums 16.
 template <int D, int NSUB, bool KV8, bool SHARED, bool FULL, bool STREAM = false>
 __device__ __forceinline__ void tile_item(const int32_t* it, int g, int poff, const AttnArgs& a,
                                           TileSmem<D, NSUB>& sm) {
@@ -1214,7 +1215,10 @@ __device__ __forceinline__ void row_item8(const int32_t* it, int g, int poff, co
 // from paying for the wildcard loop; a launch with only 16-row row items
 // runs at three waves per SIMD, and so does every launch at head_dim 64, whose
 // tiles fit 168 registers (24 requests' prefill 123 us against 138 with two).
-// Over the 8-bit cache 16-row items at head_dim 128 take two sets of loads and two waves.
+// Over the 8-bit cache 16-row items at head_dim 128 take two sets of loads and two waves,
+// and the kernels that hold more than one kind of item do not fit their registers: 20 to
+// 56 spilled ones (MIX 6, 7, 15, at head_dim 64 9, too; the bf16 kernels none), stored and
+// loaded outside the key loops, at head_dim 64 also once per item of the tail lists.
 template <int D, int MIX, bool KV8>
 constexpr int waves_per_eu() {
   return (MIX == 2 && !KV8) || D == 64 ? 3 : kTileWavesPerEu;
