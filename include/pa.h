@@ -44,8 +44,8 @@
  *  - A query at logical position a sees keys 0..a (causal, bottom-right).
  *  - Supported: block_size 16, head_dim 64 or 128, num_q_heads a multiple of
  *    num_kv_heads; dtype PA_BF16 (MFMA path, float32 accumulation) or PA_F32
- *    (float32 throughout).  The pa_kv8_* calls work on an 8-bit cache whose
- *    layout is given there.  Integers are int32; num_blocks * block_size must
+ *    (float32 throughout).  The pa_kv8_* and pa_kv4_* calls work on an 8-bit and
+ *    a 4-bit cache, whose layouts are given there.  Integers are int32; num_blocks * block_size must
  *    be below 2^31.
  *  - Not thread-safe per pool; device calls on one stream are ordered.
  */
@@ -71,7 +71,8 @@ typedef enum {
 typedef enum {
   PA_F32 = 0,
   PA_BF16 = 1,
-  PA_BF16_KV8 = 2 /* launch plans only: bf16 queries over the 8-bit cache */
+  PA_BF16_KV8 = 2, /* launch plans only: bf16 queries over the 8-bit cache */
+  PA_BF16_KV4 = 4  /* and over the 4-bit cache (3 is no type) */
 } pa_dtype;
 
 /* Message describing the calling thread's most recent error ("" if none). */
@@ -291,8 +292,8 @@ typedef struct pa_plan_info {
  * is too small the call fails with PA_ERR_ARG and *info holds the size.
  * kind PA_KIND_DECODE requires every q_len == 1, PA_KIND_VERIFY every q_len ==
  * n_q (1..8); PA_KIND_PREFILL takes any q_len >= 0 (prefill chunks and decode
- * tokens may be mixed).  dtype: PA_BF16, PA_F32, or PA_BF16_KV8 for the
- * pa_kv8_attn_* calls.  num_cus = compute units to fill (0: 256).
+ * tokens may be mixed).  dtype: PA_BF16, PA_F32, or PA_BF16_KV8 and
+ * PA_BF16_KV4 for the pa_kv8_attn_* and pa_kv4_attn_* calls.  num_cus = compute units to fill (0: 256).
  * Errors: PA_ERR_ARG, PA_ERR_UNSUPPORTED. */
 int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int32_t* seq_lens,
                  const int32_t* cu_seqlens_q, const int32_t* block_table,
@@ -585,6 +586,90 @@ int pa_kv8_attn_decode_noalloc(const void* q, const void* k_cache, const void* v
                                float scale, int32_t* plan, const pa_plan_info* info, void* out,
                                float* lse, void* stream);
 
+/* ------------------------------------------------------------------------ *
+ * The 4-bit cache.                                                           *
+ * ------------------------------------------------------------------------ */
+
+/* A cache of little more than a quarter of the bf16 cache's bytes, over the same
+ * blocks, block tables and pool:
+ *   k_cache[num_blocks][num_kv_heads][16][head_dim/2]          bytes
+ *   v_cache[num_blocks][num_kv_heads][head_dim/32][16][2][8]   bytes
+ *   scales[num_blocks][num_kv_heads][head_dim/32 + 1][16]      bytes
+ * Codes are e2m1 (1 sign, 2 exponent, 1 mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and
+ * their negatives), two in a byte, the first in its low half.  Key dims d, d + 1 (d even)
+ * of the token at offset o are k_cache[block][h][o][d/2]; value dim 32 c + 16 a + i of the
+ * tokens o, o + 1 (o even) v_cache[block][h][c][i][a][o/2].  scales[block][h][c][o] is the
+ * scale of key dims 32 c .. 32 c + 31 of the token at offset o, the last row that of its
+ * value, all dims: the power of two 2^e as the byte e + 127, e of -100 .. 100, or 255.  A
+ * code c stands for c * 2^e, which bf16 and float32 hold exactly, or, with the scale 255,
+ * for NaN (whatever the code; 255 comes with codes of zero, and attention relies on it).
+ *
+ * Storing: e is the smallest with amax <= 7 * 2^e, amax the largest magnitude among the
+ * values that share the scale (up to 7 the nearest code is 6, as far off as values below
+ * may be).  A code is x / 2^e rounded to nearest even, and 6 where that is more: finite
+ * magnitudes above 7 * 2^100 = 8.9e30 are stored as 6 * 2^100.  Where one of the values
+ * that share a scale is not finite, all of them are stored as NaN.  A token's bytes do not
+ * depend on other tokens: nothing is rounded twice, and rows may come in any pieces.
+ *
+ * Rows are found by the launch's metadata, as for the 8-bit cache.  A block that gets new
+ * tokens must be in one sequence's table only. */
+
+/* Quantise the keys/values of n_tokens new tokens into the cache: arguments, skipped rows,
+ * slots left alone and errors as pa_kv8_append; the scales must be 16-byte aligned. */
+int pa_kv4_append(const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+                  const int32_t* block_table, int32_t max_blocks_per_seq, const int32_t* seq_lens,
+                  const int32_t* cu_seqlens, int32_t n_seqs, int32_t n_tokens, void* k_cache,
+                  void* v_cache, uint8_t* scales, int32_t num_blocks, int32_t num_kv_heads,
+                  int32_t head_dim, int32_t block_size, int32_t dtype, void* stream);
+
+/* Read tokens back as rows, the inverse of pa_kv4_append with the same arguments; as
+ * pa_kv8_read. */
+int pa_kv4_read(void* k_out, int64_t k_stride, void* v_out, int64_t v_stride,
+                const int32_t* block_table, int32_t max_blocks_per_seq, const int32_t* seq_lens,
+                const int32_t* cu_seqlens, int32_t n_seqs, int32_t n_tokens, const void* k_cache,
+                const void* v_cache, const uint8_t* scales, int32_t num_blocks,
+                int32_t num_kv_heads, int32_t head_dim, int32_t block_size, int32_t dtype,
+                void* stream);
+
+/* Attention over the 4-bit cache: as the pa_kv8_attn_* calls, with plans of dtype
+ * PA_BF16_KV4 and 16-byte aligned scales.  Slots behind a sequence's last token may hold
+ * any bytes.  A key that is NaN makes the rows that see it NaN, a value that is NaN those
+ * rows where their probability of it does not round to zero; rows that do not see it stay
+ * as they are.  A row whose sum is NaN has the log-sum-exp minus infinity.  Rounding as for
+ * the 8-bit cache: each probability to bf16 for its product with the value. */
+int pa_kv4_attn_prefill(const void* q, const void* k_cache, const void* v_cache,
+                        const uint8_t* scales, int32_t num_blocks, const int32_t* block_table,
+                        int32_t max_blocks_per_seq, const int32_t* seq_lens,
+                        const int32_t* cu_seqlens_q, int32_t n_seqs, int32_t total_q,
+                        int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                        int32_t block_size, float scale, int32_t* plan, const pa_plan_info* info,
+                        void* workspace, size_t workspace_bytes, void* out, float* lse,
+                        void* stream);
+int pa_kv4_attn_decode(const void* q, const void* k_cache, const void* v_cache,
+                       const uint8_t* scales, int32_t num_blocks, const int32_t* block_table,
+                       int32_t max_blocks_per_seq, const int32_t* seq_lens,
+                       const int32_t* cu_seqlens_q, int32_t n_seqs, int32_t total_q,
+                       int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                       int32_t block_size, float scale, int32_t* plan, const pa_plan_info* info,
+                       void* workspace, size_t workspace_bytes, void* out, float* lse,
+                       void* stream);
+int pa_kv4_attn_verify(const void* q, const void* k_cache, const void* v_cache,
+                       const uint8_t* scales, int32_t num_blocks, const int32_t* block_table,
+                       int32_t max_blocks_per_seq, const int32_t* seq_lens,
+                       const int32_t* cu_seqlens_q, int32_t n_seqs, int32_t total_q,
+                       int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                       int32_t block_size, float scale, int32_t* plan, const pa_plan_info* info,
+                       void* workspace, size_t workspace_bytes, void* out, float* lse,
+                       void* stream);
+int pa_kv4_attn_decode_noalloc(const void* q, const void* k_cache, const void* v_cache,
+                               const uint8_t* scales, int32_t num_blocks,
+                               const int32_t* block_table, int32_t max_blocks_per_seq,
+                               const int32_t* seq_lens, const int32_t* cu_seqlens_q,
+                               int32_t n_seqs, int32_t total_q, int32_t num_q_heads,
+                               int32_t num_kv_heads, int32_t head_dim, int32_t block_size,
+                               float scale, int32_t* plan, const pa_plan_info* info, void* out,
+                               float* lse, void* stream);
+
 /* Norms of queries and keys for each head and the rotation by position, in one
  * pass over a step's rows, on their way from the projection to the append and
  * the attention call.  For token t, head h of q (of k likewise, with k_weight):
@@ -615,7 +700,7 @@ int pa_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_st
 
 /* Timing hook, for callers that time attention calls on the device
  * (benchmarks, profilers) without event packets between kernels: the next
- * pa_attn_* or pa_kv8_attn_* call on this thread attaches start_event to the
+ * pa_attn_*, pa_kv8_attn_* or pa_kv4_attn_* call on this thread attaches start_event to the
  * dispatch of its first kernel (recorded when that kernel starts) and stop_event
  * to the dispatch of its last (recorded when it ends), through hipExtLaunchKernel,
  * instead of separate event records, each of which idles the device for a

@@ -10,13 +10,14 @@ from __future__ import annotations
 
 import numpy as np
 
-from . import kv8
+from . import kv4, kv8
 from .apc import PrefixCacheOracle
 from .attention import kv_append, new_cache, paged_attention
 
 
 class OracleReplay:
-    def __init__(self, wl, store_values: bool = True, kv8: bool = False):
+    def __init__(self, wl, store_values: bool = True, kv8: bool = False,
+                 kv4: bool = False):
         cfg = wl.cfg
         self.wl = wl
         self.pool = PrefixCacheOracle(wl.num_blocks, cfg.block_size, wl.free_order)
@@ -29,13 +30,16 @@ class OracleReplay:
             self.v_cache = self.v_cache.astype(np.float32)
             if kv8:  # an 8-bit cache: the values its codes stand for (oracle.kv8)
                 self.exps = np.zeros((wl.num_blocks, cfg.num_kv_heads, 2), dtype=np.int64)
-        self.kv8 = kv8
+        self.kv8, self.kv4 = kv8, kv4  # kv4: the values that a 4-bit cache holds (oracle.kv4)
         self.n_cached = {}
 
     def _append(self, md, k, v):
         if self.kv8:
             kv8.append(self.k_cache, self.v_cache, self.exps, md["block_table"], md["seq_lens"],
                        md["cu_seqlens_q"], k, v)
+        elif self.kv4:
+            k, v = kv4.round_keys(k), kv4.round_values(v)
+            kv_append(self.k_cache, self.v_cache, md["slot_mapping"], k, v)
         else:
             kv_append(self.k_cache, self.v_cache, md["slot_mapping"], k, v)
 

@@ -16,7 +16,7 @@ LIB_PATH = os.path.join(_HERE, "libpa.so")
 
 PA_OK, PA_ERR_ARG, PA_ERR_UNSUPPORTED, PA_ERR_NO_BLOCKS, PA_ERR_UNKNOWN_SEQ, PA_ERR_LAUNCH = (
     0, -1, -2, -3, -4, -5)
-PA_F32, PA_BF16, PA_BF16_KV8 = 0, 1, 2
+PA_F32, PA_BF16, PA_BF16_KV8, PA_BF16_KV4 = 0, 1, 2, 4
 QK_NORM, ROPE_INTERLEAVED = 1, 2
 OP_ADD, OP_EXTEND, OP_TRUNCATE, OP_FREE = 0, 1, 2, 3
 KIND_PREFILL, KIND_DECODE, KIND_VERIFY = 0, 1, 2
@@ -33,6 +33,8 @@ EXPORTS = ["pa_last_error", "pa_abi_version", "pa_pool_create", "pa_pool_destroy
            "pa_stage_upload", "pa_attn_workspace_size", "pa_attn_decode_workspace_size",
            "pa_attn_decode_noalloc", "pa_kv8_append", "pa_kv8_read", "pa_kv8_attn_prefill",
            "pa_kv8_attn_decode", "pa_kv8_attn_verify", "pa_kv8_attn_decode_noalloc",
+           "pa_kv4_append", "pa_kv4_read", "pa_kv4_attn_prefill", "pa_kv4_attn_decode",
+           "pa_kv4_attn_verify", "pa_kv4_attn_decode_noalloc",
            "pa_qk_norm_rope", "pa_set_launch_events"]
 
 
@@ -69,6 +71,7 @@ _lib = None
 _torch = None  # the torch module, once a call needed it
 _attn = {}     # attention entry point of each launch kind
 _kv8_attn = {}  # and over the 8-bit cache
+_kv4_attn = {}  # and over the 4-bit cache
 _ROW_DTYPES = {}  # dtype codes of rows, once torch is there
 _P = C.c_void_p
 _I32P = C.POINTER(C.c_int32)
@@ -125,12 +128,14 @@ def lib():
     # decode without the workspace pair
     sig["pa_attn_decode_noalloc"] = (C.c_int, attn[1][:18] + attn[1][20:])
     rows = [_P, i64, _P, i64, _P, i32, _P, _P, i32, i32, _P, _P, _P, i32, i32, i32, i32, i32, _P]
-    sig["pa_kv8_append"] = sig["pa_kv8_read"] = (C.c_int, rows)
+    for name in ("pa_kv8_append", "pa_kv8_read", "pa_kv4_append", "pa_kv4_read"):
+        sig[name] = (C.c_int, rows)
     # the scales behind the caches, and no dtype
     kv8 = attn[1][:3] + [_P] + attn[1][3:15] + attn[1][16:]
-    for name in ("pa_kv8_attn_prefill", "pa_kv8_attn_decode", "pa_kv8_attn_verify"):
-        sig[name] = (C.c_int, kv8)
-    sig["pa_kv8_attn_decode_noalloc"] = (C.c_int, kv8[:18] + kv8[20:])
+    for bits in ("8", "4"):
+        for kind in ("prefill", "decode", "verify"):
+            sig[f"pa_kv{bits}_attn_{kind}"] = (C.c_int, kv8)
+        sig[f"pa_kv{bits}_attn_decode_noalloc"] = (C.c_int, kv8[:18] + kv8[20:])
     sig["pa_qk_norm_rope"] = (C.c_int, [_P, i64, _P, i64, _P, i32, _P, i32, i32, _P, _P, f32, i32,
                                         _P, _P, i32, i32, i32, i32, _P])
     sig["pa_set_launch_events"] = (C.c_int, [_P, _P])
@@ -142,6 +147,8 @@ def lib():
                   KIND_VERIFY: L.pa_attn_verify})
     _kv8_attn.update({KIND_PREFILL: L.pa_kv8_attn_prefill, KIND_DECODE: L.pa_kv8_attn_decode,
                       KIND_VERIFY: L.pa_kv8_attn_verify})
+    _kv4_attn.update({KIND_PREFILL: L.pa_kv4_attn_prefill, KIND_DECODE: L.pa_kv4_attn_decode,
+                      KIND_VERIFY: L.pa_kv4_attn_verify})
     _lib = L
     return L
 
@@ -613,7 +620,7 @@ def attention_decode_noalloc(q, k_cache, v_cache, block_table, seq_lens, cu_seql
         _stream(stream)))
 
 
-# -- the 8-bit cache -----------------------------------------------------------
+# -- the 8-bit and the 4-bit cache ---------------------------------------------
 def kv8_cache_shapes(num_blocks: int, num_kv_heads: int, head_dim: int, block_size: int = 16):
     """Shapes of an 8-bit cache's (k_cache, v_cache, scales); the caches are
     torch.float8_e4m3fn, the scales torch.uint8 (exponent + 127 of keys and of
@@ -621,6 +628,15 @@ def kv8_cache_shapes(num_blocks: int, num_kv_heads: int, head_dim: int, block_si
     no initialisation."""
     return ((num_blocks, num_kv_heads, head_dim // 64, block_size, 64),
             (num_blocks, num_kv_heads, head_dim, block_size), (num_blocks, num_kv_heads, 2))
+
+
+def kv4_cache_shapes(num_blocks: int, num_kv_heads: int, head_dim: int, block_size: int = 16):
+    """Shapes of a 4-bit cache's (k_cache, v_cache, scales), all torch.uint8: two e2m1
+    codes a byte; exponent + 127 for 32 dims of each token's key, and in the last row of
+    its value.  Contents need no initialisation."""
+    return ((num_blocks, num_kv_heads, block_size, head_dim // 2),
+            (num_blocks, num_kv_heads, head_dim // 32, 16, block_size),
+            (num_blocks, num_kv_heads, head_dim // 32 + 1, block_size))
 
 
 # The calls below check every tensor they take (types, shapes, strides, device): a
@@ -635,17 +651,29 @@ def _refuse(code: int, checks):
             raise PaError(code, msg)
 
 
-def _refuse_cache(t, k_cache, v_cache, scales):
-    nb, hkv, d, bs = v_cache.shape
+def _cache_form(t, bits: int, v_cache):
+    """(element type, blocks, kv-heads, head_dim, block size, shapes of k_cache, v_cache and
+    scales) of the 8- or 4-bit cache that v_cache is part of."""
+    if bits == 8:
+        nb, hkv, d, bs = v_cache.shape if v_cache.dim() == 4 else (0, 0, 0, 16)
+        return (t.float8_e4m3fn, nb, hkv, d, bs, (nb, hkv, d // 64, bs, 64), (nb, hkv, d, bs),
+                (nb, hkv, 2))
+    nb, hkv, c = v_cache.shape[:3] if v_cache.dim() == 5 else (0, 0, 0)
+    return (t.uint8, nb, hkv, 32 * c, 16, (nb, hkv, 16, 16 * c), (nb, hkv, c, 16, 16),
+            (nb, hkv, c + 1, 16))
+
+
+def _refuse_cache(t, bits, k_cache, v_cache, scales):
+    dt, _, _, _, _, ks, vs, ss = _cache_form(t, bits, v_cache)
     _refuse(PA_ERR_UNSUPPORTED, [(
-        k_cache.dtype == v_cache.dtype == t.float8_e4m3fn and scales.dtype == t.uint8,
-        f"8-bit cache of {k_cache.dtype}, {v_cache.dtype} and {scales.dtype} (supported: "
-        "float8_e4m3fn with uint8 scales)")])
+        k_cache.dtype == v_cache.dtype == dt and scales.dtype == t.uint8,
+        f"{bits}-bit cache of {k_cache.dtype}, {v_cache.dtype} and {scales.dtype} (supported: "
+        f"{str(dt)[6:]} with uint8 scales)")])
     _refuse(PA_ERR_ARG, [
-        (k_cache.shape == (nb, hkv, d // 64, bs, 64) and scales.shape == (nb, hkv, 2),
-         "8-bit cache: k_cache, v_cache and scales differ in shape"),
+        (k_cache.shape == ks and v_cache.shape == vs and scales.shape == ss,
+         f"{bits}-bit cache: k_cache, v_cache and scales differ in shape"),
         (k_cache.is_contiguous() and v_cache.is_contiguous() and scales.is_contiguous(),
-         "8-bit cache: tensors must be contiguous")])
+         f"{bits}-bit cache: tensors must be contiguous")])
 
 
 def _refuse_metadata(t, block_table, seq_lens, cu_seqlens):
@@ -686,18 +714,18 @@ def _packed(x, heads: int, d: int) -> bool:
     return s[2] == 1 and (s[1] == d or heads == 1) or x.numel() == 0
 
 
-def _kv8_rows(fn, k, v, block_table, seq_lens, cu_seqlens, k_cache, v_cache, scales, stream):
+def _quant_rows(fn, bits, k, v, block_table, seq_lens, cu_seqlens, k_cache, v_cache, scales, stream):
     t = _torch or _torch_module()
-    nb, hkv, d, bs = v_cache.shape
-    shape, dt, n, i32, e4m3 = k.shape, k.dtype, seq_lens.numel(), t.int32, t.float8_e4m3fn
+    cdt, nb, hkv, d, bs, k_shape, v_shape, s_shape = _cache_form(t, bits, v_cache)
+    shape, dt, n, i32 = k.shape, k.dtype, seq_lens.numel(), t.int32
     T, code = shape[0], _ROW_DTYPES.get(dt)
     rows, width = block_table.shape if block_table.dim() == 2 else (-1, 0)
     dev = v_cache.get_device()
     st = _stream_on(dev, stream)
     if not (shape == (T, hkv, d) and v.shape == shape and _packed(k, hkv, d)
             and _packed(v, hkv, d) and code is not None and v.dtype == dt
-            and k_cache.dtype == e4m3 and v_cache.dtype == e4m3 and scales.dtype == t.uint8
-            and k_cache.shape == (nb, hkv, d // 64, bs, 64) and scales.shape == (nb, hkv, 2)
+            and k_cache.dtype == cdt and v_cache.dtype == cdt and scales.dtype == t.uint8
+            and k_cache.shape == k_shape and v_cache.shape == v_shape and scales.shape == s_shape
             and k_cache.is_contiguous() and v_cache.is_contiguous() and scales.is_contiguous()
             and rows >= n and cu_seqlens.numel() > n
             and block_table.dtype == i32 and seq_lens.dtype == i32 and cu_seqlens.dtype == i32
@@ -706,7 +734,7 @@ def _kv8_rows(fn, k, v, block_table, seq_lens, cu_seqlens, k_cache, v_cache, sca
             and st >= 0 and k.get_device() == v.get_device() == k_cache.get_device()
             == scales.get_device() == block_table.get_device() == seq_lens.get_device()
             == cu_seqlens.get_device() == dev):
-        _refuse_cache(t, k_cache, v_cache, scales)
+        _refuse_cache(t, bits, k_cache, v_cache, scales)
         _refuse(PA_ERR_ARG, [
             (shape == (T, hkv, d) and v.shape == shape and _packed(k, hkv, d)
              and _packed(v, hkv, d),
@@ -730,32 +758,46 @@ def kv8_append(k_new, v_new, block_table, seq_lens, cu_seqlens, k_cache, v_cache
     """Quantise new K/V ([T, Hkv, D] device tensors, rows at any stride) into
     the 8-bit cache: rows cu_seqlens[r] .. cu_seqlens[r + 1] are sequence r's
     last positions."""
-    _kv8_rows((_lib or lib()).pa_kv8_append, k_new, v_new, block_table, seq_lens, cu_seqlens,
-              k_cache, v_cache, scales, stream)
+    _quant_rows((_lib or lib()).pa_kv8_append, 8, k_new, v_new, block_table, seq_lens, cu_seqlens,
+                k_cache, v_cache, scales, stream)
 
 
 def kv8_read(k_out, v_out, block_table, seq_lens, cu_seqlens, k_cache, v_cache, scales,
              stream=None):
     """Read tokens of the 8-bit cache into k_out and v_out ([T, Hkv, D]); rows
     as kv8_append's."""
-    _kv8_rows((_lib or lib()).pa_kv8_read, k_out, v_out, block_table, seq_lens, cu_seqlens,
-              k_cache, v_cache, scales, stream)
+    _quant_rows((_lib or lib()).pa_kv8_read, 8, k_out, v_out, block_table, seq_lens, cu_seqlens,
+                k_cache, v_cache, scales, stream)
 
 
-def _kv8_attn_args(q, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlens_q, plan_dev,
-                   info, out, lse, scale, stream, workspace):
-    """(arguments up to the plan info, stream) of a call over the 8-bit cache."""
+def kv4_append(k_new, v_new, block_table, seq_lens, cu_seqlens, k_cache, v_cache, scales,
+               stream=None):
+    """Quantise new K/V into the 4-bit cache; rows as kv8_append's."""
+    _quant_rows((_lib or lib()).pa_kv4_append, 4, k_new, v_new, block_table, seq_lens, cu_seqlens,
+                k_cache, v_cache, scales, stream)
+
+
+def kv4_read(k_out, v_out, block_table, seq_lens, cu_seqlens, k_cache, v_cache, scales,
+             stream=None):
+    """Read tokens of the 4-bit cache into k_out and v_out; rows as kv8_append's."""
+    _quant_rows((_lib or lib()).pa_kv4_read, 4, k_out, v_out, block_table, seq_lens, cu_seqlens,
+                k_cache, v_cache, scales, stream)
+
+
+def _quant_attn_args(bits, q, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlens_q, plan_dev,
+                     info, out, lse, scale, stream, workspace):
+    """(arguments up to the plan info, stream) of a call over the 8- or 4-bit cache."""
     t = _torch or _torch_module()
-    nb, hkv, d, bs = v_cache.shape
+    cdt, nb, hkv, d, bs, k_shape, v_shape, s_shape = _cache_form(t, bits, v_cache)
     total_q, hq, dq = q.shape
-    n, i32, e4m3 = seq_lens.numel(), t.int32, t.float8_e4m3fn
+    n, i32 = seq_lens.numel(), t.int32
     rows, width = block_table.shape if block_table.dim() == 2 else (-1, 0)
     dev = v_cache.get_device()
     st = _stream_on(dev, stream)
     if not (q.dtype == t.bfloat16 and out.dtype == t.bfloat16 and dq == d
             and out.shape == q.shape and q.is_contiguous() and out.is_contiguous()
-            and k_cache.dtype == e4m3 and v_cache.dtype == e4m3 and scales.dtype == t.uint8
-            and k_cache.shape == (nb, hkv, d // 64, bs, 64) and scales.shape == (nb, hkv, 2)
+            and k_cache.dtype == cdt and v_cache.dtype == cdt and scales.dtype == t.uint8
+            and k_cache.shape == k_shape and v_cache.shape == v_shape and scales.shape == s_shape
             and k_cache.is_contiguous() and v_cache.is_contiguous() and scales.is_contiguous()
             and rows >= n and cu_seqlens_q.numel() > n
             and block_table.dtype == i32 and seq_lens.dtype == i32 and cu_seqlens_q.dtype == i32
@@ -771,7 +813,7 @@ def _kv8_attn_args(q, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlen
             and st >= 0 and q.get_device() == out.get_device() == k_cache.get_device()
             == scales.get_device() == block_table.get_device() == seq_lens.get_device()
             == cu_seqlens_q.get_device() == dev):
-        _refuse_cache(t, k_cache, v_cache, scales)
+        _refuse_cache(t, bits, k_cache, v_cache, scales)
         _refuse(PA_ERR_UNSUPPORTED, [
             (q.dtype == out.dtype == t.bfloat16,
              f"queries {q.dtype}, output {out.dtype} (supported: bfloat16)")])
@@ -799,8 +841,8 @@ def kv8_attention(kind: int, q, k_cache, v_cache, scales, block_table, seq_lens,
     ``kind``), with a plan built for PA_BF16_KV8."""
     if _lib is None:
         lib()
-    args, st = _kv8_attn_args(q, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlens_q,
-                              plan_dev, info, out, lse, scale, stream, workspace)
+    args, st = _quant_attn_args(8, q, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlens_q,
+                                plan_dev, info, out, lse, scale, stream, workspace)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     rc = _kv8_attn[kind](*args, _dptr(workspace), ws_bytes, out.data_ptr(), _dptr(lse), st)
     if rc:
@@ -812,8 +854,32 @@ def kv8_attention_decode_noalloc(q, k_cache, v_cache, scales, block_table, seq_l
     """Decode over the 8-bit cache with the split-K partials in the library's
     per-device array (as attention_decode_noalloc)."""
     fn = (_lib or lib()).pa_kv8_attn_decode_noalloc
-    args, st = _kv8_attn_args(q, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlens_q,
-                              plan_dev, info, out, lse, scale, stream, None)
+    args, st = _quant_attn_args(8, q, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlens_q,
+                                plan_dev, info, out, lse, scale, stream, None)
+    _check(fn(*args, out.data_ptr(), _dptr(lse), st))
+
+
+def kv4_attention(kind: int, q, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlens_q,
+                  plan_dev, info: PlanInfo, workspace, out, lse=None, scale=None, stream=None):
+    """Paged attention over the 4-bit cache (prefill / decode / verify by
+    ``kind``), with a plan built for PA_BF16_KV4."""
+    if _lib is None:
+        lib()
+    args, st = _quant_attn_args(4, q, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlens_q,
+                                plan_dev, info, out, lse, scale, stream, workspace)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    rc = _kv4_attn[kind](*args, _dptr(workspace), ws_bytes, out.data_ptr(), _dptr(lse), st)
+    if rc:
+        _check(rc)
+
+
+def kv4_attention_decode_noalloc(q, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlens_q,
+                                 plan_dev, info: PlanInfo, out, lse=None, scale=None, stream=None):
+    """Decode over the 4-bit cache with the split-K partials in the library's
+    per-device array (as attention_decode_noalloc)."""
+    fn = (_lib or lib()).pa_kv4_attn_decode_noalloc
+    args, st = _quant_attn_args(4, q, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlens_q,
+                                plan_dev, info, out, lse, scale, stream, None)
     _check(fn(*args, out.data_ptr(), _dptr(lse), st))
 
 

@@ -11,7 +11,7 @@
 namespace pa {
 namespace dev {
 int launch_attn_bf16(const void* q, const void* kc, const void* vc, const uint8_t* scales,
-                     int32_t num_blocks, const int32_t* bt, int32_t max_blocks, const int32_t* seq_lens,
+                     int32_t bits, int32_t num_blocks, const int32_t* bt, int32_t max_blocks, const int32_t* seq_lens,
                      const int32_t* cu_q, int32_t hq, int32_t hkv, int32_t d, float scale,
                      const int32_t* plan, int32_t grid, int32_t n_tile, int32_t n_merge,
                      int32_t merge_narrow, bool wide_rows, bool tail, int64_t partial_rows, void* ws, void* out,
@@ -30,6 +30,16 @@ int launch_kv8_append(const void* kn, int64_t k_stride, const void* vn, int64_t 
                       uint8_t* scales, int32_t nb, int32_t hkv, int32_t d, int32_t dtype,
                       hipStream_t stream);
 int launch_kv8_read(void* k_out, int64_t k_stride, void* v_out, int64_t v_stride,
+                    const int32_t* bt, int32_t max_blocks, const int32_t* seq_lens,
+                    const int32_t* cu, int32_t n_seqs, int32_t n, const void* kc, const void* vc,
+                    const uint8_t* scales, int32_t nb, int32_t hkv, int32_t d, int32_t dtype,
+                    hipStream_t stream);
+int launch_kv4_append(const void* kn, int64_t k_stride, const void* vn, int64_t v_stride,
+                      const int32_t* bt, int32_t max_blocks, const int32_t* seq_lens,
+                      const int32_t* cu, int32_t n_seqs, int32_t n, void* kc, void* vc,
+                      uint8_t* scales, int32_t nb, int32_t hkv, int32_t d, int32_t dtype,
+                      hipStream_t stream);
+int launch_kv4_read(void* k_out, int64_t k_stride, void* v_out, int64_t v_stride,
                     const int32_t* bt, int32_t max_blocks, const int32_t* seq_lens,
                     const int32_t* cu, int32_t n_seqs, int32_t n, const void* kc, const void* vc,
                     const uint8_t* scales, int32_t nb, int32_t hkv, int32_t d, int32_t dtype,
@@ -69,14 +79,14 @@ bool aligned16(const void* p, int64_t stride, int32_t dtype) {
   return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && stride * (dtype == PA_BF16 ? 2 : 4) % 16 == 0;
 }
 
-// Checks shared by the two calls that move rows between memory and the 8-bit cache.
+// Checks shared by the calls that move rows between memory and the 8- or 4-bit cache.
 // *work: whether there is anything to do.
-int check_kv8_rows(const char* fn, const void* k_rows, int64_t k_stride, const void* v_rows,
+int check_quant_rows(const char* fn, const void* k_rows, int64_t k_stride, const void* v_rows,
                    int64_t v_stride, const int32_t* block_table, int32_t max_blocks_per_seq,
                    const int32_t* seq_lens, const int32_t* cu_seqlens, int32_t n_seqs,
                    int32_t n_tokens, const void* k_cache, const void* v_cache, const void* scales,
                    int32_t num_blocks, int32_t num_kv_heads, int32_t head_dim, int32_t block_size,
-                   int32_t dtype, bool* work) {
+                   int32_t dtype, uintptr_t scale_align, bool* work) {
   const int rc = check_shape(fn, num_blocks, num_kv_heads, head_dim, block_size, dtype);
   if (rc) return rc;
   if (n_seqs < 0 || n_tokens < 0 || max_blocks_per_seq < 1)
@@ -91,8 +101,9 @@ int check_kv8_rows(const char* fn, const void* k_rows, int64_t k_stride, const v
                 (long long)k_stride, (long long)v_stride, (long long)row);
   if (!aligned16(k_rows, k_stride, dtype) || !aligned16(v_rows, v_stride, dtype) ||
       !aligned16(k_cache, 0, dtype) || !aligned16(v_cache, 0, dtype) ||
-      (reinterpret_cast<uintptr_t>(scales) & 3))
-    return fail(PA_ERR_ARG, "%s: rows and caches must be 16-byte aligned, scales 4-byte", fn);
+      (reinterpret_cast<uintptr_t>(scales) & (scale_align - 1)))
+    return fail(PA_ERR_ARG, "%s: rows and caches must be 16-byte aligned, scales %d-byte", fn,
+                int(scale_align));
   return PA_OK;
 }
 
@@ -133,11 +144,12 @@ int attn_common(const char* fn, int32_t want_kind, const void* q, const void* k_
                 int32_t head_dim, int32_t block_size, float scale, int32_t dtype,
                 const int32_t* plan, const pa_plan_info* info, void* workspace,
                 size_t workspace_bytes, void* out, float* lse, void* stream,
-                bool noalloc = false, bool kv8 = false, const uint8_t* scales = nullptr) {
+                bool noalloc = false, int32_t bits = 16, const uint8_t* scales = nullptr) {
   clear_error();
+  const bool quant = bits < 16;  // of a cached value
   const hipEvent_t ev_start = t_ev_start, ev_stop = t_ev_stop;
   t_ev_start = t_ev_stop = nullptr;
-  int rc = check_shape(fn, num_blocks, num_kv_heads, head_dim, block_size, kv8 ? PA_BF16 : dtype);
+  int rc = check_shape(fn, num_blocks, num_kv_heads, head_dim, block_size, quant ? PA_BF16 : dtype);
   if (rc) return rc;
   if (num_q_heads <= 0 || num_q_heads % num_kv_heads)
     return fail(PA_ERR_ARG, "%s: num_q_heads %d must be a positive multiple of num_kv_heads %d",
@@ -171,12 +183,13 @@ int attn_common(const char* fn, int32_t want_kind, const void* q, const void* k_
     return PA_OK;
   }
   if (!q || !k_cache || !v_cache || !block_table || !seq_lens || !cu_seqlens_q || !out ||
-      (kv8 && !scales))
+      (quant && !scales))
     return fail(PA_ERR_ARG, "%s: NULL device pointer", fn);
-  if (kv8 && (((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k_cache) |
+  if (quant && (((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k_cache) |
                 reinterpret_cast<uintptr_t>(v_cache) | reinterpret_cast<uintptr_t>(out)) & 15) ||
-              (reinterpret_cast<uintptr_t>(scales) & 3)))
-    return fail(PA_ERR_ARG, "%s: q, out and caches must be 16-byte aligned, scales 4-byte", fn);
+              (reinterpret_cast<uintptr_t>(scales) & (bits == 4 ? 15 : 3))))
+    return fail(PA_ERR_ARG, "%s: q, out and caches must be 16-byte aligned, scales %d-byte", fn,
+                bits == 4 ? 16 : 4);
   if (dtype == PA_F32) {
     rc = dev::launch_attn_f32(q, k_cache, v_cache, num_blocks, block_table, max_blocks_per_seq,
                               seq_lens, cu_seqlens_q, n_seqs, total_q, num_q_heads, num_kv_heads,
@@ -204,7 +217,7 @@ int attn_common(const char* fn, int32_t want_kind, const void* q, const void* k_
                     "%zu bytes this call holds per device; call %s with a "
                     "workspace of that size", fn, (long long)info->workspace_bytes,
                     (size_t)PA_NOALLOC_WORKSPACE_BYTES,
-                    kv8 ? "pa_kv8_attn_decode" : "pa_attn_decode");
+                    bits == 8 ? "pa_kv8_attn_decode" : bits == 4 ? "pa_kv4_attn_decode" : "pa_attn_decode");
       workspace = nullptr;
       workspace_bytes = 0;
       if (info->workspace_bytes > 0) {
@@ -218,7 +231,7 @@ int attn_common(const char* fn, int32_t want_kind, const void* q, const void* k_
       return fail(PA_ERR_ARG, "%s: workspace of %zu bytes, plan needs %lld", fn, workspace_bytes,
                   (long long)info->workspace_bytes);
     const int64_t partial_rows = info->partial_rows;
-    rc = dev::launch_attn_bf16(q, k_cache, v_cache, scales, num_blocks, block_table, max_blocks_per_seq,
+    rc = dev::launch_attn_bf16(q, k_cache, v_cache, scales, bits, num_blocks, block_table, max_blocks_per_seq,
                                seq_lens, cu_seqlens_q, num_q_heads, num_kv_heads, head_dim, scale,
                                plan, info->grid, info->n_shared_items + info->n_tile_items,
                                n_merge,
@@ -303,10 +316,10 @@ int pa_kv8_append(const void* k_new, int64_t k_stride, const void* v_new, int64_
                   int32_t head_dim, int32_t block_size, int32_t dtype, void* stream) {
   pa::clear_error();
   bool work = false;
-  int rc = pa::check_kv8_rows("pa_kv8_append", k_new, k_stride, v_new, v_stride, block_table,
+  int rc = pa::check_quant_rows("pa_kv8_append", k_new, k_stride, v_new, v_stride, block_table,
                               max_blocks_per_seq, seq_lens, cu_seqlens, n_seqs, n_tokens, k_cache,
                               v_cache, scales, num_blocks, num_kv_heads, head_dim, block_size,
-                              dtype, &work);
+                              dtype, 4, &work);
   if (rc || !work) return rc;
   rc = pa::dev::launch_kv8_append(k_new, k_stride, v_new, v_stride, block_table,
                                   max_blocks_per_seq, seq_lens, cu_seqlens, n_seqs, n_tokens,
@@ -326,10 +339,10 @@ int pa_kv8_read(void* k_out, int64_t k_stride, void* v_out, int64_t v_stride,
                 void* stream) {
   pa::clear_error();
   bool work = false;
-  int rc = pa::check_kv8_rows("pa_kv8_read", k_out, k_stride, v_out, v_stride, block_table,
+  int rc = pa::check_quant_rows("pa_kv8_read", k_out, k_stride, v_out, v_stride, block_table,
                               max_blocks_per_seq, seq_lens, cu_seqlens, n_seqs, n_tokens, k_cache,
                               v_cache, scales, num_blocks, num_kv_heads, head_dim, block_size,
-                              dtype, &work);
+                              dtype, 4, &work);
   if (rc || !work) return rc;
   rc = pa::dev::launch_kv8_read(k_out, k_stride, v_out, v_stride, block_table, max_blocks_per_seq,
                                 seq_lens, cu_seqlens, n_seqs, n_tokens, k_cache, v_cache, scales,
@@ -337,6 +350,51 @@ int pa_kv8_read(void* k_out, int64_t k_stride, void* v_out, int64_t v_stride,
                                 static_cast<hipStream_t>(stream));
   if (rc)
     return pa::fail(PA_ERR_LAUNCH, "pa_kv8_read: %s",
+                    hipGetErrorString(static_cast<hipError_t>(rc)));
+  return PA_OK;
+}
+
+int pa_kv4_append(const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+                  const int32_t* block_table, int32_t max_blocks_per_seq, const int32_t* seq_lens,
+                  const int32_t* cu_seqlens, int32_t n_seqs, int32_t n_tokens, void* k_cache,
+                  void* v_cache, uint8_t* scales, int32_t num_blocks, int32_t num_kv_heads,
+                  int32_t head_dim, int32_t block_size, int32_t dtype, void* stream) {
+  pa::clear_error();
+  bool work = false;
+  int rc = pa::check_quant_rows("pa_kv4_append", k_new, k_stride, v_new, v_stride, block_table,
+                              max_blocks_per_seq, seq_lens, cu_seqlens, n_seqs, n_tokens, k_cache,
+                              v_cache, scales, num_blocks, num_kv_heads, head_dim, block_size,
+                              dtype, 16, &work);
+  if (rc || !work) return rc;
+  rc = pa::dev::launch_kv4_append(k_new, k_stride, v_new, v_stride, block_table,
+                                  max_blocks_per_seq, seq_lens, cu_seqlens, n_seqs, n_tokens,
+                                  k_cache, v_cache, scales, num_blocks, num_kv_heads, head_dim,
+                                  dtype, static_cast<hipStream_t>(stream));
+  if (rc)
+    return pa::fail(PA_ERR_LAUNCH, "pa_kv4_append: %s",
+                    hipGetErrorString(static_cast<hipError_t>(rc)));
+  return PA_OK;
+}
+
+int pa_kv4_read(void* k_out, int64_t k_stride, void* v_out, int64_t v_stride,
+                const int32_t* block_table, int32_t max_blocks_per_seq, const int32_t* seq_lens,
+                const int32_t* cu_seqlens, int32_t n_seqs, int32_t n_tokens, const void* k_cache,
+                const void* v_cache, const uint8_t* scales, int32_t num_blocks,
+                int32_t num_kv_heads, int32_t head_dim, int32_t block_size, int32_t dtype,
+                void* stream) {
+  pa::clear_error();
+  bool work = false;
+  int rc = pa::check_quant_rows("pa_kv4_read", k_out, k_stride, v_out, v_stride, block_table,
+                              max_blocks_per_seq, seq_lens, cu_seqlens, n_seqs, n_tokens, k_cache,
+                              v_cache, scales, num_blocks, num_kv_heads, head_dim, block_size,
+                              dtype, 16, &work);
+  if (rc || !work) return rc;
+  rc = pa::dev::launch_kv4_read(k_out, k_stride, v_out, v_stride, block_table, max_blocks_per_seq,
+                                seq_lens, cu_seqlens, n_seqs, n_tokens, k_cache, v_cache, scales,
+                                num_blocks, num_kv_heads, head_dim, dtype,
+                                static_cast<hipStream_t>(stream));
+  if (rc)
+    return pa::fail(PA_ERR_LAUNCH, "pa_kv4_read: %s",
                     hipGetErrorString(static_cast<hipError_t>(rc)));
   return PA_OK;
 }
@@ -422,35 +480,54 @@ int pa_attn_decode_noalloc(const void* q, const void* k_cache, const void* v_cac
                          dtype, plan, info, nullptr, 0, out, lse, stream, /*noalloc=*/true);
 }
 
-#define PA_KV8_ATTN_ARGS                                                                        \
+#define PA_QUANT_ATTN_ARGS                                                                      \
   const void *q, const void *k_cache, const void *v_cache, const uint8_t *scales,               \
       int32_t num_blocks, const int32_t *block_table, int32_t max_blocks_per_seq,               \
       const int32_t *seq_lens, const int32_t *cu_seqlens_q, int32_t n_seqs, int32_t total_q,    \
       int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t block_size,          \
       float scale, int32_t *plan, const pa_plan_info *info
-#define PA_KV8_ATTN_PASS                                                                        \
+#define PA_QUANT_ATTN_PASS(dtype)                                                               \
   q, k_cache, v_cache, num_blocks, block_table, max_blocks_per_seq, seq_lens, cu_seqlens_q,     \
-      n_seqs, total_q, num_q_heads, num_kv_heads, head_dim, block_size, scale, PA_BF16_KV8, plan, \
-      info
+      n_seqs, total_q, num_q_heads, num_kv_heads, head_dim, block_size, scale, dtype, plan, info
 
-int pa_kv8_attn_prefill(PA_KV8_ATTN_ARGS, void* workspace, size_t workspace_bytes, void* out,
+int pa_kv8_attn_prefill(PA_QUANT_ATTN_ARGS, void* workspace, size_t workspace_bytes, void* out,
                         float* lse, void* stream) {
-  return pa::attn_common("pa_kv8_attn_prefill", PA_KIND_PREFILL, PA_KV8_ATTN_PASS, workspace,
-                         workspace_bytes, out, lse, stream, false, true, scales);
+  return pa::attn_common("pa_kv8_attn_prefill", PA_KIND_PREFILL, PA_QUANT_ATTN_PASS(PA_BF16_KV8), workspace,
+                         workspace_bytes, out, lse, stream, false, 8, scales);
 }
-int pa_kv8_attn_decode(PA_KV8_ATTN_ARGS, void* workspace, size_t workspace_bytes, void* out,
+int pa_kv8_attn_decode(PA_QUANT_ATTN_ARGS, void* workspace, size_t workspace_bytes, void* out,
                        float* lse, void* stream) {
-  return pa::attn_common("pa_kv8_attn_decode", PA_KIND_DECODE, PA_KV8_ATTN_PASS, workspace,
-                         workspace_bytes, out, lse, stream, false, true, scales);
+  return pa::attn_common("pa_kv8_attn_decode", PA_KIND_DECODE, PA_QUANT_ATTN_PASS(PA_BF16_KV8), workspace,
+                         workspace_bytes, out, lse, stream, false, 8, scales);
 }
-int pa_kv8_attn_verify(PA_KV8_ATTN_ARGS, void* workspace, size_t workspace_bytes, void* out,
+int pa_kv8_attn_verify(PA_QUANT_ATTN_ARGS, void* workspace, size_t workspace_bytes, void* out,
                        float* lse, void* stream) {
-  return pa::attn_common("pa_kv8_attn_verify", PA_KIND_VERIFY, PA_KV8_ATTN_PASS, workspace,
-                         workspace_bytes, out, lse, stream, false, true, scales);
+  return pa::attn_common("pa_kv8_attn_verify", PA_KIND_VERIFY, PA_QUANT_ATTN_PASS(PA_BF16_KV8), workspace,
+                         workspace_bytes, out, lse, stream, false, 8, scales);
 }
-int pa_kv8_attn_decode_noalloc(PA_KV8_ATTN_ARGS, void* out, float* lse, void* stream) {
-  return pa::attn_common("pa_kv8_attn_decode_noalloc", PA_KIND_DECODE, PA_KV8_ATTN_PASS, nullptr, 0,
-                         out, lse, stream, /*noalloc=*/true, true, scales);
+int pa_kv8_attn_decode_noalloc(PA_QUANT_ATTN_ARGS, void* out, float* lse, void* stream) {
+  return pa::attn_common("pa_kv8_attn_decode_noalloc", PA_KIND_DECODE, PA_QUANT_ATTN_PASS(PA_BF16_KV8), nullptr, 0,
+                         out, lse, stream, /*noalloc=*/true, 8, scales);
+}
+
+int pa_kv4_attn_prefill(PA_QUANT_ATTN_ARGS, void* workspace, size_t workspace_bytes, void* out,
+                        float* lse, void* stream) {
+  return pa::attn_common("pa_kv4_attn_prefill", PA_KIND_PREFILL, PA_QUANT_ATTN_PASS(PA_BF16_KV4), workspace,
+                         workspace_bytes, out, lse, stream, false, 4, scales);
+}
+int pa_kv4_attn_decode(PA_QUANT_ATTN_ARGS, void* workspace, size_t workspace_bytes, void* out,
+                       float* lse, void* stream) {
+  return pa::attn_common("pa_kv4_attn_decode", PA_KIND_DECODE, PA_QUANT_ATTN_PASS(PA_BF16_KV4), workspace,
+                         workspace_bytes, out, lse, stream, false, 4, scales);
+}
+int pa_kv4_attn_verify(PA_QUANT_ATTN_ARGS, void* workspace, size_t workspace_bytes, void* out,
+                       float* lse, void* stream) {
+  return pa::attn_common("pa_kv4_attn_verify", PA_KIND_VERIFY, PA_QUANT_ATTN_PASS(PA_BF16_KV4), workspace,
+                         workspace_bytes, out, lse, stream, false, 4, scales);
+}
+int pa_kv4_attn_decode_noalloc(PA_QUANT_ATTN_ARGS, void* out, float* lse, void* stream) {
+  return pa::attn_common("pa_kv4_attn_decode_noalloc", PA_KIND_DECODE, PA_QUANT_ATTN_PASS(PA_BF16_KV4), nullptr, 0,
+                         out, lse, stream, /*noalloc=*/true, 4, scales);
 }
 
 int pa_set_launch_events(void* start_event, void* stop_event) {

@@ -364,7 +364,7 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
     return pa::fail(PA_ERR_UNSUPPORTED, "pa_attn_plan: head_dim %d (supported: 64, 128)", head_dim);
   if (block_size != 16)
     return pa::fail(PA_ERR_UNSUPPORTED, "pa_attn_plan: block_size %d (supported: 16)", block_size);
-  if (dtype != PA_F32 && dtype != PA_BF16 && dtype != PA_BF16_KV8)
+  if (dtype != PA_F32 && dtype != PA_BF16 && dtype != PA_BF16_KV8 && dtype != PA_BF16_KV4)
     return pa::fail(PA_ERR_UNSUPPORTED, "pa_attn_plan: dtype %d", dtype);
   if (block_table && max_blocks_per_seq < 1)
     return pa::fail(PA_ERR_ARG, "pa_attn_plan: max_blocks_per_seq %d < 1", max_blocks_per_seq);
@@ -417,8 +417,9 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
     // row item per key range when it holds all their rows (at most 32), else
     // on tile items, whose four wavefronts share each key tile through LDS.
     auto is_row = [&](int32_t r) { return qlen(r) > 0 && qlen(r) * G <= pa::kRowSeqRows; };
-    // Over the 8-bit cache those run as two row items that read the same keys.
-    const bool kv8 = dtype == PA_BF16_KV8;
+    // Over the 8-bit cache, and the 4-bit one, those run as two row items that read the
+    // same keys.
+    const bool kv8 = dtype == PA_BF16_KV8 || dtype == PA_BF16_KV4;
     bool few_tiles = !kv8;
     auto on_tiles = [&](int32_t r) { return few_tiles && qlen(r) * G > pa::kRowItemRows; };
     auto row_pieces = [&](int32_t r) { return cdiv(qlen(r) * G, pa::kRowItemRows); };

@@ -65,7 +65,7 @@ def plan_words_bound(cfg, n_seqs: int, total_q: int, max_blocks_per_seq: int,
     total_q query tokens (tile items, key-split items of at least 256 keys,
     merge groups, cascade member tables, per-XCD padding; in a small launch
     the key-split tiles and shared-prefix chunks that fill the chip; with
-    ``kv8`` the plan may be one over the 8-bit cache: two row items per
+    ``kv8`` the plan may be one over the 8- or 4-bit cache: two row items per
     sequence of four records each)."""
     max_keys = max_blocks_per_seq * cfg.block_size
     few = kv8 * 8 * (total_q * cfg.group // 4 + n_seqs * (2 * (max_keys // 128 + 4) + 1))
@@ -123,24 +123,32 @@ class Staging:
 
 class DeviceReplay:
     def __init__(self, wl, device: str = "cuda", kind: str | None = None, num_cus: int = 0,
-                 cascade: bool = True, stage_kernel: bool = True, kv8: bool = False):
+                 cascade: bool = True, stage_kernel: bool = True, kv8: bool = False,
+                 kv4: bool = False):
         cfg = wl.cfg
         self.wl, self.cfg, self.device = wl, cfg, torch.device(device)
         self.tdtype = torch_dtype(cfg.dtype)
         self.dcode = B.PA_BF16 if cfg.dtype == "bf16" else B.PA_F32
-        self.kv8 = kv8  # an 8-bit cache (bf16 queries)
+        # an 8-bit or a 4-bit cache (bf16 queries)
+        if kv8 and kv4:
+            raise ValueError("one cache: of 8 or of 4 bits")
+        self.kv8, self.kv4 = kv8, kv4
         self.pool = B.Pool(wl.num_blocks, cfg.block_size, wl.free_order, evict=wl.evict)
         # keys in the grouped layout [block][head][dim / 32][slot position][32]
         shape_k = (wl.num_blocks, cfg.num_kv_heads, cfg.head_dim // 32, cfg.block_size, 32)
         shape_v = (wl.num_blocks, cfg.num_kv_heads, cfg.head_dim, cfg.block_size)
         # Uninitialised on purpose: the kernels must never read unwritten slots.
         cdtype = self.tdtype
-        if kv8:
+        self._append, self._attention = B.kv_append, B.attention
+        if kv8 or kv4:
             if cfg.dtype != "bf16":
-                raise ValueError("an 8-bit cache takes bf16 queries")
-            self.dcode, cdtype = B.PA_BF16_KV8, torch.float8_e4m3fn
-            shape_k, shape_v, shape_s = B.kv8_cache_shapes(wl.num_blocks, cfg.num_kv_heads,
-                                                           cfg.head_dim, cfg.block_size)
+                raise ValueError(f"{'an 8' if kv8 else 'a 4'}-bit cache takes bf16 queries")
+            self.dcode, cdtype, shapes, self._append, self._attention = (
+                (B.PA_BF16_KV8, torch.float8_e4m3fn, B.kv8_cache_shapes, B.kv8_append,
+                 B.kv8_attention) if kv8 else
+                (B.PA_BF16_KV4, torch.uint8, B.kv4_cache_shapes, B.kv4_append, B.kv4_attention))
+            shape_k, shape_v, shape_s = shapes(wl.num_blocks, cfg.num_kv_heads, cfg.head_dim,
+                                               cfg.block_size)
             self.scales = torch.empty(shape_s, dtype=torch.uint8, device=self.device)
         self.k_cache = torch.empty(shape_k, dtype=cdtype, device=self.device)
         self.v_cache = torch.empty(shape_v, dtype=cdtype, device=self.device)
@@ -159,12 +167,12 @@ class DeviceReplay:
         slots = torch.from_numpy(md["slot_mapping"]).to(dev)
         kt = torch.from_numpy(k).to(dev, self.tdtype)
         vt = torch.from_numpy(v).to(dev, self.tdtype)
-        if self.kv8:
+        if self.kv8 or self.kv4:
             bt, sl, cu = (torch.from_numpy(md[k]).to(dev)
                           for k in ("block_table", "seq_lens", "cu_seqlens_q"))
-            B.kv8_append(kt, vt, bt, sl, cu, self.k_cache, self.v_cache, self.scales)
+            self._append(kt, vt, bt, sl, cu, self.k_cache, self.v_cache, self.scales)
         else:
-            B.kv_append(kt, vt, slots, self.k_cache, self.v_cache)
+            self._append(kt, vt, slots, self.k_cache, self.v_cache)
 
     def apply(self, op):
         p = self.pool
@@ -304,11 +312,11 @@ class DeviceReplay:
         """KV append of the launch; records the caller's staging guard after
         it unless record_guard is False (the guard is then the start event the
         caller hands to ``attend``)."""
-        if self.kv8:
-            B.kv8_append(p.k_new, p.v_new, p.block_table, p.seq_lens, p.cu, self.k_cache,
+        if self.kv8 or self.kv4:
+            self._append(p.k_new, p.v_new, p.block_table, p.seq_lens, p.cu, self.k_cache,
                          self.v_cache, self.scales, stream)
         else:
-            B.kv_append(p.k_new, p.v_new, p.slots, self.k_cache, self.v_cache, stream)
+            self._append(p.k_new, p.v_new, p.slots, self.k_cache, self.v_cache, stream)
         guard = getattr(p, "guard", None)
         if guard is not None and record_guard:
             guard.record(stream)
@@ -318,13 +326,9 @@ class DeviceReplay:
         last kernel dispatches (pa_set_launch_events)."""
         if events is not None:
             B.set_launch_events(*events)
-        if self.kv8:
-            B.kv8_attention(KIND[p.kind], p.q, self.k_cache, self.v_cache, self.scales,
-                            p.block_table, p.seq_lens, p.cu, p.plan, p.info, p.ws, p.out, p.lse,
-                            stream=stream)
-            return
-        B.attention(KIND[p.kind], p.q, self.k_cache, self.v_cache, p.block_table, p.seq_lens, p.cu,
-                    p.plan, p.info, p.ws, p.out, p.lse, stream=stream)
+        cache = (self.k_cache, self.v_cache) + ((self.scales,) if self.kv8 or self.kv4 else ())
+        self._attention(KIND[p.kind], p.q, *cache, p.block_table, p.seq_lens, p.cu, p.plan, p.info,
+                        p.ws, p.out, p.lse, stream=stream)
 
     def run(self, launch) -> Prepared:
         p = self.prepare(launch)
