@@ -119,6 +119,20 @@ int pa_seq_extend(pa_pool* pool, int64_t seq_id, const int32_t* tokens, int32_t 
  * Errors: PA_ERR_UNKNOWN_SEQ, PA_ERR_ARG. */
 int pa_seq_truncate(pa_pool* pool, int64_t seq_id, int32_t new_len);
 
+/* The pool's side of pa_kv_evict: sequence seq_id holds new_len tokens from now on, of
+ * which the first `first` are the ones that it had.  in_place = 0: the first / block_size
+ * leading blocks stay, the others are replaced by blocks from the front of the free list
+ * (the new table of pa_kv_evict; block tables taken before are the old one) and released
+ * as by pa_seq_free, without being cached: cached ones stay resident for other requests.
+ * in_place = 1: the sequence keeps its first ceil(new_len / block_size) blocks, whose
+ * contents from `first` on change (so that `first` must be at least the number of tokens in
+ * its leading cached blocks); the others return to the front of the free list.  What the
+ * blocks hold is not a prefix of its tokens any more: none of them is cached when the
+ * sequence is freed.  Tokens appended later continue at position new_len of the cache (their
+ * rotation goes by the caller's own count).  1 <= new_len <= length, 0 <= first <= new_len.
+ * Errors (pool unchanged): PA_ERR_UNKNOWN_SEQ, PA_ERR_ARG, PA_ERR_NO_BLOCKS. */
+int pa_seq_compact(pa_pool* pool, int64_t seq_id, int32_t new_len, int32_t first, int32_t in_place);
+
 /* Release a finished sequence.  Its full blocks are cached first (same rule as
  * at admission); cached blocks stay resident with no owner (idle) until
  * evicted; uncached blocks return to the back of the free list.
@@ -669,6 +683,70 @@ int pa_kv4_attn_decode_noalloc(const void* q, const void* k_cache, const void* v
                                int32_t num_kv_heads, int32_t head_dim, int32_t block_size,
                                float scale, int32_t* plan, const pa_plan_info* info, void* out,
                                float* lse, void* stream);
+
+/* ------------------------------------------------------------------------ *
+ * Eviction from live contexts by accumulated attention weight (paper:        *
+ * Section 2 and Table "playbook", KV memory bounds the requests a GPU holds; *
+ * Section 3, long inputs that short structured outputs are drawn from).      *
+ * ------------------------------------------------------------------------ */
+
+/* The attention weight that each cached key got from a launch's queries:
+ *   weights[r][h][t] = sum over the rows i of sequence r and the query heads g of kv-head h
+ *                      that see key t of exp(scale * q_ig . k_t - lse_ig)
+ * for t of [0, seq_lens[r]), added to what is there with accumulate = 1, written in its
+ * place with 0.  q, the caches' layout and the metadata are those of the attention call
+ * (before or after it; the keys of the launch's own tokens appended), lse its output
+ * [total_q][num_q_heads].  A row whose log-sum-exp is not finite counts for nothing; the
+ * weight of a key that is not finite may be NaN.  weights: [n_seqs][num_kv_heads]
+ * [weights_stride] float32; keys at or past weights_stride, sequences without rows and what
+ * lies behind a sequence's keys are left alone.  dtype: PA_BF16, with scales NULL, or
+ * PA_BF16_KV4, k_cache and scales of a 4-bit cache.  Products of bf16 numbers, exponentials
+ * and sums are float32, the sums in one order: equal calls give equal bits.  All pointers
+ * are caller-owned device memory; asynchronous on stream; allocates nothing.  Errors:
+ * PA_ERR_ARG (NULL pointer with work to do, sizes, scale, accumulate, q or cache not
+ * 16-byte, lse or weights not 4-byte aligned), PA_ERR_UNSUPPORTED (head_dim, block_size,
+ * dtype), PA_ERR_LAUNCH. */
+int pa_attn_weights(const void* q, const float* lse, const void* k_cache, const uint8_t* scales,
+                    int32_t num_blocks, const int32_t* block_table, int32_t max_blocks_per_seq,
+                    const int32_t* seq_lens, const int32_t* cu_seqlens_q, int32_t n_seqs,
+                    int32_t total_q, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                    int32_t block_size, float scale, int32_t dtype, float* weights,
+                    int64_t weights_stride, int32_t accumulate, void* stream);
+
+/* Shorten sequences to the tokens that matter.  Of sequence r's L = seq_lens[r] tokens,
+ * B = min(new_lens[r], L) stay, for each kv-head its own: the first F = min(first[r], B)
+ * (first NULL: none), the last W = min(window, B - F), and of the others the B - F - W of the
+ * largest weights[r][h][t] (NaN counts as larger than any number; of equal weights the
+ * earlier token's).  They keep their order: kept[r][h][i] is the old position of what is
+ * then at position i, its key and value move there (keys carry their rotation with them),
+ * and weights_out[r][h][i] receives its weight.  weights and weights_out are
+ * [n_seqs][num_kv_heads][weights_stride], the same array or two that do not overlap; kept
+ * is [n_seqs][num_kv_heads][kept_stride].  Entries behind B are left alone.
+ * A sequence with new_lens[r] <= 0, or whose L exceeds weights_stride or its table, or B
+ * kept_stride or the new table, is left alone as a whole.
+ *
+ * Kept tokens go to the blocks of new_table [n_seqs][new_max_blocks], from block F / 16 on;
+ * blocks before it are not touched (the tables agree there).  A block of new_table that
+ * receives tokens must be in no row of block_table, but for entry F / 16, which may be the
+ * same in both.  With new_table NULL, or block_table itself, the tokens move within the
+ * sequence's own blocks, which from F / 16 on must be in that sequence's table only;
+ * fewer workgroups share that work, since a block is written only once all that it held has
+ * been read.  pa_seq_compact gives the pool's side of both.  Tokens whose block id (old or
+ * new) is outside [0, num_blocks) are read from a clamped block, or not written.
+ *
+ * dtype: PA_F32 and PA_BF16 with scales NULL; PA_BF16_KV4, where a token's scales move too.
+ * (Tokens of the 8-bit cache share their block's scale and would be rounded again: read
+ * them with pa_kv8_read, pick rows, append them.)  All pointers are caller-owned device
+ * memory; asynchronous on stream; allocates nothing.  Errors: PA_ERR_ARG (NULL pointer with
+ * work to do, negative size, caches not 16-byte, weights or kept not 4-byte aligned, tables
+ * that are one with two widths), PA_ERR_UNSUPPORTED (head_dim, block_size, dtype),
+ * PA_ERR_LAUNCH. */
+int pa_kv_evict(const float* weights, float* weights_out, int64_t weights_stride,
+                const int32_t* block_table, int32_t max_blocks_per_seq, const int32_t* new_table,
+                int32_t new_max_blocks, const int32_t* seq_lens, const int32_t* new_lens,
+                const int32_t* first, int32_t window, int32_t n_seqs, void* k_cache, void* v_cache,
+                uint8_t* scales, int32_t num_blocks, int32_t num_kv_heads, int32_t head_dim,
+                int32_t block_size, int32_t dtype, int32_t* kept, int64_t kept_stride, void* stream);
 
 /* Norms of queries and keys for each head and the rotation by position, in one
  * pass over a step's rows, on their way from the projection to the append and

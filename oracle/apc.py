@@ -32,7 +32,11 @@ the design notes:
   fails.  Capacity is checked before anything changes;
 * truncation (rolling back draft or chunk tokens) may only drop unregistered
   blocks; they return to the *front* of the free list, so ``extend`` followed
-  by ``truncate`` restores the pool exactly.
+  by ``truncate`` restores the pool exactly;
+* compaction (chosen tokens of a sequence stay, its first ``first`` as they are) either
+  gives it new blocks behind the full ones of those, its hold on the old ones ending as at
+  release, or (in place) keeps its leading blocks, of which none registered may change.
+  Its blocks are not registered any more.
 """
 from __future__ import annotations
 
@@ -93,6 +97,8 @@ class PrefixCacheOracle:
     def _register_run(self, st):
         """Register full blocks after the sequence's registered leading run,
         in logical order, while the chain is unbroken and the prefix is new."""
+        if st.get("compacted"):
+            return
         bs, toks, blocks = self.bs, st["tokens"], st["blocks"]
         j = st["n_reg"]
         level = self._children(toks, j)
@@ -188,15 +194,45 @@ class PrefixCacheOracle:
     def free_seq(self, seq_id):
         st = self._seq(seq_id)
         self._register_run(st)
-        for b in st["blocks"]:
+        self._release(st["blocks"])
+        del self.seqs[seq_id]
+
+    def _release(self, blocks):
+        for b in blocks:
             self.ref[b] -= 1
             if self.ref[b] == 0 and b not in self.registered:
                 self.free.append(b)
-        for b in reversed(st["blocks"]):
+        for b in reversed(blocks):
             if self.ref[b] == 0 and b in self.registered:
                 self.clock += 1
                 self.stamp[b] = self.clock
-        del self.seqs[seq_id]
+
+    def compact(self, seq_id, new_len: int, first: int, in_place: bool):
+        st = self._seq(seq_id)
+        if not (1 <= new_len <= len(st["tokens"]) and 0 <= first <= new_len):
+            raise ArgError(f"cannot compact to {new_len} tokens, first {first}")
+        total = -(-new_len // self.bs)
+        if in_place:
+            if first < st["n_reg"] * self.bs:
+                raise ArgError("registered blocks would change")
+            for b in reversed(st["blocks"][total:]):
+                self.ref[b] -= 1
+                self.free.appendleft(b)
+            del st["blocks"][total:]
+        else:
+            stay = first // self.bs
+            if total - stay > self._obtainable():
+                raise NoBlocksError(f"need {total - stay} blocks")
+            old = st["blocks"][stay:]
+            del st["blocks"][stay:]
+            for _ in range(total - stay):
+                b = self._take()
+                self.ref[b] = 1
+                st["blocks"].append(b)
+            self._release(old)
+            st["n_reg"] = min(st["n_reg"], stay)
+        del st["tokens"][new_len:]
+        st["compacted"] = True
 
     def seq_len(self, seq_id) -> int:
         return len(self._seq(seq_id)["tokens"])

@@ -35,7 +35,8 @@ EXPORTS = ["pa_last_error", "pa_abi_version", "pa_pool_create", "pa_pool_destroy
            "pa_kv8_attn_decode", "pa_kv8_attn_verify", "pa_kv8_attn_decode_noalloc",
            "pa_kv4_append", "pa_kv4_read", "pa_kv4_attn_prefill", "pa_kv4_attn_decode",
            "pa_kv4_attn_verify", "pa_kv4_attn_decode_noalloc",
-           "pa_qk_norm_rope", "pa_set_launch_events"]
+           "pa_seq_compact", "pa_attn_weights", "pa_kv_evict", "pa_qk_norm_rope",
+           "pa_set_launch_events"]
 
 
 class PaError(RuntimeError):
@@ -101,6 +102,7 @@ def lib():
         "pa_seqs_extend": (C.c_int, [_P, i32, _I64P, _I32P, _I32P, _I32P]),
         "pa_seqs_truncate": (C.c_int, [_P, i32, _I64P, _I32P, _I32P]),
         "pa_seqs_free": (C.c_int, [_P, i32, _I64P, _I32P]),
+        "pa_seq_compact": (C.c_int, [_P, i64, i32, i32, i32]),
         "pa_pool_apply": (C.c_int, [_P, i32, _P, _P, _P, _P, _P, _P, _P]),
         "pa_seq_len": (C.c_int, [_P, i64, _I32P]),
         "pa_seq_blocks": (C.c_int, [_P, i64, _I32P, i32, _I32P]),
@@ -136,6 +138,10 @@ def lib():
         for kind in ("prefill", "decode", "verify"):
             sig[f"pa_kv{bits}_attn_{kind}"] = (C.c_int, kv8)
         sig[f"pa_kv{bits}_attn_decode_noalloc"] = (C.c_int, kv8[:18] + kv8[20:])
+    sig["pa_attn_weights"] = (C.c_int, [_P, _P, _P, _P, i32, _P, i32, _P, _P, i32, i32, i32, i32,
+                                        i32, i32, f32, i32, _P, i64, i32, _P])
+    sig["pa_kv_evict"] = (C.c_int, [_P, _P, i64, _P, i32, _P, i32, _P, _P, _P, i32, i32, _P, _P, _P,
+                                    i32, i32, i32, i32, i32, _P, i64, _P])
     sig["pa_qk_norm_rope"] = (C.c_int, [_P, i64, _P, i64, _P, i32, _P, i32, i32, _P, _P, f32, i32,
                                         _P, _P, i32, i32, i32, i32, _P])
     sig["pa_set_launch_events"] = (C.c_int, [_P, _P])
@@ -288,6 +294,12 @@ class Pool:
 
     def truncate(self, seq_id: int, new_len: int):
         _check(self._lib.pa_seq_truncate(self._h, int(seq_id), int(new_len)))
+
+    def compact(self, seq_id: int, new_len: int, first: int = 0, in_place: bool = False):
+        """The pool's side of kv_evict: the sequence holds new_len tokens, its first
+        ``first`` ones unchanged, in new blocks or (``in_place``) in its own."""
+        _check(self._lib.pa_seq_compact(self._h, int(seq_id), int(new_len), int(first),
+                                        int(bool(in_place))))
 
     def free(self, seq_id: int):
         _check(self._lib.pa_seq_free(self._h, int(seq_id)))
@@ -881,6 +893,140 @@ def kv4_attention_decode_noalloc(q, k_cache, v_cache, scales, block_table, seq_l
     args, st = _quant_attn_args(4, q, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlens_q,
                                 plan_dev, info, out, lse, scale, stream, None)
     _check(fn(*args, out.data_ptr(), _dptr(lse), st))
+
+
+# -- eviction from live contexts ------------------------------------------------
+def _plain_form(t, k_cache, scales):
+    """(dtype code, blocks, kv-heads, head_dim, block size) of the cache that k_cache, and for
+    the 4-bit cache scales, are part of; code None: no cache that the calls below take."""
+    dt, dim = k_cache.dtype, k_cache.dim()
+    if scales is not None:
+        if dim != 4 or dt != t.uint8:
+            return None, 0, 0, 0, 16
+        nb, hkv, bs, half = k_cache.shape
+        return PA_BF16_KV4, nb, hkv, 2 * half, bs
+    code = _ROW_DTYPES.get(dt)
+    if dim != 5 or k_cache.shape[4] != 32:
+        return None, 0, 0, 0, 16
+    nb, hkv, groups, bs, _ = k_cache.shape
+    return code, nb, hkv, 32 * groups, bs
+
+
+def attention_weights(q, lse, k_cache, block_table, seq_lens, cu_seqlens_q, weights, scales=None,
+                      accumulate: bool = False, scale=None, stream=None):
+    """weights[r, h, t] (float32 [n_seqs, Hkv, >= longest sequence]): the probabilities of
+    cached key t summed over the rows of sequence r and the query heads of kv-head h, from
+    an attention call's queries and log-sum-exps; added to what is there with
+    ``accumulate``.  k_cache of a bf16 cache, or of a 4-bit one with its scales."""
+    t = _torch or _torch_module()
+    fn = (_lib or lib()).pa_attn_weights
+    code, nb, hkv, d, bs = _plain_form(t, k_cache, scales)
+    total_q, hq, dq = q.shape
+    n, i32 = seq_lens.numel(), t.int32
+    rows, width = block_table.shape if block_table.dim() == 2 else (-1, 0)
+    dev = k_cache.get_device()
+    st = _stream_on(dev, stream)
+    if not (code in (PA_BF16, PA_BF16_KV4) and q.dtype == t.bfloat16 and dq == d
+            and q.is_contiguous() and k_cache.is_contiguous()
+            and lse.dtype == t.float32 and lse.shape == (total_q, hq) and lse.is_contiguous()
+            and weights.dtype == t.float32 and weights.dim() == 3 and weights.shape[0] >= n
+            and weights.shape[1] == hkv and weights.is_contiguous()
+            and (scales is None or (scales.dtype == t.uint8 and scales.is_contiguous()
+                 and scales.shape == (nb, hkv, d // 32 + 1, 16) and scales.get_device() == dev))
+            and rows >= n and cu_seqlens_q.numel() > n
+            and block_table.dtype == i32 and seq_lens.dtype == i32 and cu_seqlens_q.dtype == i32
+            and block_table.is_contiguous() and seq_lens.is_contiguous()
+            and cu_seqlens_q.is_contiguous()
+            and st >= 0 and q.get_device() == lse.get_device() == weights.get_device()
+            == block_table.get_device() == seq_lens.get_device() == cu_seqlens_q.get_device() == dev):
+        _refuse(PA_ERR_UNSUPPORTED, [
+            (code in (PA_BF16, PA_BF16_KV4), f"keys {k_cache.dtype} {tuple(k_cache.shape)}"
+             f"{'' if scales is None else ' with scales'}: supported are a bf16 cache's, or a "
+             "4-bit cache's with its scales"),
+            (q.dtype == t.bfloat16, f"queries {q.dtype} (supported: bfloat16)")])
+        _refuse(PA_ERR_ARG, [
+            (dq == d and q.is_contiguous(), "q must be contiguous [T, Hq, D] of the cache's head_dim"),
+            (k_cache.is_contiguous(), "k_cache must be contiguous"),
+            (lse.dtype == t.float32 and lse.shape == (total_q, hq) and lse.is_contiguous(),
+             "lse must be contiguous float32 [T, Hq]"),
+            (weights.dtype == t.float32 and weights.dim() == 3 and weights.shape[0] >= n
+             and weights.shape[1] == hkv and weights.is_contiguous(),
+             f"weights must be contiguous float32 [{n}, {hkv}, keys]"),
+            (scales is None or (scales.dtype == t.uint8 and scales.is_contiguous()
+             and scales.shape == (nb, hkv, d // 32 + 1, 16)),
+             f"scales must be contiguous uint8 [{nb}, {hkv}, {d // 32 + 1}, 16]")])
+        _refuse_metadata(t, block_table, seq_lens, cu_seqlens_q)
+        _refuse_device(q, lse, k_cache, scales, weights, block_table, seq_lens, cu_seqlens_q)
+    rc = fn(q.data_ptr(), lse.data_ptr(), k_cache.data_ptr(), _dptr(scales), nb,
+            block_table.data_ptr(), width, seq_lens.data_ptr(), cu_seqlens_q.data_ptr(), n, total_q,
+            hq, hkv, d, bs, d ** -0.5 if scale is None else scale, code, weights.data_ptr(),
+            weights.shape[2], int(bool(accumulate)), st)
+    if rc:
+        _check(rc)
+
+
+def kv_evict(weights, block_table, seq_lens, new_lens, k_cache, v_cache, kept, scales=None,
+             new_table=None, weights_out=None, first=None, window: int = 0, stream=None):
+    """Shorten sequences to new_lens tokens: the first ``first[r]``, the last ``window`` and
+    the heaviest of the rest stay, for each kv-head its own.  kept (int32 [n_seqs, Hkv, >=
+    longest new length]) receives their positions, weights_out (default: weights itself)
+    their weights; keys and values move to the blocks of new_table, by default within the
+    sequence's own.  A float32, bf16 or, with its scales, 4-bit cache."""
+    t = _torch or _torch_module()
+    fn = (_lib or lib()).pa_kv_evict
+    code, nb, hkv, d, bs = _plain_form(t, k_cache, scales)
+    v_shape = (nb, hkv, d // 32, 16, 16) if scales is not None else (nb, hkv, d, bs)
+    n, i32, f32 = seq_lens.numel(), t.int32, t.float32
+    if weights_out is None:
+        weights_out = weights
+    dev = k_cache.get_device()
+    st = _stream_on(dev, stream)
+    lists = (seq_lens, new_lens) if first is None else (seq_lens, new_lens, first)
+    tables = (block_table,) if new_table is None else (block_table, new_table)
+
+    def spare(x, dtype):
+        return (x.dtype == dtype and x.dim() == 3 and x.shape[0] >= n and x.shape[1] == hkv
+                and x.is_contiguous())
+
+    if not (code is not None and v_cache.dtype == k_cache.dtype and v_cache.shape == v_shape
+            and k_cache.is_contiguous() and v_cache.is_contiguous()
+            and (scales is None or (scales.dtype == t.uint8 and scales.is_contiguous()
+                 and scales.shape == (nb, hkv, d // 32 + 1, 16) and scales.get_device() == dev))
+            and spare(weights, f32) and spare(weights_out, f32)
+            and weights_out.shape[2] == weights.shape[2] and spare(kept, i32)
+            and all(x.dtype == i32 and x.numel() == n and x.is_contiguous()
+                    and x.get_device() == dev for x in lists)
+            and all(x.dtype == i32 and x.dim() == 2 and x.shape[0] >= n and x.is_contiguous()
+                    and x.get_device() == dev for x in tables)
+            and st >= 0 and v_cache.get_device() == weights.get_device()
+            == weights_out.get_device() == kept.get_device() == dev):
+        _refuse(PA_ERR_UNSUPPORTED, [
+            (code is not None, f"keys {k_cache.dtype} {tuple(k_cache.shape)}"
+             f"{'' if scales is None else ' with scales'}: supported are a float32 or bf16 "
+             "cache's, or a 4-bit cache's with its scales")])
+        _refuse(PA_ERR_ARG, [
+            (v_cache.dtype == k_cache.dtype and v_cache.shape == v_shape
+             and k_cache.is_contiguous() and v_cache.is_contiguous(),
+             f"k_cache and v_cache must be contiguous, v_cache {v_shape} of k_cache's type"),
+            (scales is None or (scales.dtype == t.uint8 and scales.is_contiguous()
+             and scales.shape == (nb, hkv, d // 32 + 1, 16)),
+             f"scales must be contiguous uint8 [{nb}, {hkv}, {d // 32 + 1}, 16]"),
+            (spare(weights, f32) and spare(weights_out, f32)
+             and weights_out.shape[2] == weights.shape[2],
+             f"weights and weights_out must be contiguous float32 [{n}, {hkv}, keys] of one width"),
+            (spare(kept, i32), f"kept must be contiguous int32 [{n}, {hkv}, longest new length]"),
+            (all(x.dtype == i32 and x.numel() == n and x.is_contiguous() for x in lists),
+             f"seq_lens, new_lens and first must be contiguous int32 of {n} sequences"),
+            (all(x.dtype == i32 and x.dim() == 2 and x.shape[0] >= n and x.is_contiguous()
+                 for x in tables), f"tables must be contiguous int32 [{n}, blocks]")])
+        _refuse_device(k_cache, v_cache, scales, weights, weights_out, kept, *lists, *tables)
+    rc = fn(weights.data_ptr(), weights_out.data_ptr(), weights.shape[2], block_table.data_ptr(),
+            block_table.shape[1], _dptr(new_table), 0 if new_table is None else new_table.shape[1],
+            seq_lens.data_ptr(), new_lens.data_ptr(), _dptr(first), int(window), n,
+            k_cache.data_ptr(), v_cache.data_ptr(), _dptr(scales), nb, hkv, d, bs, code,
+            kept.data_ptr(), kept.shape[2], st)
+    if rc:
+        _check(rc)
 
 
 def qk_norm_rope(q, k, positions, cos_sin, q_out, k_out, q_weight=None, k_weight=None,

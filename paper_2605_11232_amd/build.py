@@ -19,7 +19,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB_PATH = os.path.join(HERE, "libpa.so")
 
 HIP_SOURCES = ["attn_bf16.hip", "attn_kv8.hip", "attn_kv4.hip", "attn_f32.hip", "kv_append.hip",
-               "kv8.hip", "kv4.hip", "qk_norm_rope.hip", "stage.hip", "api.hip"]
+               "kv8.hip", "kv4.hip", "kv_evict.hip", "attn_weights.hip", "qk_norm_rope.hip",
+               "stage.hip", "api.hip"]
 HOST_SOURCES = ["pool.cpp", "plan.cpp", "batch.cpp", "step.cpp", "errors.cpp"]
 
 ARCH = "gfx950"

@@ -49,6 +49,17 @@ int launch_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t 
                         int32_t n_positions, int32_t rot, const void* qw, const void* kw, float eps,
                         int32_t flags, void* q_out, void* k_out, int32_t hq, int32_t hkv, int32_t d,
                         int32_t dtype, hipStream_t stream);
+int launch_attn_weights(const void* q, const float* lse, const void* kc, const uint8_t* scales,
+                        int32_t num_blocks, const int32_t* bt, int32_t max_blocks,
+                        const int32_t* seq_lens, const int32_t* cu, int32_t n_seqs, int32_t total_q,
+                        int32_t hq, int32_t hkv, int32_t d, int32_t bits, float scale, float* w,
+                        int64_t w_stride, bool add, hipStream_t stream);
+int launch_kv_evict(const float* w, float* w_out, int64_t w_stride, const int32_t* bt,
+                    int32_t max_blocks, const int32_t* bt_new, int32_t max_new,
+                    const int32_t* seq_lens, const int32_t* new_lens, const int32_t* first,
+                    int32_t window, int32_t n_seqs, void* kc, void* vc, uint8_t* scales,
+                    int32_t num_blocks, int32_t hkv, int32_t d, int32_t elem, int32_t* kept,
+                    int64_t kept_stride, bool in_place, hipStream_t stream);
 int launch_stage_upload(const void* src, void* dst, int64_t n_dwords, hipStream_t stream);
 }  // namespace dev
 
@@ -528,6 +539,84 @@ int pa_kv4_attn_verify(PA_QUANT_ATTN_ARGS, void* workspace, size_t workspace_byt
 int pa_kv4_attn_decode_noalloc(PA_QUANT_ATTN_ARGS, void* out, float* lse, void* stream) {
   return pa::attn_common("pa_kv4_attn_decode_noalloc", PA_KIND_DECODE, PA_QUANT_ATTN_PASS(PA_BF16_KV4), nullptr, 0,
                          out, lse, stream, /*noalloc=*/true, 4, scales);
+}
+
+int pa_attn_weights(const void* q, const float* lse, const void* k_cache, const uint8_t* scales,
+                    int32_t num_blocks, const int32_t* block_table, int32_t max_blocks_per_seq,
+                    const int32_t* seq_lens, const int32_t* cu_seqlens_q, int32_t n_seqs,
+                    int32_t total_q, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                    int32_t block_size, float scale, int32_t dtype, float* weights,
+                    int64_t weights_stride, int32_t accumulate, void* stream) {
+  using pa::fail;
+  static const char* fn = "pa_attn_weights";
+  pa::clear_error();
+  if (dtype != PA_BF16 && dtype != PA_BF16_KV4)
+    return fail(PA_ERR_UNSUPPORTED, "%s: dtype %d (supported: PA_BF16, PA_BF16_KV4)", fn, dtype);
+  const bool kv4 = dtype == PA_BF16_KV4;
+  const int rc = pa::check_shape(fn, num_blocks, num_kv_heads, head_dim, block_size, PA_BF16);
+  if (rc) return rc;
+  if (num_q_heads <= 0 || num_q_heads % num_kv_heads)
+    return fail(PA_ERR_ARG, "%s: num_q_heads %d must be a positive multiple of num_kv_heads %d", fn,
+                num_q_heads, num_kv_heads);
+  if (n_seqs < 0 || total_q < 0 || max_blocks_per_seq < 1 || weights_stride < 0)
+    return fail(PA_ERR_ARG, "%s: negative size or max_blocks_per_seq < 1", fn);
+  if (int64_t(total_q) * num_q_heads > INT32_MAX)
+    return fail(PA_ERR_ARG, "%s: %d tokens of %d heads: more than 2^31 - 1 rows", fn, total_q,
+                num_q_heads);
+  if (!(scale > 0.f) || scale == __builtin_huge_valf())
+    return fail(PA_ERR_ARG, "%s: scale must be positive and finite", fn);
+  if (accumulate != 0 && accumulate != 1)
+    return fail(PA_ERR_ARG, "%s: accumulate %d must be 0 or 1", fn, accumulate);
+  if (n_seqs == 0 || total_q == 0 || weights_stride == 0) return PA_OK;
+  if (!q || !lse || !k_cache || !block_table || !seq_lens || !cu_seqlens_q || !weights ||
+      (kv4 && !scales))
+    return fail(PA_ERR_ARG, "%s: NULL device pointer", fn);
+  if (((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k_cache)) & 15) ||
+      ((reinterpret_cast<uintptr_t>(lse) | reinterpret_cast<uintptr_t>(weights)) & 3))
+    return fail(PA_ERR_ARG, "%s: q and the cache must be 16-byte aligned, lse and weights 4-byte", fn);
+  const int e = pa::dev::launch_attn_weights(
+      q, lse, k_cache, scales, num_blocks, block_table, max_blocks_per_seq, seq_lens, cu_seqlens_q,
+      n_seqs, total_q, num_q_heads, num_kv_heads, head_dim, kv4 ? 4 : 16, scale, weights,
+      weights_stride, accumulate != 0, static_cast<hipStream_t>(stream));
+  if (e) return fail(PA_ERR_LAUNCH, "%s: %s", fn, hipGetErrorString(static_cast<hipError_t>(e)));
+  return PA_OK;
+}
+
+int pa_kv_evict(const float* weights, float* weights_out, int64_t weights_stride,
+                const int32_t* block_table, int32_t max_blocks_per_seq, const int32_t* new_table,
+                int32_t new_max_blocks, const int32_t* seq_lens, const int32_t* new_lens,
+                const int32_t* first, int32_t window, int32_t n_seqs, void* k_cache, void* v_cache,
+                uint8_t* scales, int32_t num_blocks, int32_t num_kv_heads, int32_t head_dim,
+                int32_t block_size, int32_t dtype, int32_t* kept, int64_t kept_stride, void* stream) {
+  using pa::fail;
+  static const char* fn = "pa_kv_evict";
+  pa::clear_error();
+  if (dtype != PA_F32 && dtype != PA_BF16 && dtype != PA_BF16_KV4)
+    return fail(PA_ERR_UNSUPPORTED, "%s: dtype %d (supported: PA_F32, PA_BF16, PA_BF16_KV4)", fn, dtype);
+  const bool kv4 = dtype == PA_BF16_KV4;
+  const int rc = pa::check_shape(fn, num_blocks, num_kv_heads, head_dim, block_size, kv4 ? PA_BF16 : dtype);
+  if (rc) return rc;
+  const bool in_place = !new_table || new_table == block_table;
+  if (n_seqs < 0 || window < 0 || weights_stride < 0 || kept_stride < 0 || max_blocks_per_seq < 1 ||
+      (!in_place && new_max_blocks < 1))
+    return fail(PA_ERR_ARG, "%s: negative size or a table of no blocks", fn);
+  if (new_table == block_table && new_table && new_max_blocks != max_blocks_per_seq)
+    return fail(PA_ERR_ARG, "%s: one table of %d and %d blocks", fn, max_blocks_per_seq, new_max_blocks);
+  if (n_seqs == 0 || weights_stride == 0 || kept_stride == 0) return PA_OK;
+  if (!weights || !weights_out || !block_table || !seq_lens || !new_lens || !k_cache || !v_cache ||
+      !kept || (kv4 && !scales))
+    return fail(PA_ERR_ARG, "%s: NULL device pointer", fn);
+  if (((reinterpret_cast<uintptr_t>(k_cache) | reinterpret_cast<uintptr_t>(v_cache)) & 15) ||
+      ((reinterpret_cast<uintptr_t>(weights) | reinterpret_cast<uintptr_t>(weights_out) |
+        reinterpret_cast<uintptr_t>(kept)) & 3))
+    return fail(PA_ERR_ARG, "%s: caches must be 16-byte aligned, weights and kept 4-byte", fn);
+  const int e = pa::dev::launch_kv_evict(
+      weights, weights_out, weights_stride, block_table, max_blocks_per_seq,
+      in_place ? block_table : new_table, in_place ? max_blocks_per_seq : new_max_blocks, seq_lens,
+      new_lens, first, window, n_seqs, k_cache, v_cache, scales, num_blocks, num_kv_heads, head_dim,
+      kv4 ? 0 : dtype == PA_BF16 ? 2 : 4, kept, kept_stride, in_place, static_cast<hipStream_t>(stream));
+  if (e) return fail(PA_ERR_LAUNCH, "%s: %s", fn, hipGetErrorString(static_cast<hipError_t>(e)));
+  return PA_OK;
 }
 
 int pa_set_launch_events(void* start_event, void* stop_event) {

@@ -1,0 +1,354 @@
+// Eviction: of each sequence and kv-head the first F tokens, the last W and the heaviest of
+// the rest stay, B in all; their keys, values and weights move together, in order.
+//
+// Two launches.  The first finds the tokens: a workgroup per (sequence, kv-head) finds the
+// (B - F - W)-th largest weight digit by digit (histograms in LDS of 11, 11 and 10 bits of
+// the weights' bits, ordered as the numbers are), then writes the positions of what stays
+// in order, of equal weights the first ones.  The second moves: a wavefront per block of 16
+// tokens that are kept.  Kept tokens only move towards the front: token i comes from a
+// position of i or more.  In place, a block is therefore written once every block before it
+// and itself have been read: a workgroup takes 16 blocks at a time and waits between.
+#include <type_traits>
+
+#include "device_common.h"
+
+namespace pa {
+namespace dev {
+namespace {
+
+struct EvictArgs {
+  const float* w;
+  float* w_out;
+  int64_t w_stride;
+  const int32_t* bt;
+  const int32_t* bt_new;
+  const int32_t* seq_lens;
+  const int32_t* new_lens;
+  const int32_t* first;  // or NULL
+  int32_t* kept;
+  int64_t kept_stride;
+  uint8_t* kc;
+  uint8_t* vc;
+  uint8_t* scales;
+  int32_t max_blocks, max_new, window, num_blocks, hkv, groups;
+};
+
+struct Lens {
+  int len, keep, front, window;  // keep 0: nothing to do
+};
+
+// A sequence's lengths; one that does not fit the arrays is left alone.
+__device__ __forceinline__ Lens lens_of(const EvictArgs& a, int r) {
+  const int L = a.seq_lens[r], B = min(a.new_lens[r], L);
+  if (B <= 0 || L > a.w_stride || L > int64_t(a.max_blocks) * kBlock || B > a.kept_stride ||
+      B > int64_t(a.max_new) * kBlock)
+    return {L, 0, 0, 0};
+  const int F = a.first ? min(max(a.first[r], 0), B) : 0;
+  return {L, B, F, min(a.window, B - F)};
+}
+
+// Order of the numbers, as unsigned: NaN last, zeros of either sign alike.
+__device__ __forceinline__ uint32_t order_of(float x) {
+  if (x != x) return ~0u;
+  const uint32_t u = __float_as_uint(x + 0.f);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+constexpr int kSelectThreads = 1024;
+constexpr int kSelectWaves = kSelectThreads / 64;
+
+__global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs a) {
+  __shared__ int hist[2048];
+  __shared__ int part[2][kSelectWaves];
+  __shared__ int found[2];
+  const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r = blockIdx.x / a.hkv;
+  const Lens n = lens_of(a, r);
+  if (n.keep == 0) return;
+  const float* w = a.w + blockIdx.x * a.w_stride;
+  int32_t* kept = a.kept + blockIdx.x * a.kept_stride;
+  const int lo = n.front, hi = n.len - n.window;  // candidates
+  const int want = n.keep - n.front - n.window;
+
+  // The want-th largest candidate T, and how many of those equal to it stay.
+  uint32_t T = 0;
+  int ties = 0;
+  if (want > 0) {
+    int left = want;
+    uint32_t prefix = 0, known = 0;  // T's bits found so far, and which
+    constexpr int kShift[3] = {21, 10, 0}, kBins[3] = {2048, 2048, 1024};
+    for (int d = 0; d < 3; ++d) {
+      for (int i = tid; i < 2048; i += kSelectThreads) hist[i] = 0;
+      __syncthreads();
+      for (int i = lo + tid; i < hi; i += kSelectThreads) {
+        const uint32_t u = order_of(w[i]);
+        if ((u & known) == prefix) atomicAdd(&hist[u >> kShift[d] & (kBins[d] - 1)], 1);
+      }
+      __syncthreads();
+      // Counts from the largest digit down: thread t holds digits 2047 - 2 t and the one
+      // below (of 1024 digits the larger half is empty).
+      const int b = 2047 - 2 * tid;
+      const int h0 = hist[b], h1 = hist[b - 1];
+      int sum = h0 + h1;
+#pragma unroll
+      for (int m = 1; m < 64; m <<= 1) {
+        const int o = __shfl_up(sum, m, 64);
+        if (lane >= m) sum += o;
+      }
+      if (lane == 63) part[0][wv] = sum;
+      __syncthreads();
+      int before = sum - h0 - h1;
+      for (int v = 0; v < wv; ++v) before += part[0][v];
+      // the digit where the count reaches `left`
+      if (before < left && before + h0 + h1 >= left) {
+        const bool low = before + h0 < left;
+        found[0] = low ? b - 1 : b;
+        found[1] = left - before - (low ? h0 : 0);
+      }
+      __syncthreads();
+      prefix |= uint32_t(found[0]) << kShift[d];
+      known |= uint32_t(kBins[d] - 1) << kShift[d];
+      left = found[1];
+      __syncthreads();
+    }
+    T = prefix;
+    ties = left;
+  }
+
+  // A wavefront takes an even share of the positions: how many stay of it, and how many
+  // equal T.
+  const int share = (n.len + kSelectThreads - 1) / kSelectThreads * 64;
+  const int p0 = min(wv * share, n.len), p1 = min(p0 + share, n.len);
+  // 0: goes, 1: equals T, 2: stays
+  auto kind = [&](int i) {
+    if (i < lo || i >= hi) return 2;
+    if (want <= 0) return 0;
+    const uint32_t u = order_of(w[i]);
+    return u > T ? 2 : u == T ? 1 : 0;
+  };
+  int stay = 0, equal = 0;
+  for (int i0 = p0; i0 < p1; i0 += 64) {
+    const int k = i0 + lane < p1 ? kind(i0 + lane) : 0;
+    stay += __popcll(__ballot(k == 2));
+    equal += __popcll(__ballot(k == 1));
+  }
+  if (lane == 0) part[0][wv] = stay, part[1][wv] = equal;
+  __syncthreads();
+  int at = 0, eq = 0;  // kept, and equal ones, before this wavefront's
+  for (int v = 0; v < wv; ++v) {
+    at += part[0][v] + max(0, min(part[1][v], ties - eq));
+    eq += part[1][v];
+  }
+  const uint64_t below = (uint64_t(1) << lane) - 1;
+  for (int i0 = p0; i0 < p1; i0 += 64) {
+    const int k = i0 + lane < p1 ? kind(i0 + lane) : 0;
+    const uint64_t e = __ballot(k == 1);
+    const bool keep = k == 2 || (k == 1 && eq + __popcll(e & below) < ties);
+    const uint64_t m = __ballot(keep);
+    if (keep) kept[at + __popcll(m & below)] = i0 + lane;
+    at += __popcll(m);
+    eq += __popcll(e);
+  }
+  __syncthreads();
+  // The weights move, in place: a thousand are read before they are written.
+  float* out = a.w_out + blockIdx.x * a.w_stride;
+  for (int i0 = 0; i0 < n.keep; i0 += kSelectThreads) {
+    const int i = i0 + tid;
+    float x = 0.f;
+    if (i < n.keep) x = w[kept[i]];
+    asm volatile("s_waitcnt vmcnt(0)" : "+v"(x) : : "memory");
+    __syncthreads();
+    if (i < n.keep) out[i] = x;
+  }
+}
+
+// One block's kept tokens on their way: 16 tokens of a (sequence, kv-head).
+// ELEM: bytes of a value (4, 2), or 0 for the 4-bit cache.
+template <int D, int ELEM>
+struct Moved {
+  static constexpr bool KV4 = ELEM == 0;
+  static constexpr int kHeadBytes = KV4 ? kBlock * D / 2 : kBlock * D * ELEM;
+  static constexpr int NK = (kHeadBytes / 16 + 63) / 64;  // 16-byte loads of keys a lane
+  static constexpr int kScaleRows = D / 32 + 1;
+  static constexpr int NV = KV4 ? 1 : D / 64;             // dims of values a lane
+  typedef typename std::conditional<ELEM == 4, uint32_t, uint16_t>::type T;
+  u32x4 k[NK];
+  u32x4 v4;                     // KV4: dims 32 c + i and 32 c + 16 + i
+  T v[KV4 ? 1 : NV][kBlock];
+  uint32_t s[2];                // KV4: scale bytes
+
+  // Source positions of the block's tokens: lane o < 16 holds token o's.
+  __device__ __forceinline__ void load(const EvictArgs& a, int g, int pos, const int32_t* bt, int lane) {
+    const int my = pos < 0 ? 0 : pos;
+    const int id = clamp_block(bt[my / kBlock], a.num_blocks);
+    auto block_of = [&](int o) { return (int64_t)__shfl(id, o, 64) * a.hkv + g; };
+    auto off_of = [&](int o) { return __shfl(my, o, 64) % kBlock; };
+    if constexpr (KV4) {
+      constexpr int U = D / 32;  // 16-byte units of a token's key
+      const int o = lane / U % kBlock;
+      const int64_t b = block_of(o);
+      k[0] = zero16();
+      if (lane < kBlock * U) k[0] = ld16(a.kc + b * kHeadBytes + off_of(o) * (D / 2) + lane % U * 16);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int u = 64 * i + lane, so = u % kBlock;
+        const int64_t sb = block_of(so);
+        const int off = off_of(so);
+        s[i] = 0;
+        if (u < kScaleRows * kBlock) s[i] = a.scales[sb * (kScaleRows * kBlock) + u / kBlock * kBlock + off];
+      }
+      v4 = zero16();
+#pragma unroll
+      for (int t = 0; t < kBlock; ++t) {
+        const int64_t vb = block_of(t);
+        const int off = off_of(t);
+        if (lane < D / 2) {
+          const u32x4 x = ld16(a.vc + vb * kHeadBytes + 16 * lane);
+          const uint32_t c0 = (off < 8 ? x[0] : x[1]) >> (4 * (off & 7)) & 15;
+          const uint32_t c1 = (off < 8 ? x[2] : x[3]) >> (4 * (off & 7)) & 15;
+          v4[t / 8] |= c0 << (4 * (t & 7));
+          v4[2 + t / 8] |= c1 << (4 * (t & 7));
+        }
+      }
+    } else {
+      constexpr int U = 2 * ELEM;  // units of a token's 32 dims
+#pragma unroll
+      for (int i = 0; i < NK; ++i) {
+        const int u = 64 * i + lane, o = u / U % kBlock, grp = u / (U * kBlock);
+        const int64_t b = block_of(o);
+        k[i] = ld16(a.kc + b * kHeadBytes + (grp * kBlock + key_slot_pos(off_of(o))) * (32 * ELEM) + u % U * 16);
+      }
+#pragma unroll
+      for (int t = 0; t < kBlock; ++t) {
+        const T* p = reinterpret_cast<const T*>(a.vc + block_of(t) * kHeadBytes) + off_of(t);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[i][t] = p[(64 * i + lane) * kBlock];
+      }
+    }
+  }
+
+  // The first `count` tokens, to block `id`.
+  __device__ __forceinline__ void store(const EvictArgs& a, int g, int id, int count, int lane) const {
+    const int64_t b = (int64_t)id * a.hkv + g;
+    if constexpr (KV4) {
+      constexpr int U = D / 32;
+      if (lane < kBlock * U && lane / U < count) st16(a.kc + b * kHeadBytes + lane * 16, k[0]);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int u = 64 * i + lane;
+        if (u < kScaleRows * kBlock && u % kBlock < count) a.scales[b * (kScaleRows * kBlock) + u] = uint8_t(s[i]);
+      }
+      if (lane < D / 2) {
+        u32x4* p = reinterpret_cast<u32x4*>(a.vc + b * kHeadBytes) + lane;
+        u32x4 x = v4;
+        if (count < kBlock) {
+          const u32x4 was = *p;
+          const uint64_t m = (uint64_t(1) << (4 * count)) - 1;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t mi = uint32_t(m >> (32 * (i & 1)));
+            x[i] = (x[i] & mi) | (was[i] & ~mi);
+          }
+        }
+        *p = x;
+      }
+    } else {
+      constexpr int U = 2 * ELEM;
+#pragma unroll
+      for (int i = 0; i < NK; ++i) {
+        const int u = 64 * i + lane, o = u / U % kBlock, grp = u / (U * kBlock);
+        if (o < count) st16(a.kc + b * kHeadBytes + (grp * kBlock + key_slot_pos(o)) * (32 * ELEM) + u % U * 16, k[i]);
+      }
+      T* vb = reinterpret_cast<T*>(a.vc + b * kHeadBytes);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        T* p = vb + (64 * i + lane) * kBlock;
+        if (count == kBlock) {
+          struct alignas(16) Row { T x[kBlock]; } row;
+#pragma unroll
+          for (int t = 0; t < kBlock; ++t) row.x[t] = v[i][t];
+          *reinterpret_cast<Row*>(p) = row;
+        } else {
+#pragma unroll
+          for (int t = 0; t < kBlock; ++t)
+            if (t < count) p[t] = v[i][t];
+        }
+      }
+    }
+  }
+};
+
+// IN_PLACE: one workgroup per (sequence, kv-head), 16 blocks at a time; else one per four
+// blocks.
+template <int D, int ELEM, bool IN_PLACE>
+__global__ __launch_bounds__(IN_PLACE ? 1024 : 256) void evict_move_kernel(EvictArgs a) {
+  constexpr int kWaves = IN_PLACE ? 16 : 4;
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int x = IN_PLACE ? blockIdx.x : blockIdx.x / a.groups;
+  const int r = x / a.hkv, g = x - r * a.hkv;
+  const Lens n = lens_of(a, r);
+  if (n.keep == 0) return;
+  const int32_t* kept = a.kept + x * a.kept_stride;
+  const int32_t* bt = a.bt + (int64_t)r * a.max_blocks;
+  const int32_t* to = a.bt_new + (int64_t)r * a.max_new;
+  const int blocks = (n.keep + kBlock - 1) / kBlock;
+  const int first = n.front / kBlock + (IN_PLACE ? 0 : (blockIdx.x - x * a.groups) * kWaves);
+  for (int b0 = first; b0 < (IN_PLACE ? blocks : min(blocks, first + kWaves)); b0 += kWaves) {
+    const int b = b0 + wv, count = min(kBlock, n.keep - b * kBlock);
+    Moved<D, ELEM> m;
+    int id = -1;
+    if (count > 0) {
+      const int o = lane % kBlock;
+      m.load(a, g, kept[b * kBlock + min(o, count - 1)], bt, lane);
+      id = to[b];
+    }
+    if constexpr (IN_PLACE) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+    }
+    if (id >= 0 && id < a.num_blocks) m.store(a, g, id, count, lane);
+  }
+}
+
+}  // namespace
+
+int launch_kv_evict(const float* w, float* w_out, int64_t w_stride, const int32_t* bt,
+                    int32_t max_blocks, const int32_t* bt_new, int32_t max_new,
+                    const int32_t* seq_lens, const int32_t* new_lens, const int32_t* first,
+                    int32_t window, int32_t n_seqs, void* kc, void* vc, uint8_t* scales,
+                    int32_t num_blocks, int32_t hkv, int32_t d, int32_t elem, int32_t* kept,
+                    int64_t kept_stride, bool in_place, hipStream_t stream) {
+  EvictArgs a{w, w_out, w_stride, bt, bt_new, seq_lens, new_lens, first, kept, kept_stride,
+              static_cast<uint8_t*>(kc), static_cast<uint8_t*>(vc), scales, max_blocks, max_new, window,
+              num_blocks, hkv, 0};
+  const int64_t heads = int64_t(n_seqs) * hkv;
+  const int64_t blocks = min((kept_stride + kBlock - 1) / kBlock, int64_t(max_new));
+  const int64_t groups = (blocks + 3) / 4;
+  if (heads * max(groups, int64_t(1)) > INT32_MAX) return static_cast<int>(hipErrorInvalidValue);
+  a.groups = int32_t(groups);
+  hipLaunchKernelGGL(evict_select_kernel, dim3(unsigned(heads)), dim3(kSelectThreads), 0, stream, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || groups == 0) return static_cast<int>(e);
+#define PA_MOVE(DD, EE)                                                                              \
+  if (in_place)                                                                                      \
+    hipLaunchKernelGGL((evict_move_kernel<DD, EE, true>), dim3(unsigned(heads)), dim3(1024), 0, stream, a); \
+  else                                                                                               \
+    hipLaunchKernelGGL((evict_move_kernel<DD, EE, false>), dim3(unsigned(heads * groups)), dim3(256), 0, stream, a)
+#define PA_MOVE_D(EE)          \
+  if (d == 128) {              \
+    PA_MOVE(128, EE);          \
+  } else {                     \
+    PA_MOVE(64, EE);           \
+  }
+  switch (elem) {
+    case 0: PA_MOVE_D(0); break;
+    case 2: PA_MOVE_D(2); break;
+    default: PA_MOVE_D(4); break;
+  }
+#undef PA_MOVE_D
+#undef PA_MOVE
+  return static_cast<int>(hipGetLastError());
+}
+
+}  // namespace dev
+}  // namespace pa

@@ -58,6 +58,7 @@ struct pa_pool {
     std::vector<int32_t> tokens;
     std::vector<int32_t> blocks;
     int32_t n_cached_run = 0;  // leading blocks of this sequence that are in the index
+    bool compacted = false;    // blocks hold chosen tokens, not a prefix: never cached
   };
   std::unordered_map<int64_t, Seq> seqs;
 
@@ -159,6 +160,7 @@ struct pa_pool {
   // Cache the sequence's full blocks after its cached run, in logical order,
   // while the chain is unbroken and each prefix is new.
   void cache_run(Seq& s) {
+    if (s.compacted) return;
     int32_t j = s.n_cached_run;
     const int64_t L = static_cast<int64_t>(s.tokens.size());
     while (static_cast<int64_t>(j + 1) * bs <= L) {
@@ -175,6 +177,18 @@ struct pa_pool {
       ++j;
     }
     s.n_cached_run = j;
+  }
+
+  // A sequence's hold on blocks (logical order) ends.
+  void release(const std::vector<int32_t>& blocks) {
+    for (int32_t b : blocks) {
+      if (--ref[b] == 0 && !cached[b]) free_list.push_back(b);
+    }
+    // blocks that became idle are stamped tail first
+    for (size_t j = blocks.size(); j-- > 0;) {
+      const int32_t b = blocks[j];
+      if (ref[b] == 0 && cached[b]) make_idle(b);
+    }
   }
 };
 
@@ -310,6 +324,49 @@ int pa_seq_truncate(pa_pool* pool, int64_t seq_id, int32_t new_len) {
   return PA_OK;
 }
 
+int pa_seq_compact(pa_pool* pool, int64_t seq_id, int32_t new_len, int32_t first, int32_t in_place) {
+  pa::clear_error();
+  if (!pool) return pa::fail(PA_ERR_ARG, "pa_seq_compact: NULL pool");
+  auto it = pool->seqs.find(seq_id);
+  if (it == pool->seqs.end())
+    return pa::fail(PA_ERR_UNKNOWN_SEQ, "pa_seq_compact: unknown sequence %lld", (long long)seq_id);
+  pa_pool::Seq& s = it->second;
+  const int64_t L = static_cast<int64_t>(s.tokens.size());
+  if (new_len < 1 || new_len > L || first < 0 || first > new_len)
+    return pa::fail(PA_ERR_ARG, "pa_seq_compact: new_len %d outside [1, %lld], or first %d outside "
+                    "[0, new_len]", new_len, (long long)L, first);
+  const size_t total = static_cast<size_t>(pa_pool::cdiv(new_len, pool->bs));
+  if (in_place) {
+    const int64_t cached_len = static_cast<int64_t>(s.n_cached_run) * pool->bs;
+    if (first < cached_len)
+      return pa::fail(PA_ERR_ARG, "pa_seq_compact: first %d, but the leading %lld tokens' blocks are "
+                      "cached", first, (long long)cached_len);
+    for (size_t j = s.blocks.size(); j-- > total;) {
+      --pool->ref[s.blocks[j]];
+      pool->free_list.push_front(s.blocks[j]);
+    }
+    s.blocks.resize(total);
+  } else {
+    const size_t stay = static_cast<size_t>(first / pool->bs);
+    const int64_t need = static_cast<int64_t>(total - stay);
+    if (need > pool->obtainable(0))
+      return pa::fail(PA_ERR_NO_BLOCKS, "pa_seq_compact: need %lld blocks, %lld obtainable",
+                      (long long)need, (long long)pool->obtainable(0));
+    const std::vector<int32_t> old(s.blocks.begin() + stay, s.blocks.end());
+    s.blocks.resize(stay);
+    for (int64_t i = 0; i < need; ++i) {
+      const int32_t b = pool->take();
+      pool->ref[b] = 1;
+      s.blocks.push_back(b);
+    }
+    pool->release(old);
+    s.n_cached_run = std::min(s.n_cached_run, static_cast<int32_t>(stay));
+  }
+  s.tokens.resize(static_cast<size_t>(new_len));
+  s.compacted = true;
+  return PA_OK;
+}
+
 int pa_seq_free(pa_pool* pool, int64_t seq_id) {
   pa::clear_error();
   if (!pool) return pa::fail(PA_ERR_ARG, "pa_seq_free: NULL pool");
@@ -318,14 +375,7 @@ int pa_seq_free(pa_pool* pool, int64_t seq_id) {
     return pa::fail(PA_ERR_UNKNOWN_SEQ, "pa_seq_free: unknown sequence %lld", (long long)seq_id);
   pa_pool::Seq& s = it->second;
   pool->cache_run(s);
-  for (int32_t b : s.blocks) {
-    if (--pool->ref[b] == 0 && !pool->cached[b]) pool->free_list.push_back(b);
-  }
-  // blocks that became idle are stamped tail first
-  for (size_t j = s.blocks.size(); j-- > 0;) {
-    const int32_t b = s.blocks[j];
-    if (pool->ref[b] == 0 && pool->cached[b]) pool->make_idle(b);
-  }
+  pool->release(s.blocks);
   pool->seqs.erase(it);
   return PA_OK;
 }
