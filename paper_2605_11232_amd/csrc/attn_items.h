@@ -553,21 +553,28 @@ __device__ __forceinline__ void tile_item(const int32_t* it, int g, int poff, co
   // KV4: as KV8; the products take the probabilities times their tokens' value scales.
   auto exps = [&](const f32x16 (&s)[NSUB], bf16x8 (&p)[NSUB][2], int buf) {
     if constexpr (KV4) {
+      // Scales of elements 4 e4 .. + 3 of tile u, keys 32 u + 16 (e4 / 2) + 8 hh +
+      // 4 (e4 % 2) .. + 3: read one group ahead, no further (all at once they push other
+      // values out of the registers).
+      auto scales_of = [&](int i) {
+        const int u = i / 4, e4 = i % 4;
+        return *reinterpret_cast<const f32x4*>(&sm.sv[buf][32 * u + 16 * (e4 >> 1) + 4 * (e4 & 1) + 8 * hh]);
+      };
       float l0 = 0.f, l1 = 0.f;
+      f32x4 next = scales_of(0);
 #pragma unroll
-      for (int u = 0; u < NSUB; ++u)
+      for (int i = 0; i < 4 * NSUB; ++i) {
+        const f32x4 sv = next;
+        if (i + 1 < 4 * NSUB) next = scales_of(i + 1);
+        asm volatile("" ::: "memory");
 #pragma unroll
-        for (int e4 = 0; e4 < 4; ++e4) {
-          // elements 4 e4 .. + 3: keys 32 u + 16 (e4 / 2) + 8 hh + 4 (e4 % 2) .. + 3
-          const f32x4 sv = *reinterpret_cast<const f32x4*>(&sm.sv[buf][32 * u + 16 * (e4 >> 1) + 4 * (e4 & 1) + 8 * hh]);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int e = 4 * e4 + k;
-            const float x = fast_exp2(fmaf(s[u][e], c, -mc));
-            p[u][e >> 3][e & 7] = (__bf16)times_scale(x, sv[k]);
-            (e < 8 ? l0 : l1) += x;
-          }
+        for (int k = 0; k < 4; ++k) {
+          const int u = i / 4, e = 4 * (i % 4) + k;
+          const float x = fast_exp2(fmaf(s[u][e], c, -mc));
+          p[u][e >> 3][e & 7] = (__bf16)times_scale(x, sv[k]);
+          (e < 8 ? l0 : l1) += x;
         }
+      }
       return l0 + l1;
     } else if constexpr (KV8) {
       float l0 = 0.f, l1 = 0.f;
@@ -1406,6 +1413,7 @@ __device__ __forceinline__ void row_item8(const int32_t* it, int g, int poff, co
 // loaded outside the key loops, at head_dim 64 also once per item of the tail lists.
 template <int D, int MIX, int BITS>
 constexpr int waves_per_eu() {
+  if (BITS == 4 && (MIX & 1)) return kTileWavesPerEu;
   return (MIX == 2 && BITS == 16) || D == 64 ? 3 : kTileWavesPerEu;
 }
 

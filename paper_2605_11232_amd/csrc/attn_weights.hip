@@ -9,6 +9,8 @@
 // probabilities over 16 rows without looking at other lanes; the two lane halves (other
 // rows) are added once at the end.  A workgroup owns its keys and goes over all rows of the
 // sequence: no atomics, one order of the sums, and keys are read once.
+#include <type_traits>
+
 #include "device_common.h"
 
 namespace pa {
@@ -25,12 +27,15 @@ struct WeightArgs {
   const int32_t* cu;
   float* w;
   int64_t w_stride;
-  int32_t max_blocks, num_blocks, total_q, hq, hkv, chunks;
+  int32_t max_blocks, num_blocks, total_q, hq, hkv;
+  int32_t chunks;  // workgroups of a (sequence, kv-head)
+  int32_t range;   // few rows: keys of a wavefront at a time
   float scale_log2;
   bool add;
 };
 
 constexpr int kRows = 32;  // rows at a time
+constexpr int kFewWaves = 16384;  // wavefronts wanted where rows are few
 
 // LDS: two tiles of rows, 16-byte unit p of row r at unit p ^ (r & 7), so that eight
 // neighbouring lanes (rows) read distinct banks; the rows' log-sum-exps (times log2 e; a row
@@ -42,9 +47,66 @@ struct RowSmem {
   int pos[2][kRows];
 };
 
-// KT: 32-key tiles of a wavefront.
-template <int D, int BITS, int KT>
-__global__ __launch_bounds__(256) void attn_weights_kernel(WeightArgs a) {
+// A sequence's rows and keys, as the kernels see them.
+struct SeqRows {
+  int qs, rows, base, keys;  // first row's token, rows of a kv-head, its position, keys with weights
+};
+__device__ __forceinline__ SeqRows rows_of(const WeightArgs& a, int r) {
+  const int qs = a.cu[r], all = a.cu[r + 1] - qs, L = a.seq_lens[r];
+  const int n = min(a.cu[r + 1], a.total_q) - qs;
+  if (qs < 0 || n <= 0 || L < all) return {0, 0, 0, 0};
+  return {qs, n * (a.hq / a.hkv), L - all, int(min(int64_t(L), min(a.w_stride, int64_t(a.max_blocks) * kBlock)))};
+}
+__device__ __forceinline__ bool counts(float lse) { return fabsf(lse) < __builtin_huge_valf(); }
+
+// Eight e2m1 codes times the power of two of a scale byte (255: NaN), as bf16 (exact).
+__device__ __forceinline__ bf16x8 bf16_of_codes(uint32_t v, uint32_t byte) {
+  const float f = __uint_as_float(byte << 23);
+  return as_bf16x8(u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v, f, 0)),
+                         __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v, f, 1)),
+                         __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v, f, 2)),
+                         __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v, f, 3))});
+}
+
+// A lane's part of key `o` of (block, kv-head) b, half hh, as the product's operand: natural
+// k-steps over a bf16 cache; over a 4-bit one dims (D/2) hh + 8 ks, which lie together.
+template <int D, int BITS>
+struct KeyRegs {
+  static constexpr int KS = D / 16;
+  u32x4 x[BITS == 16 ? KS : D / 64];
+  uint32_t sc[D / 64];
+  __device__ __forceinline__ void load(const WeightArgs& a, int64_t b, int o, int hh) {
+    if constexpr (BITS == 16) {
+      const __bf16* p = reinterpret_cast<const __bf16*>(a.kc) + b * (kBlock * D) + key_slot_pos(o) * kKeyGroup + 8 * hh;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+        x[ks] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + (ks / 2) * (kBlock * kKeyGroup) + 16 * (ks % 2)));
+    } else {
+      const uint8_t* p = a.kc + b * (kBlock * D / 2) + o * (D / 2) + hh * (D / 4);
+      const uint8_t* s = a.scales + b * ((D / 32 + 1) * kBlock) + hh * (D / 64) * kBlock + o;
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) {
+        x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + 16 * i));
+        sc[i] = s[i * kBlock];
+      }
+    }
+  }
+  __device__ __forceinline__ bf16x8 operand(int ks) const {
+    if constexpr (BITS == 16) {
+      return as_bf16x8(x[ks]);
+    } else {
+      return bf16_of_codes(x[ks / 4][ks % 4], sc[ks / 4]);
+    }
+  }
+  // 16-byte unit of a row of q that k-step ks multiplies.
+  __device__ static __forceinline__ int unit(int ks, int hh) { return BITS == 16 ? 2 * ks + hh : hh * KS + ks; }
+};
+
+// Many rows: a workgroup's four wavefronts share each tile of 32 rows through LDS; 64 keys
+// a wavefront.
+template <int D, int BITS>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void attn_weights_kernel(WeightArgs a) {
+  constexpr int KT = 2;               // 32-key tiles of a wavefront
   constexpr int KS = D / 16;          // k-steps
   constexpr int UR = D / 8;           // 16-byte units of a row
   constexpr int NL = kRows * UR / 256;  // units of a thread
@@ -54,91 +116,78 @@ __global__ __launch_bounds__(256) void attn_weights_kernel(WeightArgs a) {
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int x = blockIdx.x / a.chunks, first_chunk = blockIdx.x - x * a.chunks;
   const int r = x / a.hkv, g = x - r * a.hkv;
-  const int qs = a.cu[r], n = min(a.cu[r + 1], a.total_q) - qs;
-  const int L = min(int64_t(a.seq_lens[r]), min(a.w_stride, int64_t(a.max_blocks) * kBlock));
-  if (qs < 0 || n <= 0 || a.seq_lens[r] < a.cu[r + 1] - qs) return;
-  const int base = a.seq_lens[r] - (a.cu[r + 1] - qs);  // first row's position
-  const int G = a.hq / a.hkv, rows = n * G;
+  const SeqRows sr = rows_of(a, r);
+  const int rows = sr.rows, L = sr.keys, G = a.hq / a.hkv;
+  if (rows == 0) return;
   const float c = a.scale_log2;
   const int32_t* bt = a.bt + (int64_t)r * a.max_blocks;
+  const int step_q = kRows / G, step_h = kRows - step_q * G;  // a tile's rows, as queries and heads
 
+  // Rows of the next tile that this thread copies: units 256 i + tid, log-sum-exp tid.
+  // All of a stage's loads are issued at once; whether a row counts is looked at when it is
+  // stored.
   u32x4 raw[NL];
-  float raw_lse = 0.f;
+  float raw_z[NL], raw_lse = 0.f;
   int raw_pos = 0;
-  // the row of unit i, or the row tid for its log-sum-exp
-  auto row_of = [&](int rho, int& qi) {
-    qi = rho / G;
-    return (int64_t)(qs + qi) * a.hq + g * G + (rho - qi * G);
+  const int64_t row0 = (int64_t)sr.qs * a.hq + g * G;
+  int qi[NL], head[NL], qi_z = 0, head_z = 0;
+  auto seek_rows = [&](int r0) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int rho = r0 + (256 * i + tid) / UR;
+      qi[i] = rho / G, head[i] = rho - qi[i] * G;
+    }
+    qi_z = (r0 + tid) / G, head_z = r0 + tid - qi_z * G;
   };
-  auto counts = [](float lse) { return fabsf(lse) < __builtin_huge_valf(); };
+  auto advance = [&](int& q, int& h) {
+    q += step_q, h += step_h;
+    if (h >= G) h -= G, ++q;
+  };
   auto load_rows = [&](int r0) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const int u = 256 * i + tid, lr = u / UR, p = u % UR;
-      raw[i] = zero16();
-      if (r0 + lr < rows) {
-        int qi;
-        const int64_t row = row_of(r0 + lr, qi);
-        const u32x4 v = ld16(a.q + row * D + 8 * p);
-        if (counts(a.lse[row])) raw[i] = v;
-      }
+      const int u = 256 * i + tid, p = u % UR;
+      const bool in = r0 + u / UR < rows;
+      const int64_t row = row0 + (in ? qi[i] * a.hq + head[i] : 0);
+      raw[i] = ld16(a.q + row * D + 8 * p);
+      raw_z[i] = in ? a.lse[row] : __builtin_huge_valf();
+      advance(qi[i], head[i]);
     }
     if (tid < kRows) {
-      raw_lse = __builtin_huge_valf();
-      raw_pos = -1;
-      if (r0 + tid < rows) {
-        int qi;
-        const float lse = a.lse[row_of(r0 + tid, qi)];
-        if (counts(lse)) raw_lse = lse * kLog2e;
-        raw_pos = base + qi;
-      }
+      const bool in = r0 + tid < rows;
+      raw_lse = in ? a.lse[row0 + qi_z * a.hq + head_z] : __builtin_huge_valf();
+      raw_pos = in ? sr.base + qi_z : -1;
+      advance(qi_z, head_z);
     }
   };
   auto store_rows = [&](int buf) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       const int u = 256 * i + tid, lr = u / UR, p = u % UR;
-      st16(&sm.q[buf][8 * (lr * UR + (p ^ (lr & 7)))], raw[i]);
+      st16(&sm.q[buf][8 * (lr * UR + (p ^ (lr & 7)))], counts(raw_z[i]) ? raw[i] : zero16());
     }
-    if (tid < kRows) sm.lse[buf][tid] = raw_lse, sm.pos[buf][tid] = raw_pos;
+    if (tid < kRows) {
+      sm.lse[buf][tid] = counts(raw_lse) ? raw_lse * kLog2e : __builtin_huge_valf();
+      sm.pos[buf][tid] = raw_pos;
+    }
   };
 
   for (int64_t chunk = first_chunk; chunk * kChunk < L; chunk += a.chunks) {
     const int key0 = int(chunk) * kChunk;
     // rows from the first that sees one of the chunk's keys on
-    const int row_first = max(0, key0 - base) * G / kRows * kRows;
+    const int row_first = max(0, key0 - sr.base) * G / kRows * kRows;
+    seek_rows(row_first);
     load_rows(row_first);
-    // the keys: lane (j, hh) holds key j's dims of each k-step
     bf16x8 k[KT][KS];
     int key[KT];
 #pragma unroll
     for (int t = 0; t < KT; ++t) {
       key[t] = key0 + (w * KT + t) * 32 + j;
       const int kk = min(key[t], L - 1);
-      const int64_t b = (int64_t)clamp_block(bt[kk / kBlock], a.num_blocks) * a.hkv + g;
-      const int o = kk % kBlock;
-      if constexpr (BITS == 16) {
-        const __bf16* p = reinterpret_cast<const __bf16*>(a.kc) + b * (kBlock * D) + key_slot_pos(o) * kKeyGroup + 8 * hh;
+      KeyRegs<D, BITS> raw_k;
+      raw_k.load(a, (int64_t)clamp_block(bt[kk / kBlock], a.num_blocks) * a.hkv + g, kk % kBlock, hh);
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
-          k[t][ks] = as_bf16x8(__builtin_nontemporal_load(reinterpret_cast<const u32x4*>(
-              p + (ks / 2) * (kBlock * kKeyGroup) + 16 * (ks % 2))));
-      } else {
-        const uint8_t* p = a.kc + b * (kBlock * D / 2) + o * (D / 2) + hh * (D / 4);
-        const uint8_t* s = a.scales + b * ((D / 32 + 1) * kBlock) + hh * (D / 64) * kBlock + o;
-#pragma unroll
-        for (int i = 0; i < D / 64; ++i) {
-          const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + 16 * i));
-          const float sc = __uint_as_float(uint32_t(s[i * kBlock]) << 23);
-#pragma unroll
-          for (int u = 0; u < 4; ++u)
-            k[t][4 * i + u] = as_bf16x8(u32x4{
-                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[u], sc, 0)),
-                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[u], sc, 1)),
-                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[u], sc, 2)),
-                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[u], sc, 3))});
-        }
-      }
+      for (int ks = 0; ks < KS; ++ks) k[t][ks] = raw_k.operand(ks);
     }
     float sum[KT];
 #pragma unroll
@@ -155,28 +204,43 @@ __global__ __launch_bounds__(256) void attn_weights_kernel(WeightArgs a) {
       for (int t = 0; t < KT; ++t)
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
+      // reads of the rows go three k-steps ahead of the products
+      u32x4 qx[3];
+      auto q_of = [&](int ks) {
+        const int p = KeyRegs<D, BITS>::unit(ks, hh);
+        return ld16(&sm.q[buf][8 * (j * UR + (p ^ (j & 7)))]);
+      };
+#pragma unroll
+      for (int i = 0; i < 3; ++i) qx[i] = q_of(i);
+      __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        // the dims of k-step ks: as the keys' lanes hold them
-        const int p = BITS == 16 ? 2 * ks + hh : hh * KS + ks;
-        const bf16x8 q = as_bf16x8(ld16(&sm.q[buf][8 * (j * UR + (p ^ (j & 7)))]));
+        const bf16x8 q = as_bf16x8(qx[ks % 3]);
+        if (ks + 3 < KS) {
+          qx[ks % 3] = q_of(ks + 3);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
 #pragma unroll
         for (int t = 0; t < KT; ++t) s[t] = mfma32(q, k[t][ks], s[t]);
+        __builtin_amdgcn_sched_group_barrier(0x008, KT, 0);
       }
-      const bool masked = base + r0 / G < last_key;  // the first row does not see all keys
+      // the first row does not see all keys: positions are looked at
+      auto add = [&](auto masked) {
 #pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4) {
-        if (r0 + 8 * q4 >= rows) break;
-        const f32x4 z = *reinterpret_cast<const f32x4*>(&sm.lse[buf][8 * q4 + 4 * hh]);
+        for (int q4 = 0; q4 < 4; ++q4) {
+          const f32x4 z = *reinterpret_cast<const f32x4*>(&sm.lse[buf][8 * q4 + 4 * hh]);
 #pragma unroll
-        for (int t = 0; t < KT; ++t)
+          for (int t = 0; t < KT; ++t)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float p = fast_exp2(fmaf(s[t][4 * q4 + e], c, -z[e]));
-            if (masked) p = key[t] <= sm.pos[buf][8 * q4 + 4 * hh + e] ? p : 0.f;
-            sum[t] += p;
-          }
-      }
+            for (int e = 0; e < 4; ++e) {
+              float p = fast_exp2(fmaf(s[t][4 * q4 + e], c, -z[e]));
+              if constexpr (decltype(masked)::value) p = key[t] <= sm.pos[buf][8 * q4 + 4 * hh + e] ? p : 0.f;
+              sum[t] += p;
+            }
+        }
+      };
+      if (__builtin_amdgcn_readfirstlane(sm.pos[buf][0]) < last_key) add(std::true_type{});
+      else add(std::false_type{});
       if (more) store_rows(buf ^ 1);
       __syncthreads();
     }
@@ -191,6 +255,127 @@ __global__ __launch_bounds__(256) void attn_weights_kernel(WeightArgs a) {
   }
 }
 
+// A lane's part of a key (16x16x32 MFMA: lane (j, g4) of key j), so that the four lanes of a
+// key read the 64 bytes that lie together: dims 32 ks + 8 g4 over a bf16 cache, (D/4) g4 +
+// 8 ks over a 4-bit one.
+template <int D, int BITS>
+struct KeyRegs16 {
+  static constexpr int KS = D / 32;
+  typedef uint32_t words __attribute__((ext_vector_type(BITS == 16 ? 4 : D / 32)));
+  words x[BITS == 16 ? KS : 1];
+  uint32_t sc;
+  __device__ __forceinline__ void load(const WeightArgs& a, int64_t b, int o, int g4) {
+    if constexpr (BITS == 16) {
+      const __bf16* p = reinterpret_cast<const __bf16*>(a.kc) + b * (kBlock * D) + key_slot_pos(o) * kKeyGroup + 8 * g4;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+        x[ks] = __builtin_nontemporal_load(reinterpret_cast<const words*>(p + ks * (kBlock * kKeyGroup)));
+    } else {
+      x[0] = __builtin_nontemporal_load(reinterpret_cast<const words*>(a.kc + b * (kBlock * D / 2) + o * (D / 2) + g4 * (D / 8)));
+      sc = a.scales[b * ((D / 32 + 1) * kBlock) + (D == 128 ? g4 : g4 >> 1) * kBlock + o];
+    }
+  }
+  __device__ __forceinline__ bf16x8 operand(int ks) const {
+    if constexpr (BITS == 16) return as_bf16x8(x[ks]);
+    else return bf16_of_codes(x[0][ks], sc);
+  }
+  __device__ static __forceinline__ int unit(int ks, int g4) { return BITS == 16 ? 4 * ks + g4 : g4 * KS + ks; }
+};
+
+// Few rows (a decode or verification step): the keys are what takes time.  A wavefront
+// holds 16 NR rows in registers and goes over up to 64 blocks of keys, 32 keys ahead of those
+// that it multiplies; nothing is shared.  Sequences of more rows go over their keys once for
+// each 16 NR.
+template <int D, int BITS, int NR>
+__global__ __launch_bounds__(256) void attn_weights_few_kernel(WeightArgs a) {
+  using Keys = KeyRegs16<D, BITS>;
+  constexpr int KS = Keys::KS;
+  const int lane = threadIdx.x & 63, j = lane & 15, g4 = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int x = blockIdx.x / a.chunks;
+  const int r = x / a.hkv, g = x - r * a.hkv;
+  const SeqRows sr = rows_of(a, r);
+  const int G = a.hq / a.hkv, L = sr.keys;
+  const int32_t* bt = a.bt + (int64_t)r * a.max_blocks;
+  float* wp = a.w + ((int64_t)r * a.hkv + g) * a.w_stride;
+  const float c = a.scale_log2;
+  for (int64_t i = (blockIdx.x - x * a.chunks) * 4 + w; i * a.range < L && sr.rows > 0; i += 4 * a.chunks) {
+    const int k0 = int(i) * a.range, k1 = min(k0 + a.range, L);
+    BlockSpan span;
+    span.init(bt, a.max_blocks, k0 / kBlock);
+    for (int r0 = 0; r0 < sr.rows; r0 += 16 * NR) {
+      const int first_pos = sr.base + r0 / G;
+      bf16x8 q[NR][KS];
+      f32x4 z[NR];
+      int pos[NR][4];
+#pragma unroll
+      for (int n = 0; n < NR; ++n) {
+        // row j, its query as the product's operand, its log-sum-exp and position
+        const int lr = r0 + 16 * n + j, rho = min(lr, sr.rows - 1), qi = rho / G;
+        const int64_t row = (int64_t)(sr.qs + qi) * a.hq + g * G + (rho - qi * G);
+        const float lse = a.lse[row];
+        const bool ok = lr < sr.rows && counts(lse);
+        const float my_z = ok ? lse * kLog2e : __builtin_huge_valf();
+        const int my_pos = sr.base + qi;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const u32x4 v = ld16(a.q + row * D + 8 * Keys::unit(ks, g4));
+          q[n][ks] = as_bf16x8(ok ? v : zero16());
+        }
+        // of rows 4 g4 + e, which the lane's scores belong to
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[n][e] = __shfl(my_z, 4 * g4 + e, 64), pos[n][e] = __shfl(my_pos, 4 * g4 + e, 64);
+      }
+      Keys k[2][2];
+      auto load = [&](int t0, int s) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const int key = min(t0 + 16 * t + j, k1 - 1);
+          const int id = span.get(min(t0 / kBlock + t, (k1 - 1) / kBlock));
+          k[s][t].load(a, (int64_t)clamp_block(id, a.num_blocks) * a.hkv + g, key % kBlock, g4);
+        }
+      };
+      auto step = [&](int t0, auto b) {
+        constexpr int cur = decltype(b)::value;
+        if (t0 + 32 < k1) load(t0 + 32, 1 - cur);
+        const bool masked = t0 + 31 > first_pos;
+        float sum[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          f32x4 s[NR];
+#pragma unroll
+          for (int n = 0; n < NR; ++n) s[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) {
+            const bf16x8 x = k[cur][t].operand(ks);
+#pragma unroll
+            for (int n = 0; n < NR; ++n) s[n] = mfma16(q[n][ks], x, s[n]);
+          }
+          sum[t] = 0.f;
+#pragma unroll
+          for (int n = 0; n < NR; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float p = fast_exp2(fmaf(s[n][e], c, -z[n][e]));
+              if (masked) p = t0 + 16 * t + j <= pos[n][e] ? p : 0.f;
+              sum[t] += p;
+            }
+          sum[t] += wave_xor(sum[t], 16);
+          sum[t] += wave_xor(sum[t], 32);
+        }
+        const int key = t0 + lane;
+        const float s = lane < 16 ? sum[0] : sum[1];
+        if (lane < 32 && key < k1) wp[key] = a.add || r0 > 0 ? wp[key] + s : s;
+      };
+      load(k0, 0);
+      for (int t0 = k0; t0 < k1; t0 += 64) {
+        step(t0, std::integral_constant<int, 0>{});
+        if (t0 + 32 < k1) step(t0 + 32, std::integral_constant<int, 1>{});
+      }
+    }
+  }
+}
+
 }  // namespace
 
 int launch_attn_weights(const void* q, const float* lse, const void* kc, const uint8_t* scales,
@@ -199,31 +384,42 @@ int launch_attn_weights(const void* q, const float* lse, const void* kc, const u
                         int32_t hq, int32_t hkv, int32_t d, int32_t bits, float scale, float* w,
                         int64_t w_stride, bool add, hipStream_t stream) {
   WeightArgs a{static_cast<const __bf16*>(q), lse, static_cast<const uint8_t*>(kc), scales, bt, seq_lens,
-               cu, w, w_stride, max_blocks, num_blocks, total_q, hq, hkv, 0, scale * kLog2e, add};
+               cu, w, w_stride, max_blocks, num_blocks, total_q, hq, hkv, 0, 0, scale * kLog2e, add};
   const int64_t heads = int64_t(n_seqs) * hkv, keys = min(w_stride, int64_t(max_blocks) * kBlock);
-  const bool wide = int64_t(total_q) * (hq / hkv) > 32 * int64_t(n_seqs);
-  const int64_t chunk = wide ? 256 : 128;
-  int64_t chunks = (keys + chunk - 1) / chunk;
+  // Rows of a kv-head, of the average sequence.  32 sequences of 2048-8192 keys, 32/8 heads:
+  // bf16 16 rows 61 us (through LDS 94), 32 rows 67 (96), 64 rows 90 (103), 4 bits 30 (48), 42
+  // (49), 76 (59).
+  const int64_t rows = (int64_t(total_q) * (hq / hkv) + n_seqs - 1) / n_seqs;
+  const bool many = rows > (bits == 16 ? 64 : 32);
+  int64_t chunk = 256;  // keys of a workgroup
+  if (!many) {
+    // wavefronts of as many keys as leave enough of them to fill the chip
+    a.range = int32_t(max(int64_t(1), min(int64_t(32), keys * heads / (32 * kFewWaves)))) * 32;
+    chunk = 4 * a.range;
+  }
   // few workgroups without keys where the array is wider than the sequences are long
-  chunks = min(chunks, max(int64_t(1), 32768 / heads));
+  const int64_t chunks = min((keys + chunk - 1) / chunk, max(int64_t(1), 32768 / heads));
   if (heads * chunks > INT32_MAX) return static_cast<int>(hipErrorInvalidValue);
   a.chunks = int32_t(chunks);
   const dim3 grid(unsigned(heads * chunks));
-#define PA_W(DD, BB, KK) hipLaunchKernelGGL((attn_weights_kernel<DD, BB, KK>), grid, dim3(256), 0, stream, a)
-#define PA_W_BITS(DD)                 \
-  if (bits == 16) {                   \
-    if (wide) PA_W(DD, 16, 2);        \
-    else PA_W(DD, 16, 1);             \
-  } else {                            \
-    if (wide) PA_W(DD, 4, 2);         \
-    else PA_W(DD, 4, 1);              \
+#define PA_W(...) hipLaunchKernelGGL((__VA_ARGS__), grid, dim3(256), 0, stream, a)
+#define PA_W_ROWS(DD, BB)                                                     \
+  {                                                                           \
+    if (many) PA_W(attn_weights_kernel<DD, BB>);                              \
+    else if (BB == 16 && rows > 32) PA_W(attn_weights_few_kernel<DD, 16, 4>); \
+    else if (rows > 16) PA_W(attn_weights_few_kernel<DD, BB, 2>);              \
+    else PA_W(attn_weights_few_kernel<DD, BB, 1>);                            \
   }
+#define PA_W_BITS(DD)               \
+  if (bits == 16) PA_W_ROWS(DD, 16) \
+  else PA_W_ROWS(DD, 4)
   if (d == 128) {
     PA_W_BITS(128)
   } else {
     PA_W_BITS(64)
   }
 #undef PA_W_BITS
+#undef PA_W_ROWS
 #undef PA_W
   return static_cast<int>(hipGetLastError());
 }
