@@ -54,84 +54,106 @@ __device__ __forceinline__ uint32_t order_of(float x) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-constexpr int kSelectThreads = 1024;
-constexpr int kSelectWaves = kSelectThreads / 64;
+constexpr int kHeld = 16;  // weights of a thread that stay in registers
 
-__global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs a) {
-  __shared__ int hist[2048];
-  __shared__ int part[2][kSelectWaves];
-  __shared__ int found[2];
+// NT threads (256 where rows of weights are short: its barriers are cheaper).  A wavefront
+// takes an even share of the positions, 64 at a time; up to 16 NT of them are read once, all
+// loads issued together, further ones in each pass again.
+template <int NT>
+__global__ __launch_bounds__(NT) void evict_select_kernel(EvictArgs a) {
+  constexpr int kWaves = NT / 64, kBinsPer = 2048 / NT;
+  __shared__ int hist[3][2048];
+  __shared__ int part[2][kWaves];
+  __shared__ int found[3][2];
   const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = blockIdx.x / a.hkv;
   const Lens n = lens_of(a, r);
   if (n.keep == 0) return;
   const float* w = a.w + blockIdx.x * a.w_stride;
+  float* out = a.w_out + blockIdx.x * a.w_stride;
   int32_t* kept = a.kept + blockIdx.x * a.kept_stride;
   const int lo = n.front, hi = n.len - n.window;  // candidates
   const int want = n.keep - n.front - n.window;
+  const int share = (n.len + NT - 1) / NT * 64;
+  const int p0 = min(wv * share, n.len), p1 = min(p0 + share, n.len);
+
+  float held[kHeld];
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k) held[k] = w[max(min(p0 + 64 * k + lane, p1 - 1), 0)];
+  // f(position, weight) for the wavefront's positions, 64 at a time
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+      if (p0 + 64 * k < p1) f(p0 + 64 * k + lane, held[k]);
+    for (int i = p0 + 64 * kHeld + lane; i - lane < p1; i += 64) f(i, w[min(i, p1 - 1)]);
+  };
 
   // The want-th largest candidate T, and how many of those equal to it stay.
   uint32_t T = 0;
   int ties = 0;
   if (want > 0) {
+    for (int i = tid; i < 3 * 2048; i += NT) hist[i / 2048][i % 2048] = 0;
+    __syncthreads();
     int left = want;
     uint32_t prefix = 0, known = 0;  // T's bits found so far, and which
-    constexpr int kShift[3] = {21, 10, 0}, kBins[3] = {2048, 2048, 1024};
+    constexpr int kShift[3] = {21, 10, 0}, kMask[3] = {2047, 2047, 1023};
+#pragma unroll
     for (int d = 0; d < 3; ++d) {
-      for (int i = tid; i < 2048; i += kSelectThreads) hist[i] = 0;
+      each([&](int i, float x) {
+        const uint32_t u = order_of(x);
+        if (i >= lo && i < hi && (u & known) == prefix) atomicAdd(&hist[d][u >> kShift[d] & kMask[d]], 1);
+      });
       __syncthreads();
-      for (int i = lo + tid; i < hi; i += kSelectThreads) {
-        const uint32_t u = order_of(w[i]);
-        if ((u & known) == prefix) atomicAdd(&hist[u >> kShift[d] & (kBins[d] - 1)], 1);
+      // Counts from the largest digit down, kBinsPer of them a thread.
+      int h[kBinsPer], mine = 0;
+#pragma unroll
+      for (int q = 0; q < kBinsPer; ++q) {
+        h[q] = hist[d][2047 - kBinsPer * tid - q];
+        mine += h[q];
       }
-      __syncthreads();
-      // Counts from the largest digit down: thread t holds digits 2047 - 2 t and the one
-      // below (of 1024 digits the larger half is empty).
-      const int b = 2047 - 2 * tid;
-      const int h0 = hist[b], h1 = hist[b - 1];
-      int sum = h0 + h1;
+      int sum = mine;
 #pragma unroll
       for (int m = 1; m < 64; m <<= 1) {
         const int o = __shfl_up(sum, m, 64);
         if (lane >= m) sum += o;
       }
-      if (lane == 63) part[0][wv] = sum;
+      if (lane == 63) part[d & 1][wv] = sum;
       __syncthreads();
-      int before = sum - h0 - h1;
-      for (int v = 0; v < wv; ++v) before += part[0][v];
+      int before = sum - mine;
+      for (int v = 0; v < wv; ++v) before += part[d & 1][v];
       // the digit where the count reaches `left`
-      if (before < left && before + h0 + h1 >= left) {
-        const bool low = before + h0 < left;
-        found[0] = low ? b - 1 : b;
-        found[1] = left - before - (low ? h0 : 0);
+      if (before < left && before + mine >= left) {
+#pragma unroll
+        for (int q = 0; q < kBinsPer; ++q) {
+          if (before < left && before + h[q] >= left) found[d][0] = 2047 - kBinsPer * tid - q, found[d][1] = left - before;
+          before += h[q];
+        }
       }
       __syncthreads();
-      prefix |= uint32_t(found[0]) << kShift[d];
-      known |= uint32_t(kBins[d] - 1) << kShift[d];
-      left = found[1];
-      __syncthreads();
+      prefix |= uint32_t(found[d][0]) << kShift[d];
+      known |= uint32_t(kMask[d]) << kShift[d];
+      left = found[d][1];
     }
     T = prefix;
     ties = left;
   }
 
-  // A wavefront takes an even share of the positions: how many stay of it, and how many
-  // equal T.
-  const int share = (n.len + kSelectThreads - 1) / kSelectThreads * 64;
-  const int p0 = min(wv * share, n.len), p1 = min(p0 + share, n.len);
+  // How many of a wavefront's positions stay, and how many equal T.
   // 0: goes, 1: equals T, 2: stays
-  auto kind = [&](int i) {
+  auto kind = [&](int i, float x) {
+    if (i >= p1) return 0;
     if (i < lo || i >= hi) return 2;
     if (want <= 0) return 0;
-    const uint32_t u = order_of(w[i]);
+    const uint32_t u = order_of(x);
     return u > T ? 2 : u == T ? 1 : 0;
   };
   int stay = 0, equal = 0;
-  for (int i0 = p0; i0 < p1; i0 += 64) {
-    const int k = i0 + lane < p1 ? kind(i0 + lane) : 0;
+  each([&](int i, float x) {
+    const int k = kind(i, x);
     stay += __popcll(__ballot(k == 2));
     equal += __popcll(__ballot(k == 1));
-  }
+  });
+  __syncthreads();  // the last digit's counts have been read
   if (lane == 0) part[0][wv] = stay, part[1][wv] = equal;
   __syncthreads();
   int at = 0, eq = 0;  // kept, and equal ones, before this wavefront's
@@ -140,19 +162,23 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
     eq += part[1][v];
   }
   const uint64_t below = (uint64_t(1) << lane) - 1;
-  for (int i0 = p0; i0 < p1; i0 += 64) {
-    const int k = i0 + lane < p1 ? kind(i0 + lane) : 0;
+  each([&](int i, float x) {
+    const int k = kind(i, x);
     const uint64_t e = __ballot(k == 1);
     const bool keep = k == 2 || (k == 1 && eq + __popcll(e & below) < ties);
     const uint64_t m = __ballot(keep);
-    if (keep) kept[at + __popcll(m & below)] = i0 + lane;
+    if (keep) {
+      const int to = at + __popcll(m & below);
+      kept[to] = i;
+      if (w != out) out[to] = x;
+    }
     at += __popcll(m);
     eq += __popcll(e);
-  }
+  });
+  if (w != out) return;
   __syncthreads();
-  // The weights move, in place: a thousand are read before they are written.
-  float* out = a.w_out + blockIdx.x * a.w_stride;
-  for (int i0 = 0; i0 < n.keep; i0 += kSelectThreads) {
+  // In place, NT weights are read before they are written.
+  for (int i0 = 0; i0 < n.keep; i0 += NT) {
     const int i = i0 + tid;
     float x = 0.f;
     if (i < n.keep) x = w[kept[i]];
@@ -183,6 +209,9 @@ struct Moved {
     const int id = clamp_block(bt[my / kBlock], a.num_blocks);
     auto block_of = [&](int o) { return (int64_t)__shfl(id, o, 64) * a.hkv + g; };
     auto off_of = [&](int o) { return __shfl(my, o, 64) % kBlock; };
+    // of token t, in scalar registers: all lanes read that token's values
+    auto block_at = [&](int t) { return (int64_t)__builtin_amdgcn_readlane(id, t) * a.hkv + g; };
+    auto off_at = [&](int t) { return __builtin_amdgcn_readlane(my, t) % kBlock; };
     if constexpr (KV4) {
       constexpr int U = D / 32;  // 16-byte units of a token's key
       const int o = lane / U % kBlock;
@@ -200,15 +229,15 @@ struct Moved {
       v4 = zero16();
 #pragma unroll
       for (int t = 0; t < kBlock; ++t) {
-        const int64_t vb = block_of(t);
-        const int off = off_of(t);
-        if (lane < D / 2) {
-          const u32x4 x = ld16(a.vc + vb * kHeadBytes + 16 * lane);
-          const uint32_t c0 = (off < 8 ? x[0] : x[1]) >> (4 * (off & 7)) & 15;
-          const uint32_t c1 = (off < 8 ? x[2] : x[3]) >> (4 * (off & 7)) & 15;
-          v4[t / 8] |= c0 << (4 * (t & 7));
-          v4[2 + t / 8] |= c1 << (4 * (t & 7));
-        }
+        // the token's block, two dims of all its tokens a lane: neighbouring tokens find it in
+        // the cache (64 requests, 65000 tokens moved, 28 us; loads of the halves that hold the
+        // token 44, all 16 loads before the first use 29)
+        const u32x4 x = ld16(a.vc + block_at(t) * kHeadBytes + 16 * (lane % (D / 2)));
+        const int off = off_at(t);
+        const uint32_t c0 = (off < 8 ? x[0] : x[1]) >> (4 * (off & 7)) & 15;
+        const uint32_t c1 = (off < 8 ? x[2] : x[3]) >> (4 * (off & 7)) & 15;
+        v4[t / 8] |= c0 << (4 * (t & 7));
+        v4[2 + t / 8] |= c1 << (4 * (t & 7));
       }
     } else {
       constexpr int U = 2 * ELEM;  // units of a token's 32 dims
@@ -220,7 +249,7 @@ struct Moved {
       }
 #pragma unroll
       for (int t = 0; t < kBlock; ++t) {
-        const T* p = reinterpret_cast<const T*>(a.vc + block_of(t) * kHeadBytes) + off_of(t);
+        const T* p = reinterpret_cast<const T*>(a.vc + block_at(t) * kHeadBytes) + off_at(t);
 #pragma unroll
         for (int i = 0; i < NV; ++i) v[i][t] = p[(64 * i + lane) * kBlock];
       }
@@ -326,7 +355,10 @@ int launch_kv_evict(const float* w, float* w_out, int64_t w_stride, const int32_
   const int64_t groups = (blocks + 3) / 4;
   if (heads * max(groups, int64_t(1)) > INT32_MAX) return static_cast<int>(hipErrorInvalidValue);
   a.groups = int32_t(groups);
-  hipLaunchKernelGGL(evict_select_kernel, dim3(unsigned(heads)), dim3(kSelectThreads), 0, stream, a);
+  if (w_stride <= 16 * 256)
+    hipLaunchKernelGGL(evict_select_kernel<256>, dim3(unsigned(heads)), dim3(256), 0, stream, a);
+  else
+    hipLaunchKernelGGL(evict_select_kernel<1024>, dim3(unsigned(heads)), dim3(1024), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || groups == 0) return static_cast<int>(e);
 #define PA_MOVE(DD, EE)                                                                              \
