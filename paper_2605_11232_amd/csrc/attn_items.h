@@ -574,6 +574,13 @@ __device__ __forceinline__ void tile_item(const int32_t* it, int g, int poff, co
           p[u][e >> 3][e & 7] = (__bf16)times_scale(x, sv[k]);
           (e < 8 ? l0 : l1) += x;
         }
+        // formed here: behind the look at the sum, exponentials and scales would all wait
+        // in registers
+        if (i % 2) {
+          u32x4 t = __builtin_bit_cast(u32x4, p[i / 4][i % 4 / 2]);
+          asm volatile("" : "+v"(t), "+v"(l0), "+v"(l1));
+          p[i / 4][i % 4 / 2] = as_bf16x8(t);
+        }
       }
       return l0 + l1;
     } else if constexpr (KV8) {
@@ -1077,9 +1084,10 @@ __device__ __forceinline__ void store_row(const AttnArgs& a, const f32x4 (&acc)[
 // A operand of the PV product (16 keys of dimension 16 dt + j: two k-steps).  The
 // score's k-steps take dims 64 c + 16 g4 + 8 u .. + 7, the halves u of a lane's load.
 // The 4-bit cache: a lane takes 16 bytes of a key (head_dim 64: 8) that share a scale, and
-// 16 keys of dims 32 i + j and 32 i + 16 + j.  Row j of score tile tt is token 4 (j % 4) +
-// tt of block j / 4, so that one word holds a lane's four key scales; its score elements are
-// keys 4 e + tt.
+// 16 keys of dims 32 i + j and 32 i + 16 + j.  Score tiles hold the same tokens: four
+// neighbouring ones' keys are 256 contiguous bytes of a load (of tokens 4 apart, 64 bytes
+// at a time, 64 sequences of 2000-8000 keys at head_dim 64 took 56 us instead of 44, 32 of
+// 4000-8000 28/4 heads 31 and 27.5).
 // With kItemJoin the workgroup's four wavefronts hold the same rows over adjacent
 // keys: they leave their accumulators, references and sums in LDS, and each combines a
 // quarter of the output dims and writes them.
@@ -1143,7 +1151,8 @@ __device__ __forceinline__ void row_item8(const int32_t* it, int g, int poff, co
   // AHEAD: two register sets of K and V^T; a step loads the next one's before it uses its
   // own, so a whole step hides the memory's latency (24 sequences of 8192-20480 keys 121
   // us, 5.9 TB/s, against 145 with one set and three wavefronts per SIMD instead of two).
-  // Beside tiles or two-tile items, which leave two wavefronts anyway, one set, reloaded
+  // At head_dim 64 over the 4-bit cache one set is enough (64 sequences of 2000-8000 keys 39
+  // us, 44 with two).  Beside tiles or two-tile items, which leave two wavefronts anyway, one set, reloaded
   // as in row_item, is as good or better: 128 decode requests on 4096 shared keys 48.6 us,
   // 51.1 with two, 32 verifications on 16384 158 and 170 (an item ahead of the other that
   // reads its keys finds them in no cache).  Blocks at or past kv1 read the item's last
@@ -1171,24 +1180,23 @@ __device__ __forceinline__ void row_item8(const int32_t* it, int g, int poff, co
   constexpr int KR = KV4 ? 1 : KC, VR = KV4 ? DT / 2 : DT;
   u32x4 kreg[NB][4][KR], vreg[NB][VR];
   uint32_t ek[NB] = {}, ev[NB] = {};
-  u32x4 ev4[NB];  // KV4: scales of a block's 16 values
+  u32x4 ek4[NB], ev4[NB];  // KV4: scales of a block's 16 keys (of the lane's dims) and values
   auto load_k = [&](int t0, int s) {
     const int64_t b = block_of(t0 / kBlock + (j >> 2));
     if constexpr (KV4) {
-      const uint8_t* p = kc + b * (kBlock * D / 2) + 4 * (j & 3) * (D / 2) + g4 * (D / 8);
+      const uint8_t* p = kc + b * (kBlock * D / 2) + (j & 3) * (D / 2) + g4 * (D / 8);
 #pragma unroll
       for (int tt = 0; tt < 4; ++tt) {
         if constexpr (D == 128) {
-          kreg[s][tt][0] = raw16(p + tt * (D / 2));
+          kreg[s][tt][0] = raw16(p + 4 * tt * (D / 2));
         } else {
           u32x2 x;
-          if constexpr (TWICE) x = *reinterpret_cast<const u32x2*>(p + tt * (D / 2));
-          else x = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p + tt * (D / 2)));
+          if constexpr (TWICE) x = *reinterpret_cast<const u32x2*>(p + 4 * tt * (D / 2));
+          else x = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p + 4 * tt * (D / 2)));
           kreg[s][tt][0][0] = x[0], kreg[s][tt][0][1] = x[1];
         }
       }
-      ek[s] = *reinterpret_cast<const uint32_t*>(
-          a.scales + b * (kScaleRows * kBlock) + (D == 128 ? g4 : g4 >> 1) * kBlock + 4 * (j & 3));
+      ek4[s] = ld16(a.scales + b * (kScaleRows * kBlock) + (D == 128 ? g4 : g4 >> 1) * kBlock);
       return;
     }
     const uint8_t* p = kc + b * (kBlock * D) + (j & 3) * 64 + 16 * g4;
@@ -1237,7 +1245,7 @@ __device__ __forceinline__ void row_item8(const int32_t* it, int g, int poff, co
       for (int ks = 0; ks < 2 * KC; ++ks) {
         bf16x8 k;
         if constexpr (KV4) {
-          k = as_bf16x8(bf16_of_e2m1(kreg[cur][tt][0][ks], exponent_byte(ek[cur], tt)));
+          k = as_bf16x8(bf16_of_e2m1(kreg[cur][tt][0][ks], exponent_byte(ek4[cur][tt] >> (8 * (j & 3)), 0)));
         } else {
           const u32x4 x = kreg[cur][tt][ks / 2];
           k = as_bf16x8(bf16_of_e4m3(x[2 * (ks % 2)], x[2 * (ks % 2) + 1], sk));
@@ -1247,8 +1255,7 @@ __device__ __forceinline__ void row_item8(const int32_t* it, int g, int poff, co
       }
     }
     if (!AHEAD && more) load_k(t0 + kStep, next);
-    // Lane (j, g4), element e of score tile tt holds key t0 + 16 g4 + key_of(tt, e).
-    auto key_of = [](int tt, int e) { return KV4 ? 4 * e + tt : 4 * tt + e; };
+    // Lane (j, g4), element e of score tile tt holds key t0 + 16 g4 + 4 tt + e.
     const bool masked = t0 + kStep - 1 > amin || !more;  // wave-uniform
     if (masked) {
 #pragma unroll
@@ -1257,7 +1264,7 @@ __device__ __forceinline__ void row_item8(const int32_t* it, int g, int poff, co
         for (int tt = 0; tt < 4; ++tt)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const int key = t0 + 16 * g4 + key_of(tt, e);
+            const int key = t0 + 16 * g4 + 4 * tt + e;
             s[c][tt][e] = (key <= apos[c] && key < kv1) ? s[c][tt][e] : kNegInf;
           }
       // zero values of keys at or past kv1 (slots that may never have been written); KV4:
@@ -1296,11 +1303,10 @@ __device__ __forceinline__ void row_item8(const int32_t* it, int g, int poff, co
         for (int e = 0; e < 4; ++e) {
           const float p = fast_exp2(fmaf(s[c][tt][e], cs, -mc[c]));
           l[c] += p;
-          const int key = key_of(tt, e);
           if constexpr (KV4)
-            pb[c][key >> 3][key & 7] = (__bf16)times_scale(p, scale8(ev4[cur][key >> 2] >> (8 * (key & 3)) & 255));
+            pb[c][tt >> 1][4 * (tt & 1) + e] = (__bf16)times_scale(p, scale8(ev4[cur][tt] >> (8 * e) & 255));
           else
-            pb[c][key >> 3][key & 7] = (__bf16)p;  // as in a tile's exps
+            pb[c][tt >> 1][4 * (tt & 1) + e] = (__bf16)p;  // as in a tile's exps
         }
     }
     const float sv = scale8(ev[cur]);
@@ -1413,7 +1419,6 @@ __device__ __forceinline__ void row_item8(const int32_t* it, int g, int poff, co
 // loaded outside the key loops, at head_dim 64 also once per item of the tail lists.
 template <int D, int MIX, int BITS>
 constexpr int waves_per_eu() {
-  if (BITS == 4 && (MIX & 1)) return kTileWavesPerEu;
   return (MIX == 2 && BITS == 16) || D == 64 ? 3 : kTileWavesPerEu;
 }
 
@@ -1551,7 +1556,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(waves_per_e
             return;
           }
         }
-        row_item8<D, 1, BITS, MIX == 2, false>(it, g, poff, a, join, stat8);
+        row_item8<D, 1, BITS, MIX == 2 && !(BITS == 4 && D == 64), false>(it, g, poff, a, join, stat8);
       } else {
         row_item<D, 1>(it, g, poff, a);
       }
