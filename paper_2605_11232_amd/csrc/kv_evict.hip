@@ -188,86 +188,85 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(EvictArgs a) {
   }
 }
 
-// One block's kept tokens on their way: 16 tokens of a (sequence, kv-head).
-// ELEM: bytes of a value (4, 2), or 0 for the 4-bit cache.
-template <int D, int ELEM>
+// One block's kept tokens on their way: 16 tokens of a (sequence, kv-head), NS slices from
+// slice s0 on: keys and values of 32 dims each; of the 4-bit cache (ELEM 0; else a value's
+// bytes) slice 0 is the keys and scales, slice 1 the values.
+template <int D, int ELEM, int NS>
 struct Moved {
   static constexpr bool KV4 = ELEM == 0;
   static constexpr int kHeadBytes = KV4 ? kBlock * D / 2 : kBlock * D * ELEM;
-  static constexpr int NK = (kHeadBytes / 16 + 63) / 64;  // 16-byte loads of keys a lane
   static constexpr int kScaleRows = D / 32 + 1;
-  static constexpr int NV = KV4 ? 1 : D / 64;             // dims of values a lane
+  static constexpr int U = KV4 ? D / 32 : 2 * ELEM;  // 16-byte units of a token's (32 dims') key
+  static constexpr int NK = KV4 ? 1 : U * kBlock / 64;  // loads of a slice's keys
   typedef typename std::conditional<ELEM == 4, uint32_t, uint16_t>::type T;
-  u32x4 k[NK];
+  struct alignas(16) Half { T x[kBlock / 2]; };      // 8 tokens of a dim
+  u32x4 k[KV4 ? 1 : NS][NK];
   u32x4 v4;                     // KV4: dims 32 c + i and 32 c + 16 + i
-  T v[KV4 ? 1 : NV][kBlock];
+  Half v[KV4 ? 1 : NS];         // lane (dim, half): dim 32 s + lane % 32
   uint32_t s[2];                // KV4: scale bytes
 
-  // Source positions of the block's tokens: lane o < 16 holds token o's.
-  __device__ __forceinline__ void load(const EvictArgs& a, int g, int pos, const int32_t* bt, int lane) {
-    const int my = pos < 0 ? 0 : pos;
-    const int id = clamp_block(bt[my / kBlock], a.num_blocks);
+  // pos: old position of the block's token lane % 16.
+  __device__ __forceinline__ void load(const EvictArgs& a, int g, int s0, int pos, const int32_t* bt, int lane) {
+    const int id = clamp_block(bt[pos / kBlock], a.num_blocks);
     auto block_of = [&](int o) { return (int64_t)__shfl(id, o, 64) * a.hkv + g; };
-    auto off_of = [&](int o) { return __shfl(my, o, 64) % kBlock; };
-    // of token t, in scalar registers: all lanes read that token's values
-    auto block_at = [&](int t) { return (int64_t)__builtin_amdgcn_readlane(id, t) * a.hkv + g; };
-    auto off_at = [&](int t) { return __builtin_amdgcn_readlane(my, t) % kBlock; };
+    auto off_of = [&](int o) { return __shfl(pos, o, 64) % kBlock; };
     if constexpr (KV4) {
-      constexpr int U = D / 32;  // 16-byte units of a token's key
-      const int o = lane / U % kBlock;
-      const int64_t b = block_of(o);
-      k[0] = zero16();
-      if (lane < kBlock * U) k[0] = ld16(a.kc + b * kHeadBytes + off_of(o) * (D / 2) + lane % U * 16);
+      if (NS > 1 || s0 == 0) {
+        const int o = lane / U % kBlock;
+        k[0][0] = ld16(a.kc + block_of(o) * kHeadBytes + off_of(o) * (D / 2) + lane % U * 16);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int u = 64 * i + lane, so = u % kBlock;
-        const int64_t sb = block_of(so);
-        const int off = off_of(so);
-        s[i] = 0;
-        if (u < kScaleRows * kBlock) s[i] = a.scales[sb * (kScaleRows * kBlock) + u / kBlock * kBlock + off];
+        for (int i = 0; i < 2; ++i) {
+          const int u = min(64 * i + lane, kScaleRows * kBlock - 1), so = u % kBlock;
+          s[i] = a.scales[block_of(so) * (kScaleRows * kBlock) + u / kBlock * kBlock + off_of(so)];
+        }
       }
-      v4 = zero16();
+      if (NS > 1 || s0 == 1) {
+        v4 = zero16();
 #pragma unroll
-      for (int t = 0; t < kBlock; ++t) {
-        // the token's block, two dims of all its tokens a lane: neighbouring tokens find it in
-        // the cache (64 requests, 65000 tokens moved, 28 us; loads of the halves that hold the
-        // token 44, all 16 loads before the first use 29)
-        const u32x4 x = ld16(a.vc + block_at(t) * kHeadBytes + 16 * (lane % (D / 2)));
-        const int off = off_at(t);
-        const uint32_t c0 = (off < 8 ? x[0] : x[1]) >> (4 * (off & 7)) & 15;
-        const uint32_t c1 = (off < 8 ? x[2] : x[3]) >> (4 * (off & 7)) & 15;
-        v4[t / 8] |= c0 << (4 * (t & 7));
-        v4[2 + t / 8] |= c1 << (4 * (t & 7));
+        for (int t = 0; t < kBlock; ++t) {
+          // The token's block, two dims of all its tokens a lane: neighbouring tokens find it
+          // in the cache (64 requests, 32000 tokens moved, 28 us; loads of the halves that
+          // hold the token 44, all 16 loads before the first use 29).
+          const int64_t b = (int64_t)__builtin_amdgcn_readlane(id, t) * a.hkv + g;
+          const int off = __builtin_amdgcn_readlane(pos, t) % kBlock;
+          const u32x4 x = ld16(a.vc + b * kHeadBytes + 16 * (lane % (D / 2)));
+          const uint32_t c0 = (off < 8 ? x[0] : x[1]) >> (4 * (off & 7)) & 15;
+          const uint32_t c1 = (off < 8 ? x[2] : x[3]) >> (4 * (off & 7)) & 15;
+          v4[t / 8] |= c0 << (4 * (t & 7));
+          v4[2 + t / 8] |= c1 << (4 * (t & 7));
+        }
       }
     } else {
-      constexpr int U = 2 * ELEM;  // units of a token's 32 dims
 #pragma unroll
       for (int i = 0; i < NK; ++i) {
-        const int u = 64 * i + lane, o = u / U % kBlock, grp = u / (U * kBlock);
-        const int64_t b = block_of(o);
-        k[i] = ld16(a.kc + b * kHeadBytes + (grp * kBlock + key_slot_pos(off_of(o))) * (32 * ELEM) + u % U * 16);
+        const int u = 64 * i + lane, o = u / U;
+        const uint8_t* p = a.kc + block_of(o) * kHeadBytes + key_slot_pos(off_of(o)) * (32 * ELEM) + u % U * 16;
+#pragma unroll
+        for (int n = 0; n < NS; ++n) k[n][i] = ld16(p + (s0 + n) * (kBlock * 32 * ELEM));
       }
 #pragma unroll
-      for (int t = 0; t < kBlock; ++t) {
-        const T* p = reinterpret_cast<const T*>(a.vc + block_at(t) * kHeadBytes) + off_at(t);
+      for (int t = 0; t < kBlock / 2; ++t) {
+        const int o = lane / 32 * (kBlock / 2) + t;
+        const T* p = reinterpret_cast<const T*>(a.vc + block_of(o) * kHeadBytes) + (32 * s0 + lane % 32) * kBlock + off_of(o);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) v[i][t] = p[(64 * i + lane) * kBlock];
+        for (int n = 0; n < NS; ++n) v[n].x[t] = p[32 * n * kBlock];
       }
     }
   }
 
   // The first `count` tokens, to block `id`.
-  __device__ __forceinline__ void store(const EvictArgs& a, int g, int id, int count, int lane) const {
+  __device__ __forceinline__ void store(const EvictArgs& a, int g, int s0, int id, int count, int lane) const {
     const int64_t b = (int64_t)id * a.hkv + g;
     if constexpr (KV4) {
-      constexpr int U = D / 32;
-      if (lane < kBlock * U && lane / U < count) st16(a.kc + b * kHeadBytes + lane * 16, k[0]);
+      if (NS > 1 || s0 == 0) {
+        if (lane < kBlock * U && lane / U < count) st16(a.kc + b * kHeadBytes + lane * 16, k[0][0]);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int u = 64 * i + lane;
-        if (u < kScaleRows * kBlock && u % kBlock < count) a.scales[b * (kScaleRows * kBlock) + u] = uint8_t(s[i]);
+        for (int i = 0; i < 2; ++i) {
+          const int u = 64 * i + lane;
+          if (u < kScaleRows * kBlock && u % kBlock < count) a.scales[b * (kScaleRows * kBlock) + u] = uint8_t(s[i]);
+        }
       }
-      if (lane < D / 2) {
+      if ((NS > 1 || s0 == 1) && lane < D / 2) {
         u32x4* p = reinterpret_cast<u32x4*>(a.vc + b * kHeadBytes) + lane;
         u32x4 x = v4;
         if (count < kBlock) {
@@ -282,38 +281,43 @@ struct Moved {
         *p = x;
       }
     } else {
-      constexpr int U = 2 * ELEM;
 #pragma unroll
       for (int i = 0; i < NK; ++i) {
-        const int u = 64 * i + lane, o = u / U % kBlock, grp = u / (U * kBlock);
-        if (o < count) st16(a.kc + b * kHeadBytes + (grp * kBlock + key_slot_pos(o)) * (32 * ELEM) + u % U * 16, k[i]);
+        const int u = 64 * i + lane, o = u / U;
+        uint8_t* p = a.kc + b * kHeadBytes + key_slot_pos(o) * (32 * ELEM) + u % U * 16;
+        if (o < count) {
+#pragma unroll
+          for (int n = 0; n < NS; ++n) st16(p + (s0 + n) * (kBlock * 32 * ELEM), k[n][i]);
+        }
       }
-      T* vb = reinterpret_cast<T*>(a.vc + b * kHeadBytes);
+      const int first = lane / 32 * (kBlock / 2);
+      T* p = reinterpret_cast<T*>(a.vc + b * kHeadBytes) + (32 * s0 + lane % 32) * kBlock + first;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        T* p = vb + (64 * i + lane) * kBlock;
-        if (count == kBlock) {
-          struct alignas(16) Row { T x[kBlock]; } row;
-#pragma unroll
-          for (int t = 0; t < kBlock; ++t) row.x[t] = v[i][t];
-          *reinterpret_cast<Row*>(p) = row;
+      for (int n = 0; n < NS; ++n) {
+        if (count >= first + kBlock / 2) {
+          *reinterpret_cast<Half*>(p + 32 * n * kBlock) = v[n];
         } else {
 #pragma unroll
-          for (int t = 0; t < kBlock; ++t)
-            if (t < count) p[t] = v[i][t];
+          for (int t = 0; t < kBlock / 2; ++t)
+            if (first + t < count) p[32 * n * kBlock + t] = v[n].x[t];
         }
       }
     }
   }
 };
 
-// IN_PLACE: one workgroup per (sequence, kv-head), 16 blocks at a time; else one per four
-// blocks.
-template <int D, int ELEM, bool IN_PLACE>
+// To other blocks: one workgroup per four blocks.  In place: one per (sequence, kv-head),
+// which takes 16 blocks at a time, or, SLICED, per slice of it: slices do not wait for each
+// other.  Sliced is faster while the workgroups do not fill the chip (one context of 16000
+// tokens to a quarter, 8 kv-heads, 300 -> 107 us, 16 of 11000 tokens 325 -> 201), and slower
+// where they do (64 of 1500 tokens over the 4-bit cache 40 -> 50).
+template <int D, int ELEM, bool IN_PLACE, bool SLICED = false>
 __global__ __launch_bounds__(IN_PLACE ? 1024 : 256) void evict_move_kernel(EvictArgs a) {
   constexpr int kWaves = IN_PLACE ? 16 : 4;
+  constexpr int kAll = ELEM == 0 ? 2 : D / 32, kSlices = SLICED ? kAll : 1, NS = SLICED ? 1 : kAll;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int x = IN_PLACE ? blockIdx.x : blockIdx.x / a.groups;
+  const int x = IN_PLACE ? blockIdx.x / kSlices : blockIdx.x / a.groups;
+  const int s0 = SLICED ? blockIdx.x - x * kSlices : 0;
   const int r = x / a.hkv, g = x - r * a.hkv;
   const Lens n = lens_of(a, r);
   if (n.keep == 0) return;
@@ -324,18 +328,17 @@ __global__ __launch_bounds__(IN_PLACE ? 1024 : 256) void evict_move_kernel(Evict
   const int first = n.front / kBlock + (IN_PLACE ? 0 : (blockIdx.x - x * a.groups) * kWaves);
   for (int b0 = first; b0 < (IN_PLACE ? blocks : min(blocks, first + kWaves)); b0 += kWaves) {
     const int b = b0 + wv, count = min(kBlock, n.keep - b * kBlock);
-    Moved<D, ELEM> m;
+    Moved<D, ELEM, NS> m;
     int id = -1;
     if (count > 0) {
-      const int o = lane % kBlock;
-      m.load(a, g, kept[b * kBlock + min(o, count - 1)], bt, lane);
+      m.load(a, g, s0, kept[b * kBlock + min(lane % kBlock, count - 1)], bt, lane);
       id = to[b];
     }
     if constexpr (IN_PLACE) {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __syncthreads();
     }
-    if (id >= 0 && id < a.num_blocks) m.store(a, g, id, count, lane);
+    if (id >= 0 && id < a.num_blocks) m.store(a, g, s0, id, count, lane);
   }
 }
 
@@ -353,7 +356,7 @@ int launch_kv_evict(const float* w, float* w_out, int64_t w_stride, const int32_
   const int64_t heads = int64_t(n_seqs) * hkv;
   const int64_t blocks = min((kept_stride + kBlock - 1) / kBlock, int64_t(max_new));
   const int64_t groups = (blocks + 3) / 4;
-  if (heads * max(groups, int64_t(1)) > INT32_MAX) return static_cast<int>(hipErrorInvalidValue);
+  if (heads * max(groups, int64_t(4)) > INT32_MAX) return static_cast<int>(hipErrorInvalidValue);
   a.groups = int32_t(groups);
   if (w_stride <= 16 * 256)
     hipLaunchKernelGGL(evict_select_kernel<256>, dim3(unsigned(heads)), dim3(256), 0, stream, a);
@@ -361,8 +364,12 @@ int launch_kv_evict(const float* w, float* w_out, int64_t w_stride, const int32_
     hipLaunchKernelGGL(evict_select_kernel<1024>, dim3(unsigned(heads)), dim3(1024), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || groups == 0) return static_cast<int>(e);
+  const bool sliced = heads < 512;
 #define PA_MOVE(DD, EE)                                                                              \
-  if (in_place)                                                                                      \
+  if (in_place && sliced)                                                                            \
+    hipLaunchKernelGGL((evict_move_kernel<DD, EE, true, true>), dim3(unsigned(heads * (EE == 0 ? 2 : DD / 32))), \
+                       dim3(1024), 0, stream, a);                                                    \
+  else if (in_place)                                                                                 \
     hipLaunchKernelGGL((evict_move_kernel<DD, EE, true>), dim3(unsigned(heads)), dim3(1024), 0, stream, a); \
   else                                                                                               \
     hipLaunchKernelGGL((evict_move_kernel<DD, EE, false>), dim3(unsigned(heads * groups)), dim3(256), 0, stream, a)

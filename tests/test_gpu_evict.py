@@ -247,6 +247,40 @@ def test_evict(name, cache, d, in_place):
         assert np.array_equal(x, y)
 
 
+@pytest.mark.parametrize("cache, d", [("bf16", 128), ("f32", 64), ("kv4", 64)])
+def test_evict_of_many_sequences_in_place(cache, d):
+    """Enough (sequence, kv-head) pairs that each is one workgroup's: the same bytes as from
+    an eviction to other blocks."""
+    n, hkv = 130, 4
+    r = np.random.default_rng(d)
+    lens = r.integers(1, 400, n)
+    new = np.maximum(1, (lens * r.random(n)).astype(int))
+    first = r.integers(0, 40, n)
+    table, nb0 = tables(lens, 21)
+    fresh, more = tables(new, 22)
+    to = np.where(fresh >= 0, fresh + nb0, -1).astype(np.int32)
+    for i in range(n):
+        same = min(first[i], new[i]) // 16
+        to[i, :same] = table[i, :same]
+    c = cache_of(cache, nb0 + more, hkv, d, 23)
+    w = dev(r.random((n, hkv, 400)).astype(np.float32))
+    ints = [dev(x.astype(np.int32)) for x in (lens, new, first)]
+    results = []
+    for in_place in (False, True):  # the first leaves the old blocks as they are
+        kept = torch.full((n, hkv, 400), -1, dtype=torch.int32, device="cuda")
+        ww = w.clone()
+        B.kv_evict(ww, dev(table), *ints[:2], c.k, c.v, kept, scales=c.scales,
+                   new_table=None if in_place else dev(to), first=ints[2], window=9)
+        torch.cuda.synchronize()
+        at = table if in_place else to
+        raw = c.raw()
+        rows = [[x[at[i, np.arange(new[i]) // 16], :, np.arange(new[i]) % 16] for i in range(n)] for x in raw]
+        results.append((kept, ww, rows))
+    assert torch.equal(results[0][0], results[1][0]) and torch.equal(results[0][1], results[1][1])
+    for x, y in zip(results[0][2], results[1][2]):
+        assert all(np.array_equal(a, b) for a, b in zip(x, y))
+
+
 def test_evict_leaves_what_does_not_fit():
     """Sequences longer than the weights or the table, or that keep more than the list or the
     new table hold, stay as they are; the others are shortened.  Blocks outside the cache are
