@@ -722,13 +722,13 @@ int pa_attn_weights(const void* q, const float* lse, const void* k_cache, const 
  * and weights_out[r][h][i] receives its weight.  weights and weights_out are
  * [n_seqs][num_kv_heads][weights_stride], the same array or two that do not overlap; kept
  * is [n_seqs][num_kv_heads][kept_stride].  Entries behind B are left alone.
- * A sequence with new_lens[r] <= 0, or whose L exceeds weights_stride or its table, or B
- * kept_stride or the new table, is left alone as a whole.
+ * A sequence with new_lens[r] <= 0, or whose L exceeds weights_stride, its table or 2^30, or
+ * B kept_stride or the new table, is left alone as a whole.
  *
  * Kept tokens go to the blocks of new_table [n_seqs][new_max_blocks], from block F / 16 on;
  * blocks before it are not touched (the tables agree there).  A block of new_table that
  * receives tokens must be in no row of block_table, but for entry F / 16, which may be the
- * same in both.  With new_table NULL, or block_table itself, the tokens move within the
+ * same in both, and once in new_table.  With new_table NULL, or block_table itself, the tokens move within the
  * sequence's own blocks, which from F / 16 on must be in that sequence's table only;
  * fewer workgroups share that work, since a block is written only once all that it held has
  * been read.  pa_seq_compact gives the pool's side of both.  Tokens whose block id (old or

@@ -663,27 +663,23 @@ def _refuse(code: int, checks):
             raise PaError(code, msg)
 
 
-def _cache_form(t, bits: int, v_cache):
-    """(element type, blocks, kv-heads, head_dim, block size, shapes of k_cache, v_cache and
-    scales) of the 8- or 4-bit cache that v_cache is part of."""
-    if bits == 8:
-        nb, hkv, d, bs = v_cache.shape if v_cache.dim() == 4 else (0, 0, 0, 16)
-        return (t.float8_e4m3fn, nb, hkv, d, bs, (nb, hkv, d // 64, bs, 64), (nb, hkv, d, bs),
-                (nb, hkv, 2))
-    nb, hkv, c = v_cache.shape[:3] if v_cache.dim() == 5 else (0, 0, 0)
-    return (t.uint8, nb, hkv, 32 * c, 16, (nb, hkv, 16, 16 * c), (nb, hkv, c, 16, 16),
-            (nb, hkv, c + 1, 16))
+def _cache_form4(t, k_cache, v_cache, scales):
+    """(element type, blocks, kv-heads, head_dim, block size, whether the tensors' shapes are
+    a 4-bit cache's) of the cache that v_cache is part of."""
+    if v_cache.dim() != 5:
+        return t.uint8, 0, 0, 0, 16, False
+    nb, hkv, c, i, o = v_cache.shape
+    return (t.uint8, nb, hkv, 32 * c, 16, i == 16 and o == 16 and scales.shape == (nb, hkv, c + 1, 16)
+            and k_cache.shape == (nb, hkv, 16, 16 * c))
 
 
-def _refuse_cache(t, bits, k_cache, v_cache, scales):
-    dt, _, _, _, _, ks, vs, ss = _cache_form(t, bits, v_cache)
+def _refuse_cache(t, bits, dt, whole, k_cache, v_cache, scales):
     _refuse(PA_ERR_UNSUPPORTED, [(
         k_cache.dtype == v_cache.dtype == dt and scales.dtype == t.uint8,
         f"{bits}-bit cache of {k_cache.dtype}, {v_cache.dtype} and {scales.dtype} (supported: "
         f"{str(dt)[6:]} with uint8 scales)")])
     _refuse(PA_ERR_ARG, [
-        (k_cache.shape == ks and v_cache.shape == vs and scales.shape == ss,
-         f"{bits}-bit cache: k_cache, v_cache and scales differ in shape"),
+        (whole, f"{bits}-bit cache: k_cache, v_cache and scales differ in shape"),
         (k_cache.is_contiguous() and v_cache.is_contiguous() and scales.is_contiguous(),
          f"{bits}-bit cache: tensors must be contiguous")])
 
@@ -728,7 +724,11 @@ def _packed(x, heads: int, d: int) -> bool:
 
 def _quant_rows(fn, bits, k, v, block_table, seq_lens, cu_seqlens, k_cache, v_cache, scales, stream):
     t = _torch or _torch_module()
-    cdt, nb, hkv, d, bs, k_shape, v_shape, s_shape = _cache_form(t, bits, v_cache)
+    if bits == 8:  # written out: a call of few rows waits for these lines
+        cdt, (nb, hkv, d, bs) = t.float8_e4m3fn, v_cache.shape
+        whole = k_cache.shape == (nb, hkv, d // 64, bs, 64) and scales.shape == (nb, hkv, 2)
+    else:
+        cdt, nb, hkv, d, bs, whole = _cache_form4(t, k_cache, v_cache, scales)
     shape, dt, n, i32 = k.shape, k.dtype, seq_lens.numel(), t.int32
     T, code = shape[0], _ROW_DTYPES.get(dt)
     rows, width = block_table.shape if block_table.dim() == 2 else (-1, 0)
@@ -736,8 +736,7 @@ def _quant_rows(fn, bits, k, v, block_table, seq_lens, cu_seqlens, k_cache, v_ca
     st = _stream_on(dev, stream)
     if not (shape == (T, hkv, d) and v.shape == shape and _packed(k, hkv, d)
             and _packed(v, hkv, d) and code is not None and v.dtype == dt
-            and k_cache.dtype == cdt and v_cache.dtype == cdt and scales.dtype == t.uint8
-            and k_cache.shape == k_shape and v_cache.shape == v_shape and scales.shape == s_shape
+            and k_cache.dtype == cdt and v_cache.dtype == cdt and scales.dtype == t.uint8 and whole
             and k_cache.is_contiguous() and v_cache.is_contiguous() and scales.is_contiguous()
             and rows >= n and cu_seqlens.numel() > n
             and block_table.dtype == i32 and seq_lens.dtype == i32 and cu_seqlens.dtype == i32
@@ -746,7 +745,7 @@ def _quant_rows(fn, bits, k, v, block_table, seq_lens, cu_seqlens, k_cache, v_ca
             and st >= 0 and k.get_device() == v.get_device() == k_cache.get_device()
             == scales.get_device() == block_table.get_device() == seq_lens.get_device()
             == cu_seqlens.get_device() == dev):
-        _refuse_cache(t, bits, k_cache, v_cache, scales)
+        _refuse_cache(t, bits, cdt, whole, k_cache, v_cache, scales)
         _refuse(PA_ERR_ARG, [
             (shape == (T, hkv, d) and v.shape == shape and _packed(k, hkv, d)
              and _packed(v, hkv, d),
@@ -800,7 +799,11 @@ def _quant_attn_args(bits, q, k_cache, v_cache, scales, block_table, seq_lens, c
                      info, out, lse, scale, stream, workspace):
     """(arguments up to the plan info, stream) of a call over the 8- or 4-bit cache."""
     t = _torch or _torch_module()
-    cdt, nb, hkv, d, bs, k_shape, v_shape, s_shape = _cache_form(t, bits, v_cache)
+    if bits == 8:
+        cdt, (nb, hkv, d, bs) = t.float8_e4m3fn, v_cache.shape
+        whole = k_cache.shape == (nb, hkv, d // 64, bs, 64) and scales.shape == (nb, hkv, 2)
+    else:
+        cdt, nb, hkv, d, bs, whole = _cache_form4(t, k_cache, v_cache, scales)
     total_q, hq, dq = q.shape
     n, i32 = seq_lens.numel(), t.int32
     rows, width = block_table.shape if block_table.dim() == 2 else (-1, 0)
@@ -808,8 +811,7 @@ def _quant_attn_args(bits, q, k_cache, v_cache, scales, block_table, seq_lens, c
     st = _stream_on(dev, stream)
     if not (q.dtype == t.bfloat16 and out.dtype == t.bfloat16 and dq == d
             and out.shape == q.shape and q.is_contiguous() and out.is_contiguous()
-            and k_cache.dtype == cdt and v_cache.dtype == cdt and scales.dtype == t.uint8
-            and k_cache.shape == k_shape and v_cache.shape == v_shape and scales.shape == s_shape
+            and k_cache.dtype == cdt and v_cache.dtype == cdt and scales.dtype == t.uint8 and whole
             and k_cache.is_contiguous() and v_cache.is_contiguous() and scales.is_contiguous()
             and rows >= n and cu_seqlens_q.numel() > n
             and block_table.dtype == i32 and seq_lens.dtype == i32 and cu_seqlens_q.dtype == i32
@@ -825,7 +827,7 @@ def _quant_attn_args(bits, q, k_cache, v_cache, scales, block_table, seq_lens, c
             and st >= 0 and q.get_device() == out.get_device() == k_cache.get_device()
             == scales.get_device() == block_table.get_device() == seq_lens.get_device()
             == cu_seqlens_q.get_device() == dev):
-        _refuse_cache(t, bits, k_cache, v_cache, scales)
+        _refuse_cache(t, bits, cdt, whole, k_cache, v_cache, scales)
         _refuse(PA_ERR_UNSUPPORTED, [
             (q.dtype == out.dtype == t.bfloat16,
              f"queries {q.dtype}, output {out.dtype} (supported: bfloat16)")])

@@ -175,7 +175,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void a
   for (int64_t chunk = first_chunk; chunk * kChunk < L; chunk += a.chunks) {
     const int key0 = int(chunk) * kChunk;
     // rows from the first that sees one of the chunk's keys on
-    const int row_first = max(0, key0 - sr.base) * G / kRows * kRows;
+    const int row_first = min(max(0, key0 - sr.base), rows / G) * G / kRows * kRows;
     seek_rows(row_first);
     load_rows(row_first);
     bf16x8 k[KT][KS];

@@ -33,6 +33,8 @@ struct EvictArgs {
   int32_t max_blocks, max_new, window, num_blocks, hkv, groups;
 };
 
+constexpr int kMostTokens = 1 << 30;  // of a sequence: positions and their shares fit 32 bits
+
 struct Lens {
   int len, keep, front, window;  // keep 0: nothing to do
 };
@@ -40,7 +42,7 @@ struct Lens {
 // A sequence's lengths; one that does not fit the arrays is left alone.
 __device__ __forceinline__ Lens lens_of(const EvictArgs& a, int r) {
   const int L = a.seq_lens[r], B = min(a.new_lens[r], L);
-  if (B <= 0 || L > a.w_stride || L > int64_t(a.max_blocks) * kBlock || B > a.kept_stride ||
+  if (B <= 0 || L > kMostTokens || L > a.w_stride || L > int64_t(a.max_blocks) * kBlock || B > a.kept_stride ||
       B > int64_t(a.max_new) * kBlock)
     return {L, 0, 0, 0};
   const int F = a.first ? min(max(a.first[r], 0), B) : 0;

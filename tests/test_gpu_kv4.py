@@ -369,3 +369,161 @@ def test_blocks_past_4_gib(q_lens):
     for a, b in zip(*results):
         assert torch.equal(a, b)
     assert torch.isfinite(results[0][2].float()).all()
+
+
+# ---- together ---------------------------------------------------------------------------------
+
+class Step:
+    """A decode or verification step of one layer: append, attention, the new tokens read
+    back."""
+
+    def __init__(self, lens, n_new, hq=8, hkv=2, d=128, seed=0):
+        r = np.random.default_rng([seed, 4])
+        self.hq, self.hkv, self.d, self.T = hq, hkv, d, n_new * len(lens)
+        lens = np.array(lens)
+        self.table, nb = tables(lens + n_new, seed)
+        self.cache = Cache(nb, hkv, d, seed)
+        n = int(lens.sum())
+        k, v = rows_of(r, n, hkv, d, "bf16"), rows_of(r, n, hkv, d, "bf16")
+        m = meta(self.table, lens, lens)
+        B.kv4_append(dev(k, torch.bfloat16), dev(v, torch.bfloat16), *map(dev, m), *self.cache.args)
+        self.m = meta(self.table, lens + n_new, [n_new] * len(lens))
+        self.dm = [dev(x) for x in self.m]
+        seq = np.repeat(np.arange(len(lens)), n_new)
+        self.at = seq, np.concatenate([np.arange(x, x + n_new) for x in lens])
+        self.q = torch.empty((self.T, hq, d), dtype=torch.bfloat16, device="cuda")
+        self.k = torch.empty((self.T, hkv, d), dtype=torch.bfloat16, device="cuda")
+        self.v, self.k_back, self.v_back = (torch.empty_like(self.k) for _ in range(3))
+        self.out, self.lse = torch.empty_like(self.q), torch.empty((self.T, hq), device="cuda")
+        self.kind = B.KIND_DECODE if n_new == 1 else B.KIND_VERIFY
+        plan, self.info = B.plan(self.kind, n_new, self.m[1], self.m[2], hq, hkv, d, 16,
+                                 B.PA_BF16_KV4, block_table=self.m[0])
+        self.plan = dev(plan)
+        self.ws = torch.empty(max(16, int(self.info.workspace_bytes)), dtype=torch.uint8, device="cuda")
+
+    def feed(self, seed):
+        r = np.random.default_rng([seed, 5])
+        for x, h in ((self.q, self.hq), (self.k, self.hkv), (self.v, self.hkv)):
+            x.copy_(dev(rows_of(r, self.T, h, self.d, "bf16"), torch.bfloat16))
+
+    def step(self, stream=None):
+        B.kv4_append(self.k, self.v, *self.dm, *self.cache.args, stream=stream)
+        B.kv4_attention(self.kind, self.q, *self.cache.args, *self.dm, self.plan, self.info, self.ws,
+                        self.out, self.lse, stream=stream)
+        B.kv4_read(self.k_back, self.v_back, *self.dm, *self.cache.args, stream=stream)
+
+    def check(self, label):
+        kc, vc = self.cache.values()  # unwritten slots among them: looked at nowhere below
+        k, v = self.k.double().cpu().numpy(), self.v.double().cpu().numpy()
+        assert np.array_equal(self.k_back.double().cpu().numpy(), kv4.round_keys(k)), label
+        assert np.array_equal(self.v_back.double().cpu().numpy(), kv4.round_values(v)), label
+        seq, pos = self.at
+        blk = self.table[seq, pos // 16]
+        assert np.array_equal(kc[blk, :, pos % 16], kv4.round_keys(k)), label
+        q = self.q.double().cpu().numpy()
+        used = np.zeros(kc.shape[:1] + (16,), bool)
+        for row, L in zip(self.table, self.m[1]):
+            t = np.arange(L)
+            used[row[t // 16], t % 16] = True
+        kc, vc = np.where(used[:, None, :, None], kc, 0), np.where(used[:, None, None], vc, 0)
+        ro, rl = paged_attention(q, kc, vc, *self.m, self.hkv)
+        bo, bl = bounds(q, kc, vc, *self.m, self.hkv, ro, rl)
+        eo = np.abs(self.out.double().cpu().numpy() - ro)
+        el = np.abs(self.lse.double().cpu().numpy() - rl)
+        # Probabilities below 2^-126 of a row's largest, and their products with a value's scale,
+        # are zero in float32 and bf16: each then takes less than 2^-126 |v| from the sum, or
+        # 2^-126 times a code of at most 6.  (Codes of zero leave dims whose other terms are all
+        # of that kind.)
+        bo = bo + int(self.m[1].max()) * 2.0 ** -126 * max(6.0, np.abs(vc).max())
+        say(f"[kv4] {label}: worst out {np.max(eo / bo):.2f}, lse {np.max(el / bl):.2f} of the bound")
+        assert np.all(eo <= bo) and np.all(el <= bl), label
+
+
+@pytest.mark.parametrize("n_new, d", [(1, 128), (4, 128), (5, 64)])
+def test_step(n_new, d):
+    c = Step([100, 15, 16, 700, 33], n_new, d=d)
+    for i in range(3):  # the same positions again
+        c.feed(i)
+        c.step()
+        torch.cuda.synchronize()
+        c.check(f"step {n_new} {i}")
+
+
+def test_step_on_another_stream():
+    c = Step([100, 15, 700], 1, seed=1)
+    side = torch.cuda.Stream()
+    for i in range(2):
+        c.feed(i)
+        side.wait_stream(torch.cuda.current_stream())
+        if i == 0:
+            c.step(stream=side)
+        else:
+            with torch.cuda.stream(side):
+                c.step()
+        side.synchronize()
+        c.check(f"side stream {i}")
+
+
+def test_captured_step():
+    """A captured step replayed with other inputs between, eager work beside it."""
+    c = Step([100, 15, 700, 2000], 1, hq=16, seed=2)
+    c.feed(0)
+    c.step()  # modules are loaded outside the capture
+    torch.cuda.synchronize()
+    c.check("before the capture")
+    g = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side), torch.cuda.graph(g, stream=side):
+        c.step()
+    torch.cuda.current_stream().wait_stream(side)
+    for i in range(4):
+        c.feed(10 + i)
+        c.out.fill_(9.0)
+        g.replay()
+        torch.cuda.synchronize()
+        c.check(f"replay {i}")
+        if i == 1:
+            c.feed(20)
+            c.step()
+            torch.cuda.synchronize()
+            c.check("eager between replays")
+
+
+def test_workload_steps():
+    """Workloads of the framework on a 4-bit cache: prefix hits, chunks, drafts rolled back,
+    several launches, through the staged path."""
+    from paper_2605_11232_amd.runtime import DeviceReplay, Staging, plan_words_bound
+    for name, scale in (("prefill", 0.05), ("decode", 0.04), ("mixed", 0.03), ("verify", 0.06)):
+        wl = synth.workload(name, scale=scale, steps=2)
+        cfg = wl.cfg
+        dv, orc = DeviceReplay(wl, kv4=True).setup(), OracleReplay(wl, kv4=True).setup()
+        launches = list(wl.launches[:2]) + ([wl.step(1)] if wl.step else [])
+        n, T = max(len(x.seq_ids) for x in launches), max(x.total_q for x in launches)
+        st = [Staging(dv.device, n, wl.max_blocks_per_seq, T,
+                      plan_words_bound(cfg, n, T, wl.max_blocks_per_seq)) for _ in range(2)]
+        for i, ln in enumerate(launches):
+            rows = sorted({(int(t), int(h)) for t, h in zip(
+                np.random.default_rng(i).integers(0, ln.total_q, 60),
+                np.random.default_rng(i + 9).integers(0, cfg.num_q_heads, 60))})
+            ro = orc.launch(ln, rows=rows)
+            x = [torch.from_numpy(a.get()).to("cuda", torch.bfloat16) for a in (ln.q, ln.k_new, ln.v_new)]
+            out = torch.empty((ln.total_q, cfg.num_q_heads, cfg.head_dim), dtype=torch.bfloat16,
+                              device="cuda")
+            lse = torch.empty((ln.total_q, cfg.num_q_heads), dtype=torch.float32, device="cuda")
+            p = dv.prepare_staged(ln, st[i % 2], *x, out, lse)
+            dv.append(p)
+            dv.attend(p)
+            torch.cuda.synchronize()
+            t, h = np.array(rows).T
+            A, _ = paged_attention(ln.q.get().astype(np.float64), orc.k_cache, np.abs(orc.v_cache),
+                                   ro["meta"]["block_table"], ro["meta"]["seq_lens"],
+                                   ro["meta"]["cu_seqlens_q"], cfg.num_kv_heads, rows=rows)
+            err = np.abs(out.double().cpu().numpy() - ro["out"])[t, h]
+            # |q| |k| / sqrt(D) of normal values is below 40: 2 ds < 2^-10
+            b = 2.0 ** -8 * np.abs(ro["out"][t, h]) + (2.0 ** -8 + 2.0 ** -10) * A[t, h]
+            say(f"[kv4] {name} launch {i}: worst {np.max(err / b):.2f} of the bound")
+            assert np.all(err <= b)
+            assert np.all(np.abs(lse.double().cpu().numpy() - ro["lse"])[t, h] <= 2.0 ** -10)
+            orc.finish(ln)
+            dv.finish(ln, batched=True)
