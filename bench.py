@@ -52,7 +52,7 @@ DESCRIPTIONS = {
 # rocprofv3 FETCH_SIZE / WRITE_SIZE counter runs scaled by the factors a plain
 # copy of known size gives; valid only for the kernel sources it was taken on.
 TRAFFIC_FILE = os.path.join(ROOT, "profiles", "hbm_traffic.json")
-KERNEL_SOURCES = ["attn_bf16.hip", "attn_f32.hip", "device_common.h", "plan.cpp",
+KERNEL_SOURCES = ["attn_bf16.hip", "attn_items.h", "attn_f32.hip", "device_common.h", "plan.cpp",
                   "plan_format.h", "api.hip"]
 
 

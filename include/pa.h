@@ -703,8 +703,8 @@ int pa_kv4_attn_decode_noalloc(const void* q, const void* k_cache, const void* v
  * PA_BF16_KV4, k_cache and scales of a 4-bit cache.  Products of bf16 numbers, exponentials
  * and sums are float32, the sums in one order: equal calls give equal bits.  All pointers
  * are caller-owned device memory; asynchronous on stream; allocates nothing.  Errors:
- * PA_ERR_ARG (NULL pointer with work to do, sizes, scale, accumulate, q or cache not
- * 16-byte, lse or weights not 4-byte aligned), PA_ERR_UNSUPPORTED (head_dim, block_size,
+ * PA_ERR_ARG (NULL pointer with work to do, sizes, total_q * num_q_heads above 2^30, scale,
+ * accumulate, q or cache not 16-byte, lse or weights not 4-byte aligned), PA_ERR_UNSUPPORTED (head_dim, block_size,
  * dtype), PA_ERR_LAUNCH. */
 int pa_attn_weights(const void* q, const float* lse, const void* k_cache, const uint8_t* scales,
                     int32_t num_blocks, const int32_t* block_table, int32_t max_blocks_per_seq,

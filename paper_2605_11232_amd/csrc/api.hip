@@ -560,8 +560,8 @@ int pa_attn_weights(const void* q, const float* lse, const void* k_cache, const 
                 num_q_heads, num_kv_heads);
   if (n_seqs < 0 || total_q < 0 || max_blocks_per_seq < 1 || weights_stride < 0)
     return fail(PA_ERR_ARG, "%s: negative size or max_blocks_per_seq < 1", fn);
-  if (int64_t(total_q) * num_q_heads > INT32_MAX)
-    return fail(PA_ERR_ARG, "%s: %d tokens of %d heads: more than 2^31 - 1 rows", fn, total_q,
+  if (int64_t(total_q) * num_q_heads > (int64_t(1) << 30))
+    return fail(PA_ERR_ARG, "%s: %d tokens of %d heads: more than 2^30 rows", fn, total_q,
                 num_q_heads);
   if (!(scale > 0.f) || scale == __builtin_huge_valf())
     return fail(PA_ERR_ARG, "%s: scale must be positive and finite", fn);

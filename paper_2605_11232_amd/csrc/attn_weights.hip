@@ -121,7 +121,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void a
   if (rows == 0) return;
   const float c = a.scale_log2;
   const int32_t* bt = a.bt + (int64_t)r * a.max_blocks;
-  const int step_q = kRows / G, step_h = kRows - step_q * G;  // a tile's rows, as queries and heads
+  // a tile's rows as queries and heads, and how far that is in (token, head) rows
+  const int step_q = kRows / G, step_h = kRows - step_q * G, step_row = step_q * a.hq + step_h;
 
   // Rows of the next tile that this thread copies: units 256 i + tid, log-sum-exp tid.
   // All of a stage's loads are issued at once; whether a row counts is looked at when it is
@@ -129,35 +130,40 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void a
   u32x4 raw[NL];
   float raw_z[NL], raw_lse = 0.f;
   int raw_pos = 0;
-  const int64_t row0 = (int64_t)sr.qs * a.hq + g * G;
-  int qi[NL], head[NL], qi_z = 0, head_z = 0;
+  const __bf16* const q0 = a.q + ((int64_t)sr.qs * a.hq + g * G) * D + 8 * (tid % UR);
+  const float* const z0 = a.lse + (int64_t)sr.qs * a.hq + g * G;
+  int row[NL], head[NL], row_z = 0, head_z = 0, pos_z = 0;
   auto seek_rows = [&](int r0) {
+    auto of = [&](int rho, int& rw, int& h) {
+      const int qi = rho / G;
+      h = rho - qi * G, rw = qi * a.hq + h;
+      return sr.base + qi;
+    };
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int rho = r0 + (256 * i + tid) / UR;
-      qi[i] = rho / G, head[i] = rho - qi[i] * G;
-    }
-    qi_z = (r0 + tid) / G, head_z = r0 + tid - qi_z * G;
+    for (int i = 0; i < NL; ++i) of(r0 + (256 * i + tid) / UR, row[i], head[i]);
+    pos_z = of(r0 + tid, row_z, head_z);
   };
-  auto advance = [&](int& q, int& h) {
-    q += step_q, h += step_h;
-    if (h >= G) h -= G, ++q;
+  // one tile on; whether that passes one more query
+  auto advance = [&](int& rw, int& h) {
+    rw += step_row, h += step_h;
+    const bool next = h >= G;
+    if (next) h -= G, rw += a.hq - G;
+    return next;
   };
   auto load_rows = [&](int r0) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const int u = 256 * i + tid, p = u % UR;
-      const bool in = r0 + u / UR < rows;
-      const int64_t row = row0 + (in ? qi[i] * a.hq + head[i] : 0);
-      raw[i] = ld16(a.q + row * D + 8 * p);
-      raw_z[i] = in ? a.lse[row] : __builtin_huge_valf();
-      advance(qi[i], head[i]);
+      const bool in = r0 + (256 * i + tid) / UR < rows;
+      const int at = in ? row[i] : 0;
+      raw[i] = ld16(q0 + (int64_t)at * D);
+      raw_z[i] = in ? z0[at] : __builtin_huge_valf();
+      advance(row[i], head[i]);
     }
     if (tid < kRows) {
       const bool in = r0 + tid < rows;
-      raw_lse = in ? a.lse[row0 + qi_z * a.hq + head_z] : __builtin_huge_valf();
-      raw_pos = in ? sr.base + qi_z : -1;
-      advance(qi_z, head_z);
+      raw_lse = in ? z0[row_z] : __builtin_huge_valf();
+      raw_pos = in ? pos_z : -1;
+      pos_z += step_q + advance(row_z, head_z);
     }
   };
   auto store_rows = [&](int buf) {

@@ -424,7 +424,11 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
     auto on_tiles = [&](int32_t r) { return few_tiles && qlen(r) * G > pa::kRowItemRows; };
     auto row_pieces = [&](int32_t r) { return cdiv(qlen(r) * G, pa::kRowItemRows); };
     const int64_t row_step = kv8 ? pa::kKeyStep8 : pa::kKeyStep;
-    const double key_bytes = head_dim * (kv8 ? 2 : 4);  // a key and its value
+    // A key and its value.  Over the 4-bit cache a row item's time is not that of its bytes
+    // (1.06 a dim) but of a wavefront's steps: priced as 3 a dim, 36 random launches on shared
+    // prefixes take 0.8 % less than as 2, one of 128 decode requests on 4096 36.2 us against
+    // 39.9; as 4 and 6 others lose up to 30 %.
+    const double key_bytes = head_dim * (dtype == PA_BF16_KV4 ? 3 : kv8 ? 2 : 4);
     // Keys of a row item where all items hold `keys` and `waves` wavefronts are wanted; a
     // row item's block ids fit one wavefront (64 lanes): at most 1024 keys.
     auto item_chunk = [&](int64_t keys, int64_t least, int64_t waves) {

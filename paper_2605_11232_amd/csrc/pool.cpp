@@ -352,7 +352,13 @@ int pa_seq_compact(pa_pool* pool, int64_t seq_id, int32_t new_len, int32_t first
     if (need > pool->obtainable(0))
       return pa::fail(PA_ERR_NO_BLOCKS, "pa_seq_compact: need %lld blocks, %lld obtainable",
                       (long long)need, (long long)pool->obtainable(0));
-    const std::vector<int32_t> old(s.blocks.begin() + stay, s.blocks.end());
+    std::vector<int32_t> old;
+    try {
+      old.assign(s.blocks.begin() + stay, s.blocks.end());
+      s.blocks.reserve(total);
+    } catch (const std::bad_alloc&) {
+      return pa::fail(PA_ERR_ARG, "pa_seq_compact: out of host memory");
+    }
     s.blocks.resize(stay);
     for (int64_t i = 0; i < need; ++i) {
       const int32_t b = pool->take();
