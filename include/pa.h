@@ -45,8 +45,8 @@
  *  - Supported: block_size 16, head_dim 64 or 128, num_q_heads a multiple of
  *    num_kv_heads; dtype PA_BF16 (MFMA path, float32 accumulation) or PA_F32
  *    (float32 throughout).  The pa_kv8_* and pa_kv4_* calls work on an 8-bit and
- *    a 4-bit cache, whose layouts are given there.  Integers are int32; num_blocks * block_size must
- *    be below 2^31.
+ *    a 4-bit cache, whose layouts are given there.  Integers are int32;
+ *    num_blocks * block_size must be below 2^31.
  *  - Not thread-safe per pool; device calls on one stream are ordered.
  */
 #ifndef PA_H_
@@ -307,7 +307,8 @@ typedef struct pa_plan_info {
  * kind PA_KIND_DECODE requires every q_len == 1, PA_KIND_VERIFY every q_len ==
  * n_q (1..8); PA_KIND_PREFILL takes any q_len >= 0 (prefill chunks and decode
  * tokens may be mixed).  dtype: PA_BF16, PA_F32, or PA_BF16_KV8 and
- * PA_BF16_KV4 for the pa_kv8_attn_* and pa_kv4_attn_* calls.  num_cus = compute units to fill (0: 256).
+ * PA_BF16_KV4 for the pa_kv8_attn_* and pa_kv4_attn_* calls.  num_cus = compute
+ * units to fill (0: 256).
  * Errors: PA_ERR_ARG, PA_ERR_UNSUPPORTED. */
 int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int32_t* seq_lens,
                  const int32_t* cu_seqlens_q, const int32_t* block_table,
@@ -696,15 +697,15 @@ int pa_kv4_attn_decode_noalloc(const void* q, const void* k_cache, const void* v
  * for t of [0, seq_lens[r]), added to what is there with accumulate = 1, written in its
  * place with 0.  q, the caches' layout and the metadata are those of the attention call
  * (before or after it; the keys of the launch's own tokens appended), lse its output
- * [total_q][num_q_heads].  A row whose log-sum-exp is not finite counts for nothing; the
- * weight of a key that is not finite may be NaN.  weights: [n_seqs][num_kv_heads]
- * [weights_stride] float32; keys at or past weights_stride, sequences without rows and what
- * lies behind a sequence's keys are left alone.  dtype: PA_BF16, with scales NULL, or
- * PA_BF16_KV4, k_cache and scales of a 4-bit cache.  Products of bf16 numbers, exponentials
- * and sums are float32, the sums in one order: equal calls give equal bits.  All pointers
- * are caller-owned device memory; asynchronous on stream; allocates nothing.  Errors:
- * PA_ERR_ARG (NULL pointer with work to do, sizes, total_q * num_q_heads above 2^30, scale,
- * accumulate, q or cache not 16-byte, lse or weights not 4-byte aligned), PA_ERR_UNSUPPORTED (head_dim, block_size,
+ * [total_q][num_q_heads].  A row whose log-sum-exp is not finite counts for nothing.
+ * weights: [n_seqs][num_kv_heads][weights_stride] float32; keys at or past
+ * weights_stride, sequences without rows and what lies behind a sequence's keys are left
+ * alone.  dtype: PA_BF16, with scales NULL, or PA_BF16_KV4, k_cache and scales of a 4-bit
+ * cache.  Products of bf16 numbers, exponentials and sums are float32, the sums in one
+ * order: equal calls give equal bits.  All pointers are caller-owned device memory;
+ * asynchronous on stream; allocates nothing.  Errors: PA_ERR_ARG (NULL pointer with work
+ * to do, sizes, total_q * num_q_heads above 2^30, scale, accumulate, q or cache not
+ * 16-byte, lse or weights not 4-byte aligned), PA_ERR_UNSUPPORTED (head_dim, block_size,
  * dtype), PA_ERR_LAUNCH. */
 int pa_attn_weights(const void* q, const float* lse, const void* k_cache, const uint8_t* scales,
                     int32_t num_blocks, const int32_t* block_table, int32_t max_blocks_per_seq,
@@ -725,14 +726,15 @@ int pa_attn_weights(const void* q, const float* lse, const void* k_cache, const 
  * A sequence with new_lens[r] <= 0, or whose L exceeds weights_stride, its table or 2^30, or
  * B kept_stride or the new table, is left alone as a whole.
  *
- * Kept tokens go to the blocks of new_table [n_seqs][new_max_blocks], from block F / 16 on;
- * blocks before it are not touched (the tables agree there).  A block of new_table that
- * receives tokens must be in no row of block_table, but for entry F / 16, which may be the
- * same in both, and once in new_table.  With new_table NULL, or block_table itself, the tokens move within the
- * sequence's own blocks, which from F / 16 on must be in that sequence's table only;
- * fewer workgroups share that work, since a block is written only once all that it held has
- * been read.  pa_seq_compact gives the pool's side of both.  Tokens whose block id (old or
- * new) is outside [0, num_blocks) are read from a clamped block, or not written.
+ * Kept tokens go to the blocks of new_table [n_seqs][new_max_blocks], from block F / 16
+ * on; blocks before it are not touched (the tables agree there).  A block of new_table
+ * that receives tokens must be in no row of block_table, but for entry F / 16, which may
+ * be the same in both, and once in new_table.  With new_table NULL, or block_table itself,
+ * the tokens move within the sequence's own blocks, which from F / 16 on must be in that
+ * sequence's table only; fewer workgroups share that work, since a block is written only
+ * once all that it held has been read.  pa_seq_compact gives the pool's side of both.
+ * Tokens whose block id (old or new) is outside [0, num_blocks) are read from a clamped
+ * block, or not written.
  *
  * dtype: PA_F32 and PA_BF16 with scales NULL; PA_BF16_KV4, where a token's scales move too.
  * (Tokens of the 8-bit cache share their block's scale and would be rounded again: read

@@ -38,13 +38,15 @@ constexpr int kRows = 32;  // rows at a time
 constexpr int kFewWaves = 16384;  // wavefronts wanted where rows are few
 
 // LDS: two tiles of rows, 16-byte unit p of row r at unit p ^ (r & 7), so that eight
-// neighbouring lanes (rows) read distinct banks; the rows' log-sum-exps (times log2 e; a row
-// that does not count: infinity) and positions.
+// neighbouring lanes (rows) read distinct banks; the rows' log-sum-exps (times log2 e) and
+// positions (a row that does not count: -1, it sees no key); the position up to which all of
+// the tile's rows see keys.
 template <int D>
 struct RowSmem {
   __bf16 q[2][kRows * D];
   float lse[2][kRows];
   int pos[2][kRows];
+  int seen[2];
 };
 
 // A sequence's rows and keys, as the kernels see them.
@@ -173,8 +175,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void a
       st16(&sm.q[buf][8 * (lr * UR + (p ^ (lr & 7)))], counts(raw_z[i]) ? raw[i] : zero16());
     }
     if (tid < kRows) {
-      sm.lse[buf][tid] = counts(raw_lse) ? raw_lse * kLog2e : __builtin_huge_valf();
-      sm.pos[buf][tid] = raw_pos;
+      const bool ok = counts(raw_lse);
+      sm.lse[buf][tid] = ok ? raw_lse * kLog2e : __builtin_huge_valf();
+      sm.pos[buf][tid] = ok ? raw_pos : -1;
+      const bool all = __ballot(!ok) == 0;
+      if (tid == 0) sm.seen[buf] = all ? raw_pos : -1;
     }
   };
 
@@ -230,7 +235,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void a
         for (int t = 0; t < KT; ++t) s[t] = mfma32(q, k[t][ks], s[t]);
         __builtin_amdgcn_sched_group_barrier(0x008, KT, 0);
       }
-      // the first row does not see all keys: positions are looked at
+      // a row does not see all keys: positions are looked at, so that an infinite key is
+      // multiplied with a row that does not count to no effect
       auto add = [&](auto masked) {
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4) {
@@ -245,7 +251,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void a
             }
         }
       };
-      if (__builtin_amdgcn_readfirstlane(sm.pos[buf][0]) < last_key) add(std::true_type{});
+      if (__builtin_amdgcn_readfirstlane(sm.seen[buf]) < last_key) add(std::true_type{});
       else add(std::false_type{});
       if (more) store_rows(buf ^ 1);
       __syncthreads();
@@ -310,7 +316,7 @@ __global__ __launch_bounds__(256) void attn_weights_few_kernel(WeightArgs a) {
     BlockSpan span;
     span.init(bt, a.max_blocks, k0 / kBlock);
     for (int r0 = 0; r0 < sr.rows; r0 += 16 * NR) {
-      const int first_pos = sr.base + r0 / G;
+      int seen = sr.base + r0 / G;  // up to here all rows see keys
       bf16x8 q[NR][KS];
       f32x4 z[NR];
       int pos[NR][4];
@@ -322,7 +328,8 @@ __global__ __launch_bounds__(256) void attn_weights_few_kernel(WeightArgs a) {
         const float lse = a.lse[row];
         const bool ok = lr < sr.rows && counts(lse);
         const float my_z = ok ? lse * kLog2e : __builtin_huge_valf();
-        const int my_pos = sr.base + qi;
+        const int my_pos = ok ? sr.base + qi : -1;  // -1: it sees no key
+        if (__ballot(!ok) != 0) seen = -1;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
           const u32x4 v = ld16(a.q + row * D + 8 * Keys::unit(ks, g4));
@@ -344,7 +351,7 @@ __global__ __launch_bounds__(256) void attn_weights_few_kernel(WeightArgs a) {
       auto step = [&](int t0, auto b) {
         constexpr int cur = decltype(b)::value;
         if (t0 + 32 < k1) load(t0 + 32, 1 - cur);
-        const bool masked = t0 + 31 > first_pos;
+        const bool masked = t0 + 31 > seen;
         float sum[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {

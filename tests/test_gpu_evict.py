@@ -154,6 +154,43 @@ def test_weights(name, cache):
         assert torch.equal(narrow[i, :, :x], first[i, :, :x]) and (narrow[i, :, x:] == 7).all()
 
 
+@pytest.mark.parametrize("cache", ["bf16", "kv4"])
+@pytest.mark.parametrize("q_lens", [[3, 2], [70, 1, 9]])
+def test_weights_of_keys_that_are_not_finite(q_lens, cache):
+    """An infinite key gives nothing to rows whose score is minus infinity, and rows that do
+    not count (their log-sum-exp is not finite, as where such a key makes it so) give nothing to
+    any key; neither do the rows that fill a tile up, nor those that do not see the key."""
+    hq, hkv, d = 8, 2, 128
+    lens = [x + 60 for x in q_lens]
+    say("[evict] weights of keys that are not finite", q_lens, cache)
+    r = np.random.default_rng(71)
+    table, nb = tables(lens, 3)
+    c = cache_of(cache, nb, hkv, d)
+    m = meta(table, lens, q_lens)
+    q = rows_of(r, sum(q_lens), hq, d, "bf16")
+    q[:, :, 3] = np.where(q[:, :, 3] == 0, 1, q[:, :, 3])
+    kc, _ = c.values()
+    _, lse = paged_attention(q, kc, c.values()[1], *m, hkv)
+    lse = lse.astype(np.float32)
+    for i, L in enumerate(lens):  # the last key but one; rows that see it with a score that is not finite
+        seen = slice(m[2][i + 1] - min(2, q_lens[i]), m[2][i + 1])
+        lse[seen] = np.where(q[seen, :, 3] > 0, np.nan, lse[seen]) if cache == "bf16" else -np.inf
+    want, got = (torch.full((len(lens), hkv, max(lens)), 7.0, device="cuda") for _ in range(2))
+    args = (dev(q, torch.bfloat16), dev(lse), c.k, *map(dev, m))
+    B.attention_weights(*args, want, scales=c.scales)
+    for i, L in enumerate(lens):
+        block, slot = int(table[i][(L - 2) // 16]), (L - 2) % 16
+        if cache == "bf16":
+            c.k[block, :, 0, int(POS[slot]), 3] = float("inf")
+        else:
+            c.scales[block, :, 0, slot] = 255
+    B.attention_weights(*args, got, scales=c.scales)
+    torch.cuda.synchronize()
+    for i, L in enumerate(lens):
+        want[i, :, L - 2] = 0
+        assert torch.equal(got[i], want[i]), i
+
+
 def test_weights_of_an_attention_call():
     """From the attention call's own log-sum-exps: each row's weights sum to one, and to
     the scale that the caller gives."""
