@@ -740,8 +740,8 @@ int pa_attn_weights(const void* q, const float* lse, const void* k_cache, const 
  * (Tokens of the 8-bit cache share their block's scale and would be rounded again: read
  * them with pa_kv8_read, pick rows, append them.)  All pointers are caller-owned device
  * memory; asynchronous on stream; allocates nothing.  Errors: PA_ERR_ARG (NULL pointer with
- * work to do, negative size, caches not 16-byte, weights or kept not 4-byte aligned, tables
- * that are one with two widths), PA_ERR_UNSUPPORTED (head_dim, block_size, dtype),
+ * work to do, negative size, caches not 16-byte, weights or kept not 4-byte aligned, weights
+ * and weights_out that overlap in part, tables that are one with two widths), PA_ERR_UNSUPPORTED (head_dim, block_size, dtype),
  * PA_ERR_LAUNCH. */
 int pa_kv_evict(const float* weights, float* weights_out, int64_t weights_stride,
                 const int32_t* block_table, int32_t max_blocks_per_seq, const int32_t* new_table,

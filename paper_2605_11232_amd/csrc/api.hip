@@ -610,6 +610,10 @@ int pa_kv_evict(const float* weights, float* weights_out, int64_t weights_stride
       ((reinterpret_cast<uintptr_t>(weights) | reinterpret_cast<uintptr_t>(weights_out) |
         reinterpret_cast<uintptr_t>(kept)) & 3))
     return fail(PA_ERR_ARG, "%s: caches must be 16-byte aligned, weights and kept 4-byte", fn);
+  const uintptr_t w0 = reinterpret_cast<uintptr_t>(weights), w1 = reinterpret_cast<uintptr_t>(weights_out);
+  if (w0 != w1 && static_cast<double>(w0 < w1 ? w1 - w0 : w0 - w1) <
+                      4.0 * weights_stride * num_kv_heads * n_seqs)
+    return fail(PA_ERR_ARG, "%s: weights and weights_out overlap", fn);
   const int e = pa::dev::launch_kv_evict(
       weights, weights_out, weights_stride, block_table, max_blocks_per_seq,
       in_place ? block_table : new_table, in_place ? max_blocks_per_seq : new_max_blocks, seq_lens,

@@ -274,6 +274,15 @@ def test_evict_refusals():
         assert fn(*dict(good, **none, **kw).values()) == B.PA_OK
 
 
+def test_evict_refuses_weights_that_overlap_in_part():
+    """2 x 3 x 100 weights: 2400 bytes; an array that begins inside the other one."""
+    fn = B.lib().pa_kv_evict
+    for step in (4, 400, 2396, -4, -2396):
+        assert fn(8192, 8192 + step, 100, 64, 4, 128, 3, 64, 64, None, 2, 2, 1024, 2048, None, 16, 3, 128,
+                  16, B.PA_BF16, 64, 40, None) == B.PA_ERR_ARG, step
+        assert b"overlap" in B.lib().pa_last_error()
+
+
 def bad(code, fn, *a, **kw):
     with pytest.raises(B.PaError) as e:
         fn(*a, **kw)
