@@ -18,6 +18,7 @@ Contents
                logical token sequence, rebuilt from its block table, plus the
                oracle's own paged KV store (the same definition of the cache
                layout as the library documents, implemented independently).
+``kv8``, ``kv4``  The values that the 8-bit and the 4-bit cache hold, by their definition.
 ``brute``      Pure-Python loops over tiny inputs, no numpy, used to pin the
                vectorised float64 code.
 

@@ -1151,12 +1151,12 @@ __device__ __forceinline__ void row_item8(const int32_t* it, int g, int poff, co
   // AHEAD: two register sets of K and V^T; a step loads the next one's before it uses its
   // own, so a whole step hides the memory's latency (24 sequences of 8192-20480 keys 121
   // us, 5.9 TB/s, against 145 with one set and three wavefronts per SIMD instead of two).
-  // At head_dim 64 over the 4-bit cache one set is enough (64 sequences of 2000-8000 keys 39
-  // us, 44 with two).  Beside tiles or two-tile items, which leave two wavefronts anyway, one set, reloaded
-  // as in row_item, is as good or better: 128 decode requests on 4096 shared keys 48.6 us,
-  // 51.1 with two, 32 verifications on 16384 158 and 170 (an item ahead of the other that
-  // reads its keys finds them in no cache).  Blocks at or past kv1 read the item's last
-  // block again.
+  // Over the 4-bit cache those 24 sequences take 70 us, 5.4 TB/s; at head_dim 64 one set and
+  // three wavefronts are enough there (64 sequences of 2000-8000 keys 39 us, 44 with two).
+  // Beside tiles or two-tile items, which leave two wavefronts anyway, one set, reloaded as
+  // in row_item, is as good or better: 128 decode requests on 4096 shared keys 48.6 us, 51.1
+  // with two, 32 verifications on 16384 158 and 170 (an item ahead of the other that reads
+  // its keys finds them in no cache).  Blocks at or past kv1 read the item's last block again.
   constexpr int NB = AHEAD ? 2 : 1;
   const uint8_t* kc = reinterpret_cast<const uint8_t*>(a.kc);
   const uint8_t* vc = reinterpret_cast<const uint8_t*>(a.vc);
@@ -1416,7 +1416,8 @@ __device__ __forceinline__ void row_item8(const int32_t* it, int g, int poff, co
 // Over the 8-bit cache 16-row items at head_dim 128 take two sets of loads and two waves,
 // and the kernels that hold more than one kind of item do not fit their registers: 20 to
 // 56 spilled ones (MIX 6, 7, 15, at head_dim 64 9, too; the bf16 kernels none), stored and
-// loaded outside the key loops, at head_dim 64 also once per item of the tail lists.
+// loaded outside the key loops, at head_dim 64 also once per item of the tail lists.  Over
+// the 4-bit cache 2 to 6 spill at head_dim 128, all but MIX 2 at head_dim 64 4 to 71.
 template <int D, int MIX, int BITS>
 constexpr int waves_per_eu() {
   return (MIX == 2 && BITS == 16) || D == 64 ? 3 : kTileWavesPerEu;

@@ -35,7 +35,9 @@ struct WeightArgs {
 };
 
 constexpr int kRows = 32;  // rows at a time
-constexpr int kFewWaves = 16384;  // wavefronts wanted where rows are few
+// Wavefronts wanted where rows are few (64 requests of 2048-8192 keys: 4096 137 us, 8192 124,
+// 16384 122).
+constexpr int kFewWaves = 16384;
 
 // LDS: two tiles of rows, 16-byte unit p of row r at unit p ^ (r & 7), so that eight
 // neighbouring lanes (rows) read distinct banks; the rows' log-sum-exps (times log2 e) and
@@ -105,7 +107,12 @@ struct KeyRegs {
 };
 
 // Many rows: a workgroup's four wavefronts share each tile of 32 rows through LDS; 64 keys
-// a wavefront.
+// a wavefront, which stay in registers.  Bound by issue: a step's products and, a score, a
+// fused multiply-add, an exponential and an addition (16 sequences of 4096-12000 4-bit keys
+// under 64 rows of 28/4 heads: 76 us, of which the vector units issue for 45 and the matrix
+// units work for 25, 2.1 wavefronts a SIMD, 2.6 rounds of workgroups).  Before the rows' loads
+// went out without waits between they took 153; tiles of 64 rows 97 against 92 at the time,
+// two or eight wavefronts a workgroup, or two a SIMD, 117.
 template <int D, int BITS>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void attn_weights_kernel(WeightArgs a) {
   constexpr int KT = 2;               // 32-key tiles of a wavefront
@@ -297,7 +304,9 @@ struct KeyRegs16 {
 // Few rows (a decode or verification step): the keys are what takes time.  A wavefront
 // holds 16 NR rows in registers and goes over up to 64 blocks of keys, 32 keys ahead of those
 // that it multiplies; nothing is shared.  Sequences of more rows go over their keys once for
-// each 16 NR.
+// each 16 NR.  Bound by the keys' bytes: a decode step of 64 requests of 2048-8192 bf16 keys,
+// 32/8 heads, 121 us, 5.8 TB/s (on 32x32x16 products, whose lanes' loads of 16 bytes each lie
+// 64 apart, 149).
 template <int D, int BITS, int NR>
 __global__ __launch_bounds__(256) void attn_weights_few_kernel(WeightArgs a) {
   using Keys = KeyRegs16<D, BITS>;

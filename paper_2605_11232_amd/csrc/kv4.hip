@@ -59,7 +59,9 @@ __device__ __forceinline__ int value_word(int d, int h) {
 // its values, 8 dims a lane; 64 / (D / 4) tokens at a time, all loads issued before the
 // first is used.  The keys' codes go straight to the cache, the values' through LDS, where
 // D / 4 lanes take a square of 8 dims x 8 tokens each and transpose it; then each lane
-// stores 16 bytes, codes of tokens without rows as they were.
+// stores 16 bytes, codes of tokens without rows as they were.  Bound by the rows' bytes where
+// there are many (64 prompts of 256-1024 tokens, 8 kv-heads of 128: 173 MB read, 45 written,
+// 49 us, 4.5 TB/s), by latency where there are few (a token of 256 sequences 4.8 us).
 template <typename T, int D>
 __global__ __launch_bounds__(256) void kv4_append_kernel(const T* __restrict__ k_new,
                                                          const T* __restrict__ v_new, KvRowArgs a) {
@@ -178,7 +180,9 @@ __device__ __forceinline__ float scale_of(uint32_t byte) {
 }
 
 // One wavefront per (block, kv-head), all loads issued before the first store.  Eight dims
-// of a token a lane; the values' codes are transposed on the way, as in append.
+// of a token a lane; the values' codes are transposed on the way, as in append.  Bound by what
+// it writes, past the caches: 16 sequences of 4096-12000 tokens, 8 kv-heads of 128, 524 MB
+// written, 138 read, 119 us, 5.6 TB/s.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void kv4_read_kernel(T* __restrict__ k_out, T* __restrict__ v_out,
                                                        KvRowArgs a) {
