@@ -112,7 +112,9 @@ struct KeyRegs {
 // under 64 rows of 28/4 heads: 76 us, of which the vector units issue for 45 and the matrix
 // units work for 25, 2.1 wavefronts a SIMD, 2.6 rounds of workgroups).  Before the rows' loads
 // went out without waits between they took 153; tiles of 64 rows 97 against 92 at the time,
-// two or eight wavefronts a workgroup, or two a SIMD, 117.
+// two or eight wavefronts a workgroup, or two a SIMD, 117.  One key tile's probabilities between
+// the other's products, in one wavefront, take 123 (32 registers spilled), at two wavefronts a
+// SIMD 102: products of a single accumulator wait for each other.
 template <int D, int BITS>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void attn_weights_kernel(WeightArgs a) {
   constexpr int KT = 2;               // 32-key tiles of a wavefront
