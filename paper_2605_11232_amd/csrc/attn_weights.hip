@@ -276,6 +276,105 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void a
   }
 }
 
+// Many rows of few keys, where workgroups of 256 keys would leave most of the chip idle: a
+// workgroup owns 32 keys, each of its wavefronts goes over every 16th tile of the rows, in
+// LDS of its own without barriers, and the wavefronts' sums are added in order.  Bound by
+// latency: a tile's loads, its score products and exponentials, one after the other (one
+// sequence of 700 keys under 1680 rows of 4 kv-heads 10.9 us, 53.8 by the kernel above).
+template <int D>
+struct WaveRows {
+  __bf16 q[kRows * D];
+  float lse[kRows];
+  int pos[kRows];
+};
+template <int D, int BITS>
+__global__ __launch_bounds__(1024) void attn_weights_split_kernel(WeightArgs a) {
+  constexpr int NW = 16, KS = D / 16, UR = D / 8;
+  constexpr int NL = kRows * UR / 64;  // 16-byte units of a lane
+  __shared__ __align__(16) WaveRows<D> sm[NW];
+  __shared__ float part[NW][32];
+  const int lane = threadIdx.x & 63, j = lane & 31, hh = lane >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int x = blockIdx.x / a.chunks, first_chunk = blockIdx.x - x * a.chunks;
+  const int r = x / a.hkv, g = x - r * a.hkv;
+  const SeqRows sr = rows_of(a, r);
+  const int rows = sr.rows, L = sr.keys, G = a.hq / a.hkv;
+  if (rows == 0) return;
+  const float c = a.scale_log2;
+  const int32_t* bt = a.bt + (int64_t)r * a.max_blocks;
+  const __bf16* const q0 = a.q + ((int64_t)sr.qs * a.hq + g * G) * D + 8 * (lane % UR);
+  const float* const z0 = a.lse + (int64_t)sr.qs * a.hq + g * G;
+  WaveRows<D>& mine = sm[w];
+  u32x4 raw[NL];
+  float raw_lse = 0.f;
+  int raw_pos = 0;
+  auto load_rows = [&](int r0) {
+    const int rho = min(r0 + j, rows - 1), qi = rho / G, at = qi * a.hq + rho - qi * G;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) raw[i] = ld16(q0 + (int64_t)__shfl(at, (64 * i + lane) / UR, 64) * D);
+    raw_lse = z0[at];
+    raw_pos = r0 + j < rows ? sr.base + qi : -1;
+  };
+  for (int64_t chunk = first_chunk; chunk * 32 < L; chunk += a.chunks) {
+    const int key0 = int(chunk) * 32, key = key0 + j, kk = min(key, L - 1), last_key = min(key0 + 32, L) - 1;
+    int r0 = min(max(0, key0 - sr.base), rows / G) * G / kRows * kRows + w * kRows;
+    if (r0 < rows) load_rows(r0);
+    KeyRegs<D, BITS> raw_k;
+    raw_k.load(a, (int64_t)clamp_block(bt[kk / kBlock], a.num_blocks) * a.hkv + g, kk % kBlock, hh);
+    float sum = 0.f;
+    for (; r0 < rows; r0 += NW * kRows) {
+      wave_lds_order();
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        const int u = 64 * i + lane, lr = u / UR, p = u % UR;
+        st16(&mine.q[8 * (lr * UR + (p ^ (lr & 7)))], raw[i]);
+      }
+      const bool ok = raw_pos >= 0 && counts(raw_lse);
+      const bool all = __ballot(!ok) == 0;
+      const int seen = all ? __builtin_amdgcn_readfirstlane(raw_pos) : -1;
+      if (hh == 0) {
+        mine.lse[j] = ok ? raw_lse * kLog2e : __builtin_huge_valf();
+        mine.pos[j] = ok ? raw_pos : -1;
+      }
+      wave_lds_order();
+      if (r0 + NW * kRows < rows) load_rows(r0 + NW * kRows);
+      f32x16 s;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const int p = KeyRegs<D, BITS>::unit(ks, hh);
+        s = mfma32(as_bf16x8(ld16(&mine.q[8 * (j * UR + (p ^ (j & 7)))])), raw_k.operand(ks), s);
+      }
+      auto add = [&](auto masked) {
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          const f32x4 z = *reinterpret_cast<const f32x4*>(&mine.lse[8 * q4 + 4 * hh]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float p = fast_exp2(fmaf(s[4 * q4 + e], c, -z[e]));
+            if constexpr (decltype(masked)::value) p = key <= mine.pos[8 * q4 + 4 * hh + e] ? p : 0.f;
+            sum += p;
+          }
+        }
+      };
+      if (seen < last_key) add(std::true_type{});
+      else add(std::false_type{});
+    }
+    sum += wave_xor(sum, 32);
+    if (hh == 0) part[w][j] = sum;
+    __syncthreads();
+    if (threadIdx.x < 32 && key < L) {
+      float total = part[0][j];
+#pragma unroll
+      for (int v = 1; v < NW; ++v) total += part[v][j];
+      float* p = a.w + ((int64_t)r * a.hkv + g) * a.w_stride + key;
+      *p = a.add ? *p + total : total;
+    }
+    __syncthreads();
+  }
+}
+
 // A lane's part of a key (16x16x32 MFMA: lane (j, g4) of key j), so that the four lanes of a
 // key read the 64 bytes that lie together: dims 32 ks + 8 g4 over a bf16 cache, (D/4) g4 +
 // 8 ks over a 4-bit one.
@@ -416,7 +515,16 @@ int launch_attn_weights(const void* q, const float* lse, const void* kc, const u
   const int64_t rows = (int64_t(total_q) * (hq / hkv) + n_seqs - 1) / n_seqs;
   const bool many = rows > (bits == 16 ? 64 : 32);
   int64_t chunk = 256;  // keys of a workgroup
-  if (!many) {
+  // Where workgroups of 256 keys are few, of 32 keys.  In units of 10 ns the former, up to one
+  // a CU, take 360 + 95 for each 32 rows, a round of the latter 300 + 13 (4 kv-heads of 128,
+  // bf16; workgroups of 256 keys: us by them and by 32 keys): 448 rows 4: 17.3 and 6.3, 80:
+  // 18.1 and 16.8, 160: 18.5 and 27.7; 1680 rows 12: 53.8 and 10.9, 80: 54.6 and 33.8, 160:
+  // 56.7 and 59.4; 140 rows 24: 8.4 and 5.3, 80: 8.5 and 11.7.
+  const int64_t steps = (rows + kRows - 1) / kRows, rounds = (heads * ((keys + 31) / 32) + 255) / 256;
+  const bool split = many && rounds * (300 + 13 * steps) < 360 + 95 * steps;
+  if (split) {
+    chunk = 32;
+  } else if (!many) {
     // wavefronts of as many keys as leave enough of them to fill the chip
     a.range = int32_t(max(int64_t(1), min(int64_t(32), keys * heads / (32 * kFewWaves)))) * 32;
     chunk = 4 * a.range;
@@ -429,7 +537,9 @@ int launch_attn_weights(const void* q, const float* lse, const void* kc, const u
 #define PA_W(...) hipLaunchKernelGGL((__VA_ARGS__), grid, dim3(256), 0, stream, a)
 #define PA_W_ROWS(DD, BB)                                                     \
   {                                                                           \
-    if (many) PA_W(attn_weights_kernel<DD, BB>);                              \
+    if (split)                                                                \
+      hipLaunchKernelGGL((attn_weights_split_kernel<DD, BB>), grid, dim3(1024), 0, stream, a); \
+    else if (many) PA_W(attn_weights_kernel<DD, BB>);                         \
     else if (BB == 16 && rows > 32) PA_W(attn_weights_few_kernel<DD, 16, 4>); \
     else if (rows > 16) PA_W(attn_weights_few_kernel<DD, BB, 2>);              \
     else PA_W(attn_weights_few_kernel<DD, BB, 1>);                            \

@@ -54,6 +54,12 @@ __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_ex
 
 __device__ __forceinline__ float wave_xor(float v, int mask) { return __shfl_xor(v, mask, 64); }
 
+// Order of a wavefront's own LDS accesses: the hardware keeps it, this the compiler.
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // A wavefront's view of 64 consecutive entries of a block-table row, one per
 // lane, with the next 64 loaded one window ahead: block ids are then read with
 // v_readlane (no scalar-memory wait inside the key loop).

@@ -97,12 +97,6 @@ struct Raw8 {
   }
 };
 
-// Order of a wavefront's own LDS accesses: the hardware keeps it, this the compiler.
-__device__ __forceinline__ void wave_lds_order() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
-
 // Transpose of 4 x 4 bytes: byte i of word k becomes byte k of word i.
 __device__ __forceinline__ void transpose4(uint32_t (&w)[4]) {
   const uint32_t a = __builtin_amdgcn_perm(w[1], w[0], 0x05010400), b = __builtin_amdgcn_perm(w[1], w[0], 0x07030602);

@@ -98,6 +98,12 @@ WEIGHTS = {
     "wide-group": (64, 1, 128, [3, 1], [100, 290]),
     "one-head-each": (4, 4, 64, [1, 3, 90], [70, 33, 95]),
     "odd-group": (33, 1, 128, [4, 2], [40, 129]),
+    # enough sequences that workgroups of many keys are chosen, lengths of one and more of them
+    "sequences": (12, 4, 128, [22 + 13 * i % 79 for i in range(24)], [150 + 97 * i % 551 for i in range(24)]),
+    "sequences-64": (24, 8, 64, [11 + 9 * i % 50 for i in range(36)], [64 + 31 * i % 190 for i in range(36)]),
+    # one sequence, more tiles of rows than a workgroup has wavefronts
+    "long-prompt": (28, 4, 128, [301], [777]),
+    "long-prompt-64": (64, 8, 64, [150], [150]),
 }
 
 
