@@ -58,6 +58,12 @@ constexpr int64_t kRowWavesPerCu = 10;      // row-item split target
 // decode requests of 32/8 heads on 2048 shared keys 31.4, 27.1, 27.0, 84 at head_dim 64
 // 21.7, 18.4, 20.5.
 constexpr int64_t kRowWavesPerCu8 = 5, kWideRowWavesPerCu8 = 4;
+// Over the 4-bit cache at head_dim 64, whose items hold one set of loads and run three to a
+// SIMD, more: 135 decode requests of 496-992 keys, 32/8 heads, 24.2 us at 5, 20.5 at 8, 23 of
+// 1277-2554 14.6 and 13.2, 13 of 4261-8522 on 1102 shared 23.4 and 19.1; 43 random decode
+// launches 3.2 % less time (at 10 and 12 others lose up to 12 %).  Beside prompts' tiles no
+// more: 12 chunks of 512 tokens and 84 decode requests 154 us at 5, 157 at 8.
+constexpr int64_t kRowWavesPerCu4 = 8;
 // Up to so many keys a shared prefix's chunk there takes twice what the longest row item
 // does, unless the launch leaves every other CU without a workgroup: 64 decode requests
 // 26.9 us with chunks of 512, 29.1 with 256 (768: 33.3), 4 verifications on 4096 shared
@@ -542,7 +548,12 @@ extern "C" int pa_attn_plan(int32_t kind, int32_t n_q, int32_t n_seqs, const int
             ? kPrivateTileKeys
             : few_tile_keys(few, num_kv_heads, head_dim, num_cus, num_cus - long_tiles, row_steps,
                             !cg_keys.empty() || longest_row > kMinRowKeys);
-    const int64_t target_waves = int64_t(num_cus) * (!kv8 ? kRowWavesPerCu : wide_rows ? kWideRowWavesPerCu8 : kRowWavesPerCu8);
+    bool many_waves = dtype == PA_BF16_KV4 && head_dim == 64;
+    for (int32_t r = 0; r < n_seqs && many_waves; ++r) many_waves = qlen(r) == 0 || is_row(r);
+    const int64_t target_waves =
+        int64_t(num_cus) * (!kv8 ? kRowWavesPerCu
+                            : wide_rows ? kWideRowWavesPerCu8
+                            : many_waves ? kRowWavesPerCu4 : kRowWavesPerCu8);
     // The sequences with the fewest private keys, up to kTailWork of the row
     // work, get half-length items: ordered longest first, those run last, so
     // the launch drains sooner.  A sequence keeps at most cdiv(L, kMinRowKeys)
