@@ -60,9 +60,11 @@ constexpr int kHeld = 16;  // weights of a thread that stay in registers
 
 // NT threads (256 where rows of weights are short: its barriers are cheaper).  A wavefront
 // takes an even share of the positions, 64 at a time; up to 16 NT of them are read once, all
-// loads issued together, further ones in each pass again.  Bound by the passes' barriers and
+// loads issued together, further ones in each pass again, as many at a time.  Bound by the passes' barriers and
 // LDS atomics, not by bytes (8 kv-heads of 16 contexts of 6000-16000 tokens 19 us, 33 with the
-// weights read in each pass; of 64 contexts of 1000-2000, with 256 threads, 12, 15).
+// weights read in each pass; of 64 contexts of 1000-2000, with 256 threads, 12, 15; an eviction
+// from one 4-bit context of 45000 tokens 61, 72 with the further ones read one by one, 67 with
+// 32 NT held, which costs one of 6000 17 -> 21).
 template <int NT>
 __global__ __launch_bounds__(NT) void evict_select_kernel(EvictArgs a) {
   constexpr int kWaves = NT / 64, kBinsPer = 2048 / NT;
@@ -89,7 +91,14 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(EvictArgs a) {
 #pragma unroll
     for (int k = 0; k < kHeld; ++k)
       if (p0 + 64 * k < p1) f(p0 + 64 * k + lane, held[k]);
-    for (int i = p0 + 64 * kHeld + lane; i - lane < p1; i += 64) f(i, w[min(i, p1 - 1)]);
+    for (int i = p0 + 64 * kHeld; i < p1; i += 64 * kHeld) {
+      float x[kHeld];
+#pragma unroll
+      for (int k = 0; k < kHeld; ++k) x[k] = w[min(i + 64 * k + lane, p1 - 1)];
+#pragma unroll
+      for (int k = 0; k < kHeld; ++k)
+        if (i + 64 * k < p1) f(i + 64 * k + lane, x[k]);
+    }
   };
 
   // The want-th largest candidate T, and how many of those equal to it stay.
