@@ -663,16 +663,6 @@ def _refuse(code: int, checks):
             raise PaError(code, msg)
 
 
-def _cache_form4(t, k_cache, v_cache, scales):
-    """(element type, blocks, kv-heads, head_dim, block size, whether the tensors' shapes are
-    a 4-bit cache's) of the cache that v_cache is part of."""
-    if v_cache.dim() != 5:
-        return t.uint8, 0, 0, 0, 16, False
-    nb, hkv, c, i, o = v_cache.shape
-    return (t.uint8, nb, hkv, 32 * c, 16, i == 16 and o == 16 and scales.shape == (nb, hkv, c + 1, 16)
-            and k_cache.shape == (nb, hkv, 16, 16 * c))
-
-
 def _refuse_cache(t, bits, dt, whole, k_cache, v_cache, scales):
     _refuse(PA_ERR_UNSUPPORTED, [(
         k_cache.dtype == v_cache.dtype == dt and scales.dtype == t.uint8,
@@ -723,20 +713,30 @@ def _packed(x, heads: int, d: int) -> bool:
 
 
 def _quant_rows(fn, bits, k, v, block_table, seq_lens, cu_seqlens, k_cache, v_cache, scales, stream):
+    # a call of few rows waits for these lines: each is asked for once, and written out
     t = _torch or _torch_module()
-    if bits == 8:  # written out: a call of few rows waits for these lines
-        cdt, (nb, hkv, d, bs) = t.float8_e4m3fn, v_cache.shape
+    i32, u8, vc = t.int32, t.uint8, v_cache.shape
+    if bits == 8:
+        cdt, (nb, hkv, d, bs) = t.float8_e4m3fn, vc
         whole = k_cache.shape == (nb, hkv, d // 64, bs, 64) and scales.shape == (nb, hkv, 2)
+    elif len(vc) == 5:
+        cdt, (nb, hkv, c, i, bs) = u8, vc
+        d = 32 * c
+        whole = (i == 16 and bs == 16 and scales.shape == (nb, hkv, c + 1, 16)
+                 and k_cache.shape == (nb, hkv, 16, 16 * c))
     else:
-        cdt, nb, hkv, d, bs, whole = _cache_form4(t, k_cache, v_cache, scales)
-    shape, dt, n, i32 = k.shape, k.dtype, seq_lens.numel(), t.int32
+        cdt, nb, hkv, d, bs, whole = u8, 0, 0, 0, 16, False
+    shape, dt, n, ks, vs = k.shape, k.dtype, seq_lens.numel(), k.stride(), v.stride()
     T, code = shape[0], _ROW_DTYPES.get(dt)
-    rows, width = block_table.shape if block_table.dim() == 2 else (-1, 0)
+    table = block_table.shape
+    rows, width = table if len(table) == 2 else (-1, 0)
     dev = v_cache.get_device()
     st = _stream_on(dev, stream)
-    if not (shape == (T, hkv, d) and v.shape == shape and _packed(k, hkv, d)
-            and _packed(v, hkv, d) and code is not None and v.dtype == dt
-            and k_cache.dtype == cdt and v_cache.dtype == cdt and scales.dtype == t.uint8 and whole
+    # a row's heads packed: the last stride one, the heads' the width or of one head
+    if not (shape == (T, hkv, d) and v.shape == shape
+            and (ks[2] == vs[2] == 1 and (ks[1] == vs[1] == d or hkv == 1) or T == 0 or d == 0)
+            and code is not None and v.dtype == dt
+            and k_cache.dtype == cdt and v_cache.dtype == cdt and scales.dtype == u8 and whole
             and k_cache.is_contiguous() and v_cache.is_contiguous() and scales.is_contiguous()
             and rows >= n and cu_seqlens.numel() > n
             and block_table.dtype == i32 and seq_lens.dtype == i32 and cu_seqlens.dtype == i32
@@ -756,8 +756,8 @@ def _quant_rows(fn, bits, k, v, block_table, seq_lens, cu_seqlens, k_cache, v_ca
         _dtype_code(k)
         _refuse_device(k, v, k_cache, v_cache, scales, block_table, seq_lens, cu_seqlens)
     # a single row's stride means nothing
-    ks, vs = (k.stride(0), v.stride(0)) if T > 1 else (hkv * d, hkv * d)
-    rc = fn(k.data_ptr(), ks, v.data_ptr(), vs, block_table.data_ptr(), width,
+    k_row, v_row = (ks[0], vs[0]) if T > 1 else (hkv * d, hkv * d)
+    rc = fn(k.data_ptr(), k_row, v.data_ptr(), v_row, block_table.data_ptr(), width,
             seq_lens.data_ptr(), cu_seqlens.data_ptr(), n, T, k_cache.data_ptr(),
             v_cache.data_ptr(), scales.data_ptr(), nb, hkv, d, bs, code, st)
     if rc:
@@ -799,19 +799,25 @@ def _quant_attn_args(bits, q, k_cache, v_cache, scales, block_table, seq_lens, c
                      info, out, lse, scale, stream, workspace):
     """(arguments up to the plan info, stream) of a call over the 8- or 4-bit cache."""
     t = _torch or _torch_module()
+    i32, bf16, u8, vc, shape = t.int32, t.bfloat16, t.uint8, v_cache.shape, q.shape
     if bits == 8:
-        cdt, (nb, hkv, d, bs) = t.float8_e4m3fn, v_cache.shape
+        cdt, (nb, hkv, d, bs) = t.float8_e4m3fn, vc
         whole = k_cache.shape == (nb, hkv, d // 64, bs, 64) and scales.shape == (nb, hkv, 2)
+    elif len(vc) == 5:
+        cdt, (nb, hkv, c, i, bs) = u8, vc
+        d = 32 * c
+        whole = (i == 16 and bs == 16 and scales.shape == (nb, hkv, c + 1, 16)
+                 and k_cache.shape == (nb, hkv, 16, 16 * c))
     else:
-        cdt, nb, hkv, d, bs, whole = _cache_form4(t, k_cache, v_cache, scales)
-    total_q, hq, dq = q.shape
-    n, i32 = seq_lens.numel(), t.int32
-    rows, width = block_table.shape if block_table.dim() == 2 else (-1, 0)
+        cdt, nb, hkv, d, bs, whole = u8, 0, 0, 0, 16, False
+    total_q, hq, dq = shape
+    n, table = seq_lens.numel(), block_table.shape
+    rows, width = table if len(table) == 2 else (-1, 0)
     dev = v_cache.get_device()
     st = _stream_on(dev, stream)
-    if not (q.dtype == t.bfloat16 and out.dtype == t.bfloat16 and dq == d
-            and out.shape == q.shape and q.is_contiguous() and out.is_contiguous()
-            and k_cache.dtype == cdt and v_cache.dtype == cdt and scales.dtype == t.uint8 and whole
+    if not (q.dtype == bf16 and out.dtype == bf16 and dq == d
+            and out.shape == shape and q.is_contiguous() and out.is_contiguous()
+            and k_cache.dtype == cdt and v_cache.dtype == cdt and scales.dtype == u8 and whole
             and k_cache.is_contiguous() and v_cache.is_contiguous() and scales.is_contiguous()
             and rows >= n and cu_seqlens_q.numel() > n
             and block_table.dtype == i32 and seq_lens.dtype == i32 and cu_seqlens_q.dtype == i32
