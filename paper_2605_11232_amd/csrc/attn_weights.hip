@@ -29,6 +29,7 @@ struct WeightArgs {
   int64_t w_stride;
   int32_t max_blocks, num_blocks, total_q, hq, hkv;
   int32_t chunks;  // workgroups of a (sequence, kv-head)
+  int32_t heads;   // (sequence, kv-head) pairs, where all their first workgroups come first, or 0
   int32_t range;   // few rows: keys of a wavefront at a time
   float scale_log2;
   bool add;
@@ -125,7 +126,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void a
   __shared__ __align__(16) RowSmem<D> sm;
   const int tid = threadIdx.x, lane = tid & 63, j = lane & 31, hh = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int x = blockIdx.x / a.chunks, first_chunk = blockIdx.x - x * a.chunks;
+  int x = blockIdx.x / a.chunks, first_chunk = blockIdx.x - x * a.chunks;
+  if (a.heads > 0) {
+    first_chunk = blockIdx.x / a.heads;
+    x = (blockIdx.x - first_chunk * a.heads + first_chunk) % a.heads;
+  }
   const int r = x / a.hkv, g = x - r * a.hkv;
   const SeqRows sr = rows_of(a, r);
   const int rows = sr.rows, L = sr.keys, G = a.hq / a.hkv;
@@ -507,7 +512,7 @@ int launch_attn_weights(const void* q, const float* lse, const void* kc, const u
                         int32_t hq, int32_t hkv, int32_t d, int32_t bits, float scale, float* w,
                         int64_t w_stride, bool add, hipStream_t stream) {
   WeightArgs a{static_cast<const __bf16*>(q), lse, static_cast<const uint8_t*>(kc), scales, bt, seq_lens,
-               cu, w, w_stride, max_blocks, num_blocks, total_q, hq, hkv, 0, 0, scale * kLog2e, add};
+               cu, w, w_stride, max_blocks, num_blocks, total_q, hq, hkv, 0, 0, 0, scale * kLog2e, add};
   const int64_t heads = int64_t(n_seqs) * hkv, keys = min(w_stride, int64_t(max_blocks) * kBlock);
   // Rows of a kv-head, of the average sequence.  32 sequences of 2048-8192 keys, 32/8 heads:
   // bf16 16 rows 61 us (through LDS 94), 32 rows 67 (96), 64 rows 90 (103), 4 bits 30 (48), 42
@@ -533,6 +538,13 @@ int launch_attn_weights(const void* q, const float* lse, const void* kc, const u
   const int64_t chunks = min((keys + chunk - 1) / chunk, max(int64_t(1), 32768 / heads));
   if (heads * chunks > INT32_MAX) return static_cast<int>(hipErrorInvalidValue);
   a.chunks = int32_t(chunks);
+  // A prompt's first keys have the most rows: where new tokens are many beside the keys, all
+  // sequences' first workgroups go first, and the next ones' XCDs are others.  Else a sequence's
+  // go together, whose rows stay in the L2 caches.  us one way and the other: 33 prompts of
+  // 1167-1320 tokens, 28/4 heads, 450 and 341, 60 of 100-2000 on the 4-bit cache 1231 and 579,
+  // 12 of 1000-1500 on 3000-5000 keys, 32/8 heads, 738 and 669; 16 of 64 tokens on 4096-12000
+  // 80 and 85, 20 of 200-600 on 1000-2000 180 and 205.
+  if (many && !split && 6 * int64_t(total_q) >= keys * n_seqs) a.heads = int32_t(heads);
   const dim3 grid(unsigned(heads * chunks));
 #define PA_W(...) hipLaunchKernelGGL((__VA_ARGS__), grid, dim3(256), 0, stream, a)
 #define PA_W_ROWS(DD, BB)                                                     \

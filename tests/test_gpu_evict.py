@@ -101,6 +101,10 @@ WEIGHTS = {
     # enough sequences that workgroups of many keys are chosen, lengths of one and more of them
     "sequences": (12, 4, 128, [22 + 13 * i % 79 for i in range(24)], [150 + 97 * i % 551 for i in range(24)]),
     "sequences-64": (24, 8, 64, [11 + 9 * i % 50 for i in range(36)], [64 + 31 * i % 190 for i in range(36)]),
+    # and prompts, whose first workgroups go first
+    "prompts": (12, 4, 128, [70 + 11 * i % 130 for i in range(80)],
+                [70 + 11 * i % 130 + 20 * (i % 3) for i in range(80)]),
+    "prompts-64": (24, 8, 64, [41 + 17 * i % 90 for i in range(70)], [41 + 17 * i % 90 for i in range(70)]),
     # one sequence, more tiles of rows than a workgroup has wavefronts
     "long-prompt": (28, 4, 128, [301], [777]),
     "long-prompt-64": (64, 8, 64, [150], [150]),
