@@ -10,6 +10,8 @@
 // As in the 8-bit cache one wavefront owns one (sequence, block, kv-head) of the launch:
 // two tokens' value codes share a byte, which one wavefront reads, changes and writes.
 // Scales belong to one token, so earlier tokens' codes stay as they are.
+#include <type_traits>
+
 #include "kv_rows.h"
 
 namespace pa {
@@ -155,9 +157,10 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(const T* __restrict__ k
   }
 }
 
-// Eight codes times a power of two (or NaN), stored as T.
+// Codes times a power of two (or NaN), 16 bytes of them stored as T: eight bf16 numbers, or
+// the four low codes in float32.
 template <typename T>
-__device__ __forceinline__ void store8(T* p, uint32_t c, float s) {
+__device__ __forceinline__ void store16(T* p, uint32_t c, float s) {
   if constexpr (sizeof(T) == 2) {
     u32x4 r;
     r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0));
@@ -168,9 +171,7 @@ __device__ __forceinline__ void store8(T* p, uint32_t c, float s) {
                                 reinterpret_cast<u32x4*>(p));
   } else {
     const f32x2 r0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.f, 0), r1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.f, 1);
-    const f32x2 r2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.f, 2), r3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.f, 3);
     __builtin_nontemporal_store(f32x4{r0[0] * s, r0[1] * s, r1[0] * s, r1[1] * s}, reinterpret_cast<f32x4*>(p));
-    __builtin_nontemporal_store(f32x4{r2[0] * s, r2[1] * s, r3[0] * s, r3[1] * s}, reinterpret_cast<f32x4*>(p + 4));
   }
 }
 
@@ -179,18 +180,22 @@ __device__ __forceinline__ float scale_of(uint32_t byte) {
   return byte == kScaleNan ? __builtin_nanf("") : __uint_as_float(byte << 23);
 }
 
-// One wavefront per (block, kv-head), all loads issued before the first store.  Eight dims
-// of a token a lane; the values' codes are transposed on the way, as in append.  Bound by what
-// it writes, past the caches: 16 sequences of 4096-12000 tokens, 8 kv-heads of 128, 524 MB
-// written, 138 read, 119 us, 5.6 TB/s.
+// One wavefront per (block, kv-head), all loads issued before the first store.  16 bytes of a
+// token's row a lane, so that a store is of whole lines (float32 rows written as two halves of
+// 32 bytes a lane took 191 us for 64 x 640 tokens, 63 this way); the values' codes are
+// transposed on the way, as in append.  Bound by what it writes, past the caches: 16 sequences
+// of 4096-12000 tokens, 8 kv-heads of 128, 524 MB written, 138 read, 119 us, 5.6 TB/s.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void kv4_read_kernel(T* __restrict__ k_out, T* __restrict__ v_out,
                                                        KvRowArgs a) {
-  constexpr int LR = D / 8;          // lanes of a token
+  constexpr int W = D / 8;           // words of a token's codes
+  constexpr int PD = 16 / sizeof(T); // dims of a lane
+  constexpr int LR = D / PD;         // lanes of a token
   constexpr int TI = 64 / LR;        // tokens at a time
+  typedef typename std::conditional<PD == 8, uint32_t, uint16_t>::type Codes;
   constexpr int NI = kBlock / TI;
   constexpr int NS = D / 32 + 1;
-  __shared__ __align__(16) uint32_t vt_sh[4][kBlock][LR + 1];
+  __shared__ __align__(16) uint32_t vt_sh[4][kBlock][W + 1];
   __shared__ __align__(16) uint32_t vb_sh[4][2 * D];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t i = (int64_t)blockIdx.x * 4 + w;
@@ -200,25 +205,26 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(T* __restrict__ k_out, T*
   const BlockRows b = find_rows(a, int(slot));
   if (b.off0 == b.off1 || b.id < 0 || b.id >= a.num_blocks) return;
   const int64_t bh = (int64_t)b.id * a.hkv + h;
-  const uint32_t* kb = reinterpret_cast<const uint32_t*>(a.kc + bh * (kBlock * D / 2));
+  const Codes* kb = reinterpret_cast<const Codes*>(a.kc + bh * (kBlock * D / 2));
   const uint8_t* vb = a.vc + bh * (kBlock * D / 2);
   const uint8_t* sb = a.scales + bh * (NS * kBlock);
-  uint32_t (*vt)[LR + 1] = vt_sh[w];
+  uint32_t (*vt)[W + 1] = vt_sh[w];
   uint32_t* vn = vb_sh[w];
   const int c = lane % LR, sub = lane / LR;
-  uint32_t k[NI], sk[NI], sv[NI];
+  Codes k[NI];
+  uint8_t sk[NI], sv[NI];
   u32x4 v = zero16();
   if (lane < D / 2) v = ld16(vb + 16 * lane);
 #pragma unroll
   for (int u = 0; u < NI; ++u) {
     k[u] = kb[u * 64 + lane];
-    sk[u] = sb[c / 4 * kBlock + u * TI + sub];
+    sk[u] = sb[c * PD / 32 * kBlock + u * TI + sub];
     sv[u] = sb[(NS - 1) * kBlock + u * TI + sub];
   }
   if (lane < D / 2) st16(vn + 4 * lane, v);
   wave_lds_order();
   if (lane < D / 4) {
-    const int dw = lane % LR, half = lane / LR;
+    const int dw = lane % W, half = lane / W;
     uint32_t q[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) q[j] = vn[value_word(8 * dw + j, half)];
@@ -232,8 +238,9 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(T* __restrict__ k_out, T*
     const int o = u * TI + sub;
     if (o < b.off0 || o >= b.off1) continue;
     const int64_t row = b.row0 + o - b.off0;
-    store8(k_out + row * a.k_stride + (int64_t)h * D + 8 * c, k[u], scale_of(sk[u]));
-    store8(v_out + row * a.v_stride + (int64_t)h * D + 8 * c, vt[o][c], scale_of(sv[u]));
+    const uint32_t v_codes = PD == 8 ? vt[o][c] : vt[o][c / 2] >> (16 * (c % 2));
+    store16(k_out + row * a.k_stride + (int64_t)h * D + PD * c, k[u], scale_of(sk[u]));
+    store16(v_out + row * a.v_stride + (int64_t)h * D + PD * c, v_codes, scale_of(sv[u]));
   }
 }
 
