@@ -81,15 +81,20 @@ __device__ __forceinline__ float pow2(int e) { return __uint_as_float(uint32_t(e
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
-// Eight values of T as loaded, and as float32.  Non-temporal: the rows are read once (64
-// prompts whose rows are in no cache 49 us, 55 with plain loads; 46 where the last-level
-// cache holds them all).
+// Eight values of T as loaded, and as float32.  Non-temporal where a load takes whole lines:
+// the rows are read once (64 bf16 prompts whose rows are in no cache 49 us, 55 with plain
+// loads; 46 where the last-level cache holds them all).  A float32 row's lines are read in two
+// halves of each lane's 32 bytes, the second from the cache (128000 tokens, 8 kv-heads of 128,
+// to the 4-bit cache 243 us, 258 with non-temporal loads, to the 8-bit one 257 and 276).
 template <typename T>
 struct Raw8 {
   u32x4 x[sizeof(T) / 2];
   __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-    for (size_t i = 0; i < sizeof(T) / 2; ++i) x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + 16 / sizeof(T) * i));
+    for (size_t i = 0; i < sizeof(T) / 2; ++i) {
+      const u32x4* q = reinterpret_cast<const u32x4*>(p + 16 / sizeof(T) * i);
+      x[i] = sizeof(T) == 2 ? __builtin_nontemporal_load(q) : *q;
+    }
   }
   __device__ __forceinline__ float at(int i) const {
     if constexpr (sizeof(T) == 2) return __uint_as_float(i % 2 ? x[0][i / 2] & 0xFFFF0000u : x[0][i / 2] << 16);
