@@ -282,22 +282,25 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void a
 }
 
 // Many rows of few keys, where workgroups of 256 keys would leave most of the chip idle: a
-// workgroup owns 32 keys, each of its wavefronts goes over every 16th tile of the rows, in
-// LDS of its own without barriers, and the wavefronts' sums are added in order.  Bound by
-// latency: a tile's loads, its score products and exponentials, one after the other (one
-// sequence of 700 keys under 1680 rows of 4 kv-heads 10.9 us, 53.8 by the kernel above).
+// workgroup owns 32 KT keys, each of its NW wavefronts goes over every NW-th tile of the rows,
+// in LDS of its own without barriers, and the wavefronts' sums are added in order.  8
+// wavefronts on 64 keys, or 16 on 32 where those are no more workgroups than CUs (12 on 64
+// are 5 to 20 % slower than 8).  Bound by latency and by the rows' way through LDS, which 64
+// keys share instead of 256 (one sequence of 700 keys under 1680 rows of 4 kv-heads 10.9 us,
+// 53.8 by the kernel above; in which two or three groups of wavefronts that divide the rows
+// take as long as one up to 256 workgroups, since their barriers keep them in step).
 template <int D>
 struct WaveRows {
   __bf16 q[kRows * D];
   float lse[kRows];
   int pos[kRows];
 };
-template <int D, int BITS>
-__global__ __launch_bounds__(1024) void attn_weights_split_kernel(WeightArgs a) {
-  constexpr int NW = 16, KS = D / 16, UR = D / 8;
+template <int D, int BITS, int NW, int KT>
+__global__ __launch_bounds__(64 * NW) void attn_weights_split_kernel(WeightArgs a) {
+  constexpr int KS = D / 16, UR = D / 8, kChunk = 32 * KT;
   constexpr int NL = kRows * UR / 64;  // 16-byte units of a lane
   __shared__ __align__(16) WaveRows<D> sm[NW];
-  __shared__ float part[NW][32];
+  __shared__ float part[NW][kChunk];
   const int lane = threadIdx.x & 63, j = lane & 31, hh = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int x = blockIdx.x / a.chunks, first_chunk = blockIdx.x - x * a.chunks;
@@ -320,13 +323,21 @@ __global__ __launch_bounds__(1024) void attn_weights_split_kernel(WeightArgs a) 
     raw_lse = z0[at];
     raw_pos = r0 + j < rows ? sr.base + qi : -1;
   };
-  for (int64_t chunk = first_chunk; chunk * 32 < L; chunk += a.chunks) {
-    const int key0 = int(chunk) * 32, key = key0 + j, kk = min(key, L - 1), last_key = min(key0 + 32, L) - 1;
+  for (int64_t chunk = first_chunk; chunk * kChunk < L; chunk += a.chunks) {
+    const int key0 = int(chunk) * kChunk, last_key = min(key0 + kChunk, L) - 1;
     int r0 = min(max(0, key0 - sr.base), rows / G) * G / kRows * kRows + w * kRows;
     if (r0 < rows) load_rows(r0);
-    KeyRegs<D, BITS> raw_k;
-    raw_k.load(a, (int64_t)clamp_block(bt[kk / kBlock], a.num_blocks) * a.hkv + g, kk % kBlock, hh);
-    float sum = 0.f;
+    bf16x8 k[KT][KS];
+    float sum[KT];
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+      const int kk = min(key0 + 32 * t + j, L - 1);
+      KeyRegs<D, BITS> raw_k;
+      raw_k.load(a, (int64_t)clamp_block(bt[kk / kBlock], a.num_blocks) * a.hkv + g, kk % kBlock, hh);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) k[t][ks] = raw_k.operand(ks);
+      sum[t] = 0.f;
+    }
     for (; r0 < rows; r0 += NW * kRows) {
       wave_lds_order();
 #pragma unroll
@@ -343,36 +354,47 @@ __global__ __launch_bounds__(1024) void attn_weights_split_kernel(WeightArgs a) 
       }
       wave_lds_order();
       if (r0 + NW * kRows < rows) load_rows(r0 + NW * kRows);
-      f32x16 s;
+      f32x16 s[KT];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = 0.f;
+      for (int t = 0; t < KT; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         const int p = KeyRegs<D, BITS>::unit(ks, hh);
-        s = mfma32(as_bf16x8(ld16(&mine.q[8 * (j * UR + (p ^ (j & 7)))])), raw_k.operand(ks), s);
+        const bf16x8 q = as_bf16x8(ld16(&mine.q[8 * (j * UR + (p ^ (j & 7)))]));
+#pragma unroll
+        for (int t = 0; t < KT; ++t) s[t] = mfma32(q, k[t][ks], s[t]);
       }
       auto add = [&](auto masked) {
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4) {
           const f32x4 z = *reinterpret_cast<const f32x4*>(&mine.lse[8 * q4 + 4 * hh]);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float p = fast_exp2(fmaf(s[4 * q4 + e], c, -z[e]));
-            if constexpr (decltype(masked)::value) p = key <= mine.pos[8 * q4 + 4 * hh + e] ? p : 0.f;
-            sum += p;
-          }
+          for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float p = fast_exp2(fmaf(s[t][4 * q4 + e], c, -z[e]));
+              if constexpr (decltype(masked)::value)
+                p = key0 + 32 * t + j <= mine.pos[8 * q4 + 4 * hh + e] ? p : 0.f;
+              sum[t] += p;
+            }
         }
       };
       if (seen < last_key) add(std::true_type{});
       else add(std::false_type{});
     }
-    sum += wave_xor(sum, 32);
-    if (hh == 0) part[w][j] = sum;
-    __syncthreads();
-    if (threadIdx.x < 32 && key < L) {
-      float total = part[0][j];
 #pragma unroll
-      for (int v = 1; v < NW; ++v) total += part[v][j];
+    for (int t = 0; t < KT; ++t) {
+      sum[t] += wave_xor(sum[t], 32);
+      if (hh == 0) part[w][32 * t + j] = sum[t];
+    }
+    __syncthreads();
+    const int key = key0 + threadIdx.x;
+    if (threadIdx.x < kChunk && key < L) {
+      float total = part[0][threadIdx.x];
+#pragma unroll
+      for (int v = 1; v < NW; ++v) total += part[v][threadIdx.x];
       float* p = a.w + ((int64_t)r * a.hkv + g) * a.w_stride + key;
       *p = a.add ? *p + total : total;
     }
@@ -520,15 +542,19 @@ int launch_attn_weights(const void* q, const float* lse, const void* kc, const u
   const int64_t rows = (int64_t(total_q) * (hq / hkv) + n_seqs - 1) / n_seqs;
   const bool many = rows > (bits == 16 ? 64 : 32);
   int64_t chunk = 256;  // keys of a workgroup
-  // Where workgroups of 256 keys are few, of 32 keys.  In units of 10 ns the former, up to one
-  // a CU, take 360 + 95 for each 32 rows, a round of the latter 300 + 13 (4 kv-heads of 128,
-  // bf16; workgroups of 256 keys: us by them and by 32 keys): 448 rows 4: 17.3 and 6.3, 80:
-  // 18.1 and 16.8, 160: 18.5 and 27.7; 1680 rows 12: 53.8 and 10.9, 80: 54.6 and 33.8, 160:
-  // 56.7 and 59.4; 140 rows 24: 8.4 and 5.3, 80: 8.5 and 11.7.
-  const int64_t steps = (rows + kRows - 1) / kRows, rounds = (heads * ((keys + 31) / 32) + 255) / 256;
-  const bool split = many && rounds * (300 + 13 * steps) < 360 + 95 * steps;
+  // Where workgroups of 256 keys are few, of 64 keys, and of 32 where those are no more than
+  // CUs.  In units of 10 ns the first, up to one a CU, take 360 + 95 for each 32 rows, a round
+  // of the second 500 + 20, at head_dim 64 300 + 12 (4 or 8 kv-heads of 128, bf16; workgroups
+  // of 256 keys: us by them, by 64 keys and by 32): 1200 rows 16: 41 11.3 9.1, 64: 42 17.1 24,
+  // 192: 44 39 55, 256: 45 48 70; 120 rows 64: 7.6 5.6 8.1, 128: 7.8 9.1 13.7; 10500 rows
+  // 24: 322 62 50, 96: 327 119 140, 192: 327 194 265, 384: 339 353 507.
+  const int64_t steps = (rows + kRows - 1) / kRows, n64 = heads * ((keys + 63) / 64);
+  const bool split = many && n64 <= 2048 &&
+                     max(n64, int64_t(256)) * (d == 64 ? 300 + 12 * steps : 500 + 20 * steps) <
+                         256 * (360 + 95 * steps);
+  const bool fine = split && heads * ((keys + 31) / 32) <= 256;
   if (split) {
-    chunk = 32;
+    chunk = fine ? 32 : 64;
   } else if (!many) {
     // wavefronts of as many keys as leave enough of them to fill the chip
     a.range = int32_t(max(int64_t(1), min(int64_t(32), keys * heads / (32 * kFewWaves)))) * 32;
@@ -549,8 +575,10 @@ int launch_attn_weights(const void* q, const float* lse, const void* kc, const u
 #define PA_W(...) hipLaunchKernelGGL((__VA_ARGS__), grid, dim3(256), 0, stream, a)
 #define PA_W_ROWS(DD, BB)                                                     \
   {                                                                           \
-    if (split)                                                                \
-      hipLaunchKernelGGL((attn_weights_split_kernel<DD, BB>), grid, dim3(1024), 0, stream, a); \
+    if (fine)                                                                 \
+      hipLaunchKernelGGL((attn_weights_split_kernel<DD, BB, 16, 1>), grid, dim3(1024), 0, stream, a); \
+    else if (split)                                                           \
+      hipLaunchKernelGGL((attn_weights_split_kernel<DD, BB, 8, 2>), grid, dim3(512), 0, stream, a); \
     else if (many) PA_W(attn_weights_kernel<DD, BB>);                         \
     else if (BB == 16 && rows > 32) PA_W(attn_weights_few_kernel<DD, 16, 4>); \
     else if (rows > 16) PA_W(attn_weights_few_kernel<DD, BB, 2>);              \

@@ -105,6 +105,9 @@ WEIGHTS = {
     "prompts": (12, 4, 128, [70 + 11 * i % 130 for i in range(80)],
                 [70 + 11 * i % 130 + 20 * (i % 3) for i in range(80)]),
     "prompts-64": (24, 8, 64, [41 + 17 * i % 90 for i in range(70)], [41 + 17 * i % 90 for i in range(70)]),
+    # few sequences: workgroups of 64 keys
+    "some": (8, 4, 128, [90, 33, 140, 61, 100, 75], [700, 1033, 340, 61, 905, 500]),
+    "some-64": (16, 8, 64, [40, 77, 120], [840, 1277, 620]),
     # one sequence, more tiles of rows than a workgroup has wavefronts
     "long-prompt": (28, 4, 128, [301], [777]),
     "long-prompt-64": (64, 8, 64, [150], [150]),
@@ -155,13 +158,15 @@ def test_weights(name, cache):
         assert torch.all((w[i, :, :lens[i]].double() - 2 * x).abs() <= 4 * pieces * 2.0 ** -24 * x)
     say(f"[evict] {name}: worst {worst:.2f} of the bound")
     assert (first[n] == 7).all()
-    # an array narrower than the sequences: the keys that fit
+    # an array narrower than the sequences: the keys that fit.  How the rows are divided goes by
+    # the array's width, too, so that a sum's order may be another; it is as near the formula.
     narrow = torch.full((n, hkv, max(1, max(lens) // 2)), 7.0, device="cuda")
     B.attention_weights(*args, narrow, scales=c.scales)
     torch.cuda.synchronize()
     for i in range(n):
         x = min(lens[i], narrow.shape[2]) if q_lens[i] else 0
-        assert torch.equal(narrow[i, :, :x], first[i, :, :x]) and (narrow[i, :, x:] == 7).all()
+        got = narrow[i].double().cpu().numpy()
+        assert np.all(np.abs(got[:, :x] - ref[i][:, :x]) <= bound[i][:, :x]) and (got[:, x:] == 7).all()
 
 
 @pytest.mark.parametrize("cache", ["bf16", "kv4"])
