@@ -61,7 +61,7 @@ constexpr int kHeld = 16;  // weights of a thread that stay in registers
 // NT threads (256 where rows of weights are short: its barriers are cheaper).  A wavefront
 // takes an even share of the positions, 64 at a time; up to 16 NT of them are read once, all
 // loads issued together, further ones in each pass again, as many at a time.  Bound by the passes' barriers and
-// LDS atomics, not by bytes (8 kv-heads of 16 contexts of 6000-16000 tokens 19 us, 33 with the
+// LDS atomics, not by bytes (8 kv-heads of 16 contexts of 6000-16000 tokens 18 us, 33 with the
 // weights read in each pass; of 64 contexts of 1000-2000, with 256 threads, 12, 15; an eviction
 // from one 4-bit context of 45000 tokens 61, 72 with the further ones read one by one, 67 with
 // 32 NT held, which costs one of 6000 17 -> 21).
@@ -83,21 +83,26 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(EvictArgs a) {
   const int share = (n.len + NT - 1) / NT * 64;
   const int p0 = min(wv * share, n.len), p1 = min(p0 + share, n.len);
 
+  // A candidate's order, 0 (less than that of any number) for other positions.
+  auto order = [&](int i, float x) { return i >= lo && i < hi && i < p1 ? order_of(x) : 0u; };
   float held[kHeld];
+  uint32_t orders[kHeld];
 #pragma unroll
   for (int k = 0; k < kHeld; ++k) held[k] = w[max(min(p0 + 64 * k + lane, p1 - 1), 0)];
-  // f(position, weight) for the wavefront's positions, 64 at a time
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k) orders[k] = order(p0 + 64 * k + lane, held[k]);
+  // f(position, weight, order) for the wavefront's positions, 64 at a time
   auto each = [&](auto f) {
 #pragma unroll
     for (int k = 0; k < kHeld; ++k)
-      if (p0 + 64 * k < p1) f(p0 + 64 * k + lane, held[k]);
+      if (p0 + 64 * k < p1) f(p0 + 64 * k + lane, held[k], orders[k]);
     for (int i = p0 + 64 * kHeld; i < p1; i += 64 * kHeld) {
       float x[kHeld];
 #pragma unroll
       for (int k = 0; k < kHeld; ++k) x[k] = w[min(i + 64 * k + lane, p1 - 1)];
 #pragma unroll
       for (int k = 0; k < kHeld; ++k)
-        if (i + 64 * k < p1) f(i + 64 * k + lane, x[k]);
+        if (i + 64 * k < p1) f(i + 64 * k + lane, x[k], order(i + 64 * k + lane, x[k]));
     }
   };
 
@@ -112,9 +117,8 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(EvictArgs a) {
     constexpr int kShift[3] = {21, 10, 0}, kMask[3] = {2047, 2047, 1023};
 #pragma unroll
     for (int d = 0; d < 3; ++d) {
-      each([&](int i, float x) {
-        const uint32_t u = order_of(x);
-        if (i >= lo && i < hi && (u & known) == prefix) atomicAdd(&hist[d][u >> kShift[d] & kMask[d]], 1);
+      each([&](int, float, uint32_t u) {
+        if (u != 0 && (u & known) == prefix) atomicAdd(&hist[d][u >> kShift[d] & kMask[d]], 1);
       });
       __syncthreads();
       // Counts from the largest digit down, kBinsPer of them a thread.
@@ -153,16 +157,14 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(EvictArgs a) {
 
   // How many of a wavefront's positions stay, and how many equal T.
   // 0: goes, 1: equals T, 2: stays
-  auto kind = [&](int i, float x) {
-    if (i >= p1) return 0;
-    if (i < lo || i >= hi) return 2;
+  auto kind = [&](int i, uint32_t u) {
+    if (u == 0) return i < p1 ? 2 : 0;  // first and last ones; behind the wavefront's
     if (want <= 0) return 0;
-    const uint32_t u = order_of(x);
     return u > T ? 2 : u == T ? 1 : 0;
   };
   int stay = 0, equal = 0;
-  each([&](int i, float x) {
-    const int k = kind(i, x);
+  each([&](int i, float, uint32_t u) {
+    const int k = kind(i, u);
     stay += __popcll(__ballot(k == 2));
     equal += __popcll(__ballot(k == 1));
   });
@@ -175,8 +177,8 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(EvictArgs a) {
     eq += part[1][v];
   }
   const uint64_t below = (uint64_t(1) << lane) - 1;
-  each([&](int i, float x) {
-    const int k = kind(i, x);
+  each([&](int i, float x, uint32_t u) {
+    const int k = kind(i, u);
     const uint64_t e = __ballot(k == 1);
     const bool keep = k == 2 || (k == 1 && eq + __popcll(e & below) < ties);
     const uint64_t m = __ballot(keep);
