@@ -31,6 +31,9 @@ struct WeightArgs {
   int32_t chunks;  // workgroups of a (sequence, kv-head)
   int32_t heads;   // (sequence, kv-head) pairs, where all their first workgroups come first, or 0
   int32_t range;   // few rows: keys of a wavefront at a time
+  int32_t n_seqs;
+  int32_t limit;   // few rows: sequences of more rows are left to the other kernels, which take
+  bool longs;      // only those then
   float scale_log2;
   bool add;
 };
@@ -61,6 +64,21 @@ __device__ __forceinline__ SeqRows rows_of(const WeightArgs& a, int r) {
   const int n = min(a.cu[r + 1], a.total_q) - qs;
   if (qs < 0 || n <= 0 || L < all) return {0, 0, 0, 0};
   return {qs, n * (a.hq / a.hkv), L - all, int(min(int64_t(L), min(a.w_stride, int64_t(a.max_blocks) * kBlock)))};
+}
+// The n-th sequence of more than a.limit rows, or -1.
+__device__ __forceinline__ int nth_long(const WeightArgs& a, int n) {
+  const int lane = threadIdx.x & 63;
+  for (int r0 = 0; r0 < a.n_seqs; r0 += 64) {
+    const int r = r0 + lane;
+    uint64_t m = __ballot(r < a.n_seqs && rows_of(a, min(r, a.n_seqs - 1)).rows > a.limit);
+    const int c = __popcll(m);
+    if (n < c) {
+      for (; n > 0; --n) m &= m - 1;
+      return r0 + __builtin_ctzll(m);
+    }
+    n -= c;
+  }
+  return -1;
 }
 __device__ __forceinline__ bool counts(float lse) { return fabsf(lse) < __builtin_huge_valf(); }
 
@@ -131,7 +149,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void a
     first_chunk = blockIdx.x / a.heads;
     x = (blockIdx.x - first_chunk * a.heads + first_chunk) % a.heads;
   }
-  const int r = x / a.hkv, g = x - r * a.hkv;
+  int r = x / a.hkv;
+  const int g = x - r * a.hkv;
+  if (a.longs) {
+    r = __builtin_amdgcn_readfirstlane(nth_long(a, r));
+    if (r < 0) return;
+  }
   const SeqRows sr = rows_of(a, r);
   const int rows = sr.rows, L = sr.keys, G = a.hq / a.hkv;
   if (rows == 0) return;
@@ -304,7 +327,12 @@ __global__ __launch_bounds__(64 * NW) void attn_weights_split_kernel(WeightArgs 
   const int lane = threadIdx.x & 63, j = lane & 31, hh = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int x = blockIdx.x / a.chunks, first_chunk = blockIdx.x - x * a.chunks;
-  const int r = x / a.hkv, g = x - r * a.hkv;
+  int r = x / a.hkv;
+  const int g = x - r * a.hkv;
+  if (a.longs) {
+    r = __builtin_amdgcn_readfirstlane(nth_long(a, r));
+    if (r < 0) return;
+  }
   const SeqRows sr = rows_of(a, r);
   const int rows = sr.rows, L = sr.keys, G = a.hq / a.hkv;
   if (rows == 0) return;
@@ -448,7 +476,7 @@ __global__ __launch_bounds__(256) void attn_weights_few_kernel(WeightArgs a) {
   const int32_t* bt = a.bt + (int64_t)r * a.max_blocks;
   float* wp = a.w + ((int64_t)r * a.hkv + g) * a.w_stride;
   const float c = a.scale_log2;
-  for (int64_t i = (blockIdx.x - x * a.chunks) * 4 + w; i * a.range < L && sr.rows > 0; i += 4 * a.chunks) {
+  for (int64_t i = (blockIdx.x - x * a.chunks) * 4 + w; i * a.range < L && sr.rows > 0 && sr.rows <= a.limit; i += 4 * a.chunks) {
     const int k0 = int(i) * a.range, k1 = min(k0 + a.range, L);
     BlockSpan span;
     span.init(bt, a.max_blocks, k0 / kBlock);
@@ -528,19 +556,11 @@ __global__ __launch_bounds__(256) void attn_weights_few_kernel(WeightArgs a) {
 
 }  // namespace
 
-int launch_attn_weights(const void* q, const float* lse, const void* kc, const uint8_t* scales,
-                        int32_t num_blocks, const int32_t* bt, int32_t max_blocks,
-                        const int32_t* seq_lens, const int32_t* cu, int32_t n_seqs, int32_t total_q,
-                        int32_t hq, int32_t hkv, int32_t d, int32_t bits, float scale, float* w,
-                        int64_t w_stride, bool add, hipStream_t stream) {
-  WeightArgs a{static_cast<const __bf16*>(q), lse, static_cast<const uint8_t*>(kc), scales, bt, seq_lens,
-               cu, w, w_stride, max_blocks, num_blocks, total_q, hq, hkv, 0, 0, 0, scale * kLog2e, add};
-  const int64_t heads = int64_t(n_seqs) * hkv, keys = min(w_stride, int64_t(max_blocks) * kBlock);
-  // Rows of a kv-head, of the average sequence.  32 sequences of 2048-8192 keys, 32/8 heads:
-  // bf16 16 rows 61 us (through LDS 94), 32 rows 67 (96), 64 rows 90 (103), 4 bits 30 (48), 42
-  // (49), 76 (59).
-  const int64_t rows = (int64_t(total_q) * (hq / hkv) + n_seqs - 1) / n_seqs;
-  const bool many = rows > (bits == 16 ? 64 : 32);
+// The kernels for many rows: n_seqs sequences at most, of which the host reckons with `likely`
+// of `rows` rows a kv-head.
+void launch_many(WeightArgs a, int64_t n_seqs, int64_t rows, int64_t likely, int64_t keys, int32_t d,
+                 int32_t bits, hipStream_t stream) {
+  const int64_t heads = n_seqs * a.hkv;
   int64_t chunk = 256;  // keys of a workgroup
   // Where workgroups of 256 keys are few, of 64 keys, and of 32 where those are no more than
   // CUs.  In units of 10 ns the first, up to one a CU, take 360 + 95 for each 32 rows, a round
@@ -548,21 +568,13 @@ int launch_attn_weights(const void* q, const float* lse, const void* kc, const u
   // of 256 keys: us by them, by 64 keys and by 32): 1200 rows 16: 41 11.3 9.1, 64: 42 17.1 24,
   // 192: 44 39 55, 256: 45 48 70; 120 rows 64: 7.6 5.6 8.1, 128: 7.8 9.1 13.7; 10500 rows
   // 24: 322 62 50, 96: 327 119 140, 192: 327 194 265, 384: 339 353 507.
-  const int64_t steps = (rows + kRows - 1) / kRows, n64 = heads * ((keys + 63) / 64);
-  const bool split = many && n64 <= 2048 &&
-                     max(n64, int64_t(256)) * (d == 64 ? 300 + 12 * steps : 500 + 20 * steps) <
-                         256 * (360 + 95 * steps);
-  const bool fine = split && heads * ((keys + 31) / 32) <= 256;
-  if (split) {
-    chunk = fine ? 32 : 64;
-  } else if (!many) {
-    // wavefronts of as many keys as leave enough of them to fill the chip
-    a.range = int32_t(max(int64_t(1), min(int64_t(32), keys * heads / (32 * kFewWaves)))) * 32;
-    chunk = 4 * a.range;
-  }
+  const int64_t steps = (rows + kRows - 1) / kRows, n64 = likely * a.hkv * ((keys + 63) / 64);
+  const bool split = n64 <= 2048 && max(n64, int64_t(256)) * (d == 64 ? 300 + 12 * steps : 500 + 20 * steps) <
+                                        256 * (360 + 95 * steps);
+  const bool fine = split && likely * a.hkv * ((keys + 31) / 32) <= 256;
+  if (split) chunk = fine ? 32 : 64;
   // few workgroups without keys where the array is wider than the sequences are long
   const int64_t chunks = min((keys + chunk - 1) / chunk, max(int64_t(1), 32768 / heads));
-  if (heads * chunks > INT32_MAX) return static_cast<int>(hipErrorInvalidValue);
   a.chunks = int32_t(chunks);
   // A prompt's first keys have the most rows: where new tokens are many beside the keys, all
   // sequences' first workgroups go first, and the next ones' XCDs are others.  Else a sequence's
@@ -570,30 +582,69 @@ int launch_attn_weights(const void* q, const float* lse, const void* kc, const u
   // 1167-1320 tokens, 28/4 heads, 450 and 341, 60 of 100-2000 on the 4-bit cache 1231 and 579,
   // 12 of 1000-1500 on 3000-5000 keys, 32/8 heads, 738 and 669; 16 of 64 tokens on 4096-12000
   // 80 and 85, 20 of 200-600 on 1000-2000 180 and 205.
-  if (many && !split && 6 * int64_t(total_q) >= keys * n_seqs) a.heads = int32_t(heads);
+  if (!split && 6 * rows >= keys * (a.hq / a.hkv)) a.heads = int32_t(heads);
   const dim3 grid(unsigned(heads * chunks));
-#define PA_W(...) hipLaunchKernelGGL((__VA_ARGS__), grid, dim3(256), 0, stream, a)
-#define PA_W_ROWS(DD, BB)                                                     \
-  {                                                                           \
-    if (fine)                                                                 \
-      hipLaunchKernelGGL((attn_weights_split_kernel<DD, BB, 16, 1>), grid, dim3(1024), 0, stream, a); \
-    else if (split)                                                           \
-      hipLaunchKernelGGL((attn_weights_split_kernel<DD, BB, 8, 2>), grid, dim3(512), 0, stream, a); \
-    else if (many) PA_W(attn_weights_kernel<DD, BB>);                         \
-    else if (BB == 16 && rows > 32) PA_W(attn_weights_few_kernel<DD, 16, 4>); \
-    else if (rows > 16) PA_W(attn_weights_few_kernel<DD, BB, 2>);              \
-    else PA_W(attn_weights_few_kernel<DD, BB, 1>);                            \
+#define PA_W(N, ...) hipLaunchKernelGGL((__VA_ARGS__), grid, dim3(N), 0, stream, a)
+#define PA_W_MANY(DD, BB)                                              \
+  {                                                                    \
+    if (fine) PA_W(1024, attn_weights_split_kernel<DD, BB, 16, 1>);    \
+    else if (split) PA_W(512, attn_weights_split_kernel<DD, BB, 8, 2>); \
+    else PA_W(256, attn_weights_kernel<DD, BB>);                       \
   }
-#define PA_W_BITS(DD)               \
-  if (bits == 16) PA_W_ROWS(DD, 16) \
-  else PA_W_ROWS(DD, 4)
-  if (d == 128) {
-    PA_W_BITS(128)
-  } else {
-    PA_W_BITS(64)
+#define PA_W_FEW(DD, BB)                                                               \
+  {                                                                                    \
+    if (BB == 16 && rows > 32) PA_W(256, attn_weights_few_kernel<DD, 16, 4>);          \
+    else if (rows > 16) PA_W(256, attn_weights_few_kernel<DD, BB, 2>);                 \
+    else PA_W(256, attn_weights_few_kernel<DD, BB, 1>);                                \
+  }
+#define PA_W_BITS(M)                 \
+  if (d == 128 && bits == 16) M(128, 16) \
+  else if (d == 128) M(128, 4)       \
+  else if (bits == 16) M(64, 16)     \
+  else M(64, 4)
+  PA_W_BITS(PA_W_MANY)
+}
+
+int launch_attn_weights(const void* q, const float* lse, const void* kc, const uint8_t* scales,
+                        int32_t num_blocks, const int32_t* bt, int32_t max_blocks,
+                        const int32_t* seq_lens, const int32_t* cu, int32_t n_seqs, int32_t total_q,
+                        int32_t hq, int32_t hkv, int32_t d, int32_t bits, float scale, float* w,
+                        int64_t w_stride, bool add, hipStream_t stream) {
+  WeightArgs a{static_cast<const __bf16*>(q), lse, static_cast<const uint8_t*>(kc), scales, bt, seq_lens,
+               cu, w, w_stride, max_blocks, num_blocks, total_q, hq, hkv, 0, 0, 0, n_seqs, INT32_MAX, false, scale * kLog2e, add};
+  const int64_t heads = int64_t(n_seqs) * hkv, keys = min(w_stride, int64_t(max_blocks) * kBlock);
+  // Rows of a kv-head, of the average sequence.  32 sequences of 2048-8192 keys, 32/8 heads:
+  // bf16 16 rows 61 us (through LDS 94), 32 rows 67 (96), 64 rows 90 (103), 4 bits 30 (48), 42
+  // (49), 76 (59).
+  const int64_t rows = (int64_t(total_q) * (hq / hkv) + n_seqs - 1) / n_seqs;
+  const bool many = rows > (bits == 16 ? 64 : 32);
+  if (heads > INT32_MAX) return static_cast<int>(hipErrorInvalidValue);
+  if (many) {
+    launch_many(a, n_seqs, rows, n_seqs, keys, d, bits, stream);
+    return static_cast<int>(hipGetLastError());
+  }
+  // wavefronts of as many keys as leave enough of them to fill the chip
+  a.range = int32_t(max(int64_t(1), min(int64_t(32), keys * heads / (32 * kFewWaves)))) * 32;
+  const int64_t chunks = min((keys + 4 * a.range - 1) / (4 * a.range), max(int64_t(1), 32768 / heads));
+  a.chunks = int32_t(chunks);
+  // Prompts among requests of few rows: a launch of its own for sequences of more than `limit`
+  // rows, as many as there can be, unless all have the same number (us with one launch and
+  // two: 95 requests of 500-1500 keys, 32/8 heads of 64 dims on the 4-bit cache, and prompts of
+  // 512 and 100 tokens 166 and 46, 199 of 200-1000 and one of 1000 804 and 97, 64 of 2000-6000
+  // and one of 512 341 and 175).
+  const int64_t G = hq / hkv, limit = bits == 16 ? 128 : 64, longs = min(int64_t(n_seqs), total_q * G / (limit + 1));
+  const bool mixed = total_q % n_seqs != 0 && (int64_t(total_q) - n_seqs + 1) * G > limit;
+  if (mixed) a.limit = int32_t(limit);
+  const dim3 grid(unsigned(heads * chunks));
+  PA_W_BITS(PA_W_FEW)
+  if (mixed) {
+    a.longs = true;
+    const int64_t likely = min(longs, int64_t(2));
+    launch_many(a, longs, (int64_t(total_q) - n_seqs + 1) * G / likely, likely, keys, d, bits, stream);
   }
 #undef PA_W_BITS
-#undef PA_W_ROWS
+#undef PA_W_FEW
+#undef PA_W_MANY
 #undef PA_W
   return static_cast<int>(hipGetLastError());
 }

@@ -108,6 +108,11 @@ WEIGHTS = {
     # few sequences: workgroups of 64 keys
     "some": (8, 4, 128, [90, 33, 140, 61, 100, 75], [700, 1033, 340, 61, 905, 500]),
     "some-64": (16, 8, 64, [40, 77, 120], [840, 1277, 620]),
+    # prompts among requests of few rows, one behind the first 64 sequences, and sequences
+    # without rows
+    "mixed": (8, 2, 128, [1] * 9 + [150, 0, 1, 40, 33, 32] + [1] * 3, [300 + 57 * i for i in range(18)]),
+    "mixed-64": (4, 1, 64, [1] * 70 + [200, 2, 0, 0, 17, 16, 90], [201 + 13 * i % 400 for i in range(77)]),
+    "mixed-prompts": (32, 8, 128, [1] * 41 + [300, 500, 77], [500 + 31 * i % 700 for i in range(44)]),
     # one sequence, more tiles of rows than a workgroup has wavefronts
     "long-prompt": (28, 4, 128, [301], [777]),
     "long-prompt-64": (64, 8, 64, [150], [150]),
