@@ -8,7 +8,9 @@
 // S = Q K^T on 32x32x16 MFMA with a key in each lane, so a lane adds its key's
 // probabilities over 16 rows without looking at other lanes; the two lane halves (other
 // rows) are added once at the end.  A workgroup owns its keys and goes over all rows of the
-// sequence: no atomics, one order of the sums, and keys are read once.
+// sequence: no atomics, one order of the sums, and keys are read once.  Three ways: many
+// rows that a workgroup's wavefronts share; many rows of few keys, which they divide; few
+// rows, which stay in registers.
 #include <type_traits>
 
 #include "device_common.h"
@@ -611,7 +613,8 @@ int launch_attn_weights(const void* q, const float* lse, const void* kc, const u
                         int32_t hq, int32_t hkv, int32_t d, int32_t bits, float scale, float* w,
                         int64_t w_stride, bool add, hipStream_t stream) {
   WeightArgs a{static_cast<const __bf16*>(q), lse, static_cast<const uint8_t*>(kc), scales, bt, seq_lens,
-               cu, w, w_stride, max_blocks, num_blocks, total_q, hq, hkv, 0, 0, 0, n_seqs, INT32_MAX, false, scale * kLog2e, add};
+               cu, w, w_stride, max_blocks, num_blocks, total_q, hq, hkv, 0, 0, 0, n_seqs, INT32_MAX, false,
+               scale * kLog2e, add};
   const int64_t heads = int64_t(n_seqs) * hkv, keys = min(w_stride, int64_t(max_blocks) * kBlock);
   // Rows of a kv-head, of the average sequence.  32 sequences of 2048-8192 keys, 32/8 heads:
   // bf16 16 rows 61 us (through LDS 94), 32 rows 67 (96), 64 rows 90 (103), 4 bits 30 (48), 42
