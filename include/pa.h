@@ -130,8 +130,24 @@ int pa_seq_truncate(pa_pool* pool, int64_t seq_id, int32_t new_len);
  * blocks hold is not a prefix of its tokens any more: none of them is cached when the
  * sequence is freed.  Tokens appended later continue at position new_len of the cache (their
  * rotation goes by the caller's own count).  1 <= new_len <= length, 0 <= first <= new_len.
+ * The blocks that the sequence gives back may be handed out by any later call on the pool,
+ * the next pa_seq_compact among them, while the eviction still has to read them: queue this
+ * sequence's pa_kv_evict before any device call that writes to blocks handed out after this
+ * one.  One pa_kv_evict for several sequences needs pa_seqs_compact.
  * Errors (pool unchanged): PA_ERR_UNKNOWN_SEQ, PA_ERR_ARG, PA_ERR_NO_BLOCKS. */
 int pa_seq_compact(pa_pool* pool, int64_t seq_id, int32_t new_len, int32_t first, int32_t in_place);
+
+/* The same for n sequences that one pa_kv_evict call shortens: sequence i to new_lens[i]
+ * tokens, of which the first first[i] (first NULL: none) stay as they are.  All new blocks
+ * are taken before any old one is released, so that no block of a new table from entry
+ * first[i] / block_size on is in any of the old tables.  A sequence of new_lens[i] tokens or
+ * fewer stays as it is, its blocks and what of them is cached included (pa_kv_evict keeps all
+ * of its tokens).  The other rules are those of pa_seq_compact; that pa_kv_evict call comes
+ * before any device call that writes to blocks handed out later.  The call is all or
+ * nothing.  Errors (pool unchanged): PA_ERR_UNKNOWN_SEQ, PA_ERR_ARG (also an id that appears
+ * twice), PA_ERR_NO_BLOCKS. */
+int pa_seqs_compact(pa_pool* pool, int32_t n, const int64_t* seq_ids, const int32_t* new_lens,
+                    const int32_t* first, int32_t in_place);
 
 /* Release a finished sequence.  Its full blocks are cached first (same rule as
  * at admission); cached blocks stay resident with no owner (idle) until
@@ -732,7 +748,10 @@ int pa_attn_weights(const void* q, const float* lse, const void* k_cache, const 
  * be the same in both, and once in new_table.  With new_table NULL, or block_table itself,
  * the tokens move within the sequence's own blocks, which from F / 16 on must be in that
  * sequence's table only; fewer workgroups share that work, since a block is written only
- * once all that it held has been read.  pa_seq_compact gives the pool's side of both.
+ * once all that it held has been read.  A sequence of which all tokens stay (B = L) may have
+ * its blocks, shared ones too, in both tables, and moves none in place: such blocks are not
+ * touched.  pa_seqs_compact gives the pool's side of a call, pa_seq_compact that of a call
+ * for one sequence.
  * Tokens whose block id (old or new) is outside [0, num_blocks) are read from a clamped
  * block, or not written.
  *

@@ -36,7 +36,9 @@ the design notes:
 * compaction (chosen tokens of a sequence stay, its first ``first`` as they are) either
   gives it new blocks behind the full ones of those, its hold on the old ones ending as at
   release, or (in place) keeps its leading blocks, of which none registered may change.
-  Its blocks are not registered any more.
+  Its blocks are not registered any more.  Several sequences are compacted together, all or
+  none: every new block is taken before any old one is released, and a sequence that is no
+  longer than its new length stays as it is.
 """
 from __future__ import annotations
 
@@ -233,6 +235,41 @@ class PrefixCacheOracle:
             st["n_reg"] = min(st["n_reg"], stay)
         del st["tokens"][new_len:]
         st["compacted"] = True
+
+    def compact_many(self, seq_ids, new_lens, first, in_place: bool):
+        todo, need, seen = [], 0, set()
+        for sid, new_len, front in zip(seq_ids, new_lens, first):
+            st = self._seq(sid)
+            if sid in seen:
+                raise ArgError("a sequence appears twice in one batch")
+            seen.add(sid)
+            if not (new_len >= 1 and 0 <= front <= new_len):
+                raise ArgError(f"cannot compact to {new_len} tokens, first {front}")
+            if new_len >= len(st["tokens"]):
+                continue
+            if in_place and front < st["n_reg"] * self.bs:
+                raise ArgError("registered blocks would change")
+            stay, total = (-(-new_len // self.bs) if in_place else front // self.bs), -(-new_len // self.bs)
+            todo.append((st, new_len, stay, total, st["blocks"][stay:]))
+            need += total - stay
+        if need > self._obtainable():
+            raise NoBlocksError(f"need {need} blocks")
+        for st, new_len, stay, total, old in todo:
+            new = [self._take() for _ in range(total - stay)]
+            for b in new:
+                self.ref[b] = 1
+            st["blocks"] = st["blocks"][:stay] + new
+            del st["tokens"][new_len:]
+            st["compacted"] = True
+            if not in_place:
+                st["n_reg"] = min(st["n_reg"], stay)
+        for _, _, _, _, old in todo:
+            if in_place:
+                for b in reversed(old):
+                    self.ref[b] -= 1
+                    self.free.appendleft(b)
+            else:
+                self._release(old)
 
     def seq_len(self, seq_id) -> int:
         return len(self._seq(seq_id)["tokens"])

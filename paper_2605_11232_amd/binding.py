@@ -35,7 +35,7 @@ EXPORTS = ["pa_last_error", "pa_abi_version", "pa_pool_create", "pa_pool_destroy
            "pa_kv8_attn_decode", "pa_kv8_attn_verify", "pa_kv8_attn_decode_noalloc",
            "pa_kv4_append", "pa_kv4_read", "pa_kv4_attn_prefill", "pa_kv4_attn_decode",
            "pa_kv4_attn_verify", "pa_kv4_attn_decode_noalloc",
-           "pa_seq_compact", "pa_attn_weights", "pa_kv_evict", "pa_qk_norm_rope",
+           "pa_seq_compact", "pa_seqs_compact", "pa_attn_weights", "pa_kv_evict", "pa_qk_norm_rope",
            "pa_set_launch_events"]
 
 
@@ -103,6 +103,7 @@ def lib():
         "pa_seqs_truncate": (C.c_int, [_P, i32, _I64P, _I32P, _I32P]),
         "pa_seqs_free": (C.c_int, [_P, i32, _I64P, _I32P]),
         "pa_seq_compact": (C.c_int, [_P, i64, i32, i32, i32]),
+        "pa_seqs_compact": (C.c_int, [_P, i32, _I64P, _I32P, _I32P, i32]),
         "pa_pool_apply": (C.c_int, [_P, i32, _P, _P, _P, _P, _P, _P, _P]),
         "pa_seq_len": (C.c_int, [_P, i64, _I32P]),
         "pa_seq_blocks": (C.c_int, [_P, i64, _I32P, i32, _I32P]),
@@ -296,8 +297,10 @@ class Pool:
         _check(self._lib.pa_seq_truncate(self._h, int(seq_id), int(new_len)))
 
     def compact(self, seq_id: int, new_len: int, first: int = 0, in_place: bool = False):
-        """The pool's side of kv_evict: the sequence holds new_len tokens, its first
-        ``first`` ones unchanged, in new blocks or (``in_place``) in its own."""
+        """The pool's side of a kv_evict of this sequence alone: it holds new_len tokens, its
+        first ``first`` ones unchanged, in new blocks or (``in_place``) in its own.  Calls
+        that follow may hand out the blocks that it gives back: one kv_evict for several
+        sequences needs compact_many."""
         _check(self._lib.pa_seq_compact(self._h, int(seq_id), int(new_len), int(first),
                                         int(bool(in_place))))
 
@@ -325,6 +328,17 @@ class Pool:
         nl = _i32(new_lens)
         _check(self._lib.pa_seqs_truncate(self._h, ids.size, ids.ctypes.data_as(_I64P), _ptr(nl),
                                           None))
+
+    def compact_many(self, seq_ids, new_lens, first=None, in_place: bool = False):
+        """The pool's side of one kv_evict for these sequences (first: an array, or None for
+        none): all of them or, where it raises, none; those of new_lens tokens or fewer stay
+        as they are."""
+        ids = np.ascontiguousarray(seq_ids, dtype=np.int64)
+        nl, fr = _i32(new_lens), None if first is None else _i32(first)
+        if nl.shape != ids.shape or (fr is not None and fr.shape != ids.shape):
+            raise ValueError("compact_many: arrays of inconsistent length")
+        _check(self._lib.pa_seqs_compact(self._h, ids.size, ids.ctypes.data_as(_I64P), _ptr(nl),
+                                         None if fr is None else _ptr(fr), int(bool(in_place))))
 
     def free_many(self, seq_ids):
         ids = np.ascontiguousarray(seq_ids, dtype=np.int64)

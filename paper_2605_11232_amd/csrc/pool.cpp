@@ -27,6 +27,7 @@
 #include <new>
 #include <set>
 #include <unordered_map>
+#include <unordered_set>
 #include <vector>
 
 #include "internal.h"
@@ -192,6 +193,83 @@ struct pa_pool {
   }
 };
 
+namespace {
+// Compaction of n sequences at once: everything is checked, then every new block is taken, and
+// only then old ones are released, so that no new table has a block of any old table behind
+// the part that stays (one eviction call reads all old tables while it writes the new ones).
+// `keep_short`: sequences of new_len tokens or fewer stay as they are; else longer new_lens
+// are refused.
+int compact(const char* fn, pa_pool* pool, int32_t n, const int64_t* seq_ids,
+            const int32_t* new_lens, const int32_t* first, bool in_place, bool keep_short) {
+  pa::clear_error();
+  if (!pool || n < 0 || (n > 0 && (!seq_ids || !new_lens)))
+    return pa::fail(PA_ERR_ARG, "%s: NULL argument or n < 0", fn);
+  struct Part {
+    pa_pool::Seq* s;
+    size_t new_len, stay, total;  // blocks that stay, and of the new table
+    std::vector<int32_t> old;
+  };
+  std::vector<Part> parts;
+  try {
+    parts.reserve(static_cast<size_t>(n));
+    std::unordered_set<int64_t> seen;
+    int64_t need = 0;
+    for (int32_t i = 0; i < n; ++i) {
+      auto it = pool->seqs.find(seq_ids[i]);
+      if (it == pool->seqs.end())
+        return pa::fail(PA_ERR_UNKNOWN_SEQ, "%s: unknown sequence %lld", fn, (long long)seq_ids[i]);
+      if (!seen.insert(seq_ids[i]).second)
+        return pa::fail(PA_ERR_ARG, "%s: sequence %lld appears twice", fn, (long long)seq_ids[i]);
+      pa_pool::Seq& s = it->second;
+      const int64_t L = static_cast<int64_t>(s.tokens.size());
+      const int32_t len = new_lens[i], front = first ? first[i] : 0;
+      if (len < 1 || (!keep_short && len > L) || front < 0 || front > len)
+        return pa::fail(PA_ERR_ARG, "%s: new_len %d outside [1, %lld], or first %d outside "
+                        "[0, new_len]", fn, len, (long long)L, front);
+      if (keep_short && len >= L) continue;
+      const int64_t cached_len = static_cast<int64_t>(s.n_cached_run) * pool->bs;
+      if (in_place && front < cached_len)
+        return pa::fail(PA_ERR_ARG, "%s: first %d, but the leading %lld tokens' blocks are cached",
+                        fn, front, (long long)cached_len);
+      Part p{&s, static_cast<size_t>(len), static_cast<size_t>(front / pool->bs),
+             static_cast<size_t>(pa_pool::cdiv(len, pool->bs)), {}};
+      if (!in_place) {
+        need += static_cast<int64_t>(p.total - p.stay);
+        p.old.assign(s.blocks.begin() + p.stay, s.blocks.end());
+      }
+      parts.push_back(std::move(p));
+    }
+    if (need > pool->obtainable(0))
+      return pa::fail(PA_ERR_NO_BLOCKS, "%s: need %lld blocks, %lld obtainable", fn,
+                      (long long)need, (long long)pool->obtainable(0));
+  } catch (const std::bad_alloc&) {
+    return pa::fail(PA_ERR_ARG, "%s: out of host memory", fn);
+  }
+  for (Part& p : parts) {
+    pa_pool::Seq& s = *p.s;
+    if (in_place) {
+      for (size_t j = s.blocks.size(); j-- > p.total;) {
+        --pool->ref[s.blocks[j]];
+        pool->free_list.push_front(s.blocks[j]);
+      }
+      s.blocks.resize(p.total);
+    } else {
+      // no more blocks than before: the vector does not grow
+      for (size_t j = p.stay; j < p.total; ++j) {
+        s.blocks[j] = pool->take();
+        pool->ref[s.blocks[j]] = 1;
+      }
+      s.blocks.resize(p.total);
+      s.n_cached_run = std::min(s.n_cached_run, static_cast<int32_t>(p.stay));
+    }
+    s.tokens.resize(p.new_len);
+    s.compacted = true;
+  }
+  for (const Part& p : parts) pool->release(p.old);
+  return PA_OK;
+}
+}  // namespace
+
 namespace pa {
 int32_t pool_block_size(const pa_pool* pool) { return pool->bs; }
 }  // namespace pa
@@ -325,52 +403,12 @@ int pa_seq_truncate(pa_pool* pool, int64_t seq_id, int32_t new_len) {
 }
 
 int pa_seq_compact(pa_pool* pool, int64_t seq_id, int32_t new_len, int32_t first, int32_t in_place) {
-  pa::clear_error();
-  if (!pool) return pa::fail(PA_ERR_ARG, "pa_seq_compact: NULL pool");
-  auto it = pool->seqs.find(seq_id);
-  if (it == pool->seqs.end())
-    return pa::fail(PA_ERR_UNKNOWN_SEQ, "pa_seq_compact: unknown sequence %lld", (long long)seq_id);
-  pa_pool::Seq& s = it->second;
-  const int64_t L = static_cast<int64_t>(s.tokens.size());
-  if (new_len < 1 || new_len > L || first < 0 || first > new_len)
-    return pa::fail(PA_ERR_ARG, "pa_seq_compact: new_len %d outside [1, %lld], or first %d outside "
-                    "[0, new_len]", new_len, (long long)L, first);
-  const size_t total = static_cast<size_t>(pa_pool::cdiv(new_len, pool->bs));
-  if (in_place) {
-    const int64_t cached_len = static_cast<int64_t>(s.n_cached_run) * pool->bs;
-    if (first < cached_len)
-      return pa::fail(PA_ERR_ARG, "pa_seq_compact: first %d, but the leading %lld tokens' blocks are "
-                      "cached", first, (long long)cached_len);
-    for (size_t j = s.blocks.size(); j-- > total;) {
-      --pool->ref[s.blocks[j]];
-      pool->free_list.push_front(s.blocks[j]);
-    }
-    s.blocks.resize(total);
-  } else {
-    const size_t stay = static_cast<size_t>(first / pool->bs);
-    const int64_t need = static_cast<int64_t>(total - stay);
-    if (need > pool->obtainable(0))
-      return pa::fail(PA_ERR_NO_BLOCKS, "pa_seq_compact: need %lld blocks, %lld obtainable",
-                      (long long)need, (long long)pool->obtainable(0));
-    std::vector<int32_t> old;
-    try {
-      old.assign(s.blocks.begin() + stay, s.blocks.end());
-      s.blocks.reserve(total);
-    } catch (const std::bad_alloc&) {
-      return pa::fail(PA_ERR_ARG, "pa_seq_compact: out of host memory");
-    }
-    s.blocks.resize(stay);
-    for (int64_t i = 0; i < need; ++i) {
-      const int32_t b = pool->take();
-      pool->ref[b] = 1;
-      s.blocks.push_back(b);
-    }
-    pool->release(old);
-    s.n_cached_run = std::min(s.n_cached_run, static_cast<int32_t>(stay));
-  }
-  s.tokens.resize(static_cast<size_t>(new_len));
-  s.compacted = true;
-  return PA_OK;
+  return compact("pa_seq_compact", pool, 1, &seq_id, &new_len, &first, in_place != 0, false);
+}
+
+int pa_seqs_compact(pa_pool* pool, int32_t n, const int64_t* seq_ids, const int32_t* new_lens,
+                    const int32_t* first, int32_t in_place) {
+  return compact("pa_seqs_compact", pool, n, seq_ids, new_lens, first, in_place != 0, true);
 }
 
 int pa_seq_free(pa_pool* pool, int64_t seq_id) {
