@@ -1019,7 +1019,7 @@ def kv_evict(weights, block_table, seq_lens, new_lens, k_cache, v_cache, kept, s
             and all(x.dtype == i32 and x.numel() == n and x.is_contiguous()
                     and x.get_device() == dev for x in lists)
             and all(x.dtype == i32 and x.dim() == 2 and x.shape[0] >= n and x.is_contiguous()
-                    and x.get_device() == dev for x in tables)
+                    and x.get_device() == dev and (x.shape[1] > 0 or n == 0) for x in tables)
             and st >= 0 and v_cache.get_device() == weights.get_device()
             == weights_out.get_device() == kept.get_device() == dev):
         _refuse(PA_ERR_UNSUPPORTED, [
@@ -1039,8 +1039,10 @@ def kv_evict(weights, block_table, seq_lens, new_lens, k_cache, v_cache, kept, s
             (spare(kept, i32), f"kept must be contiguous int32 [{n}, {hkv}, longest new length]"),
             (all(x.dtype == i32 and x.numel() == n and x.is_contiguous() for x in lists),
              f"seq_lens, new_lens and first must be contiguous int32 of {n} sequences"),
+            # a table of no blocks has no address, which would mean a move in place
             (all(x.dtype == i32 and x.dim() == 2 and x.shape[0] >= n and x.is_contiguous()
-                 for x in tables), f"tables must be contiguous int32 [{n}, blocks]")])
+                 and (x.shape[1] > 0 or n == 0) for x in tables),
+             f"tables must be contiguous int32 [{n}, 1 block or more]")])
         _refuse_device(k_cache, v_cache, scales, weights, weights_out, kept, *lists, *tables)
     rc = fn(weights.data_ptr(), weights_out.data_ptr(), weights.shape[2], block_table.data_ptr(),
             block_table.shape[1], _dptr(new_table), 0 if new_table is None else new_table.shape[1],

@@ -183,3 +183,16 @@ def test_against_the_oracle(seed, evict):
     for x in live:
         pool.free(x), orc.free_seq(x)
     assert pool.free_list() == orc.free_list() and pool.stats() == orc.stats()
+
+
+def test_eviction_refuses_tables_of_no_blocks():
+    """An empty tensor has no address; an eviction to it is not one in place."""
+    import torch
+    k = torch.zeros((4, 2, 4, 16, 32), dtype=torch.bfloat16)
+    v = torch.zeros((4, 2, 128, 16), dtype=torch.bfloat16)
+    bt, sl, nl = (torch.zeros(s, dtype=torch.int32) for s in ((1, 2), 1, 1))
+    w, kept = torch.zeros((1, 2, 20)), torch.zeros((1, 2, 9), dtype=torch.int32)
+    for tables in ((bt, torch.zeros((1, 0), dtype=torch.int32)), (bt[:, :0].contiguous(), None)):
+        with pytest.raises(B.PaError) as e:
+            B.kv_evict(w, tables[0], sl, nl, k, v, kept, new_table=tables[1])
+        assert e.value.code == "arg" and "tables" in str(e.value)
