@@ -760,8 +760,10 @@ int pa_attn_weights(const void* q, const float* lse, const void* k_cache, const 
  * them with pa_kv8_read, pick rows, append them.)  All pointers are caller-owned device
  * memory; asynchronous on stream; allocates nothing.  Errors: PA_ERR_ARG (NULL pointer with
  * work to do, negative size, caches not 16-byte, weights or kept not 4-byte aligned, weights
- * and weights_out that overlap in part, tables that are one with two widths), PA_ERR_UNSUPPORTED (head_dim, block_size, dtype),
- * PA_ERR_LAUNCH. */
+ * and weights_out that overlap in part, tables that are one with two widths),
+ * PA_ERR_UNSUPPORTED (head_dim, block_size, dtype), PA_ERR_LAUNCH (also, with nothing done,
+ * for arrays so large that a launch would take 2^32 work-items: for each sequence and kv-head
+ * 1024, and 4 for each token of the smaller of kept_stride and the new table). */
 int pa_kv_evict(const float* weights, float* weights_out, int64_t weights_stride,
                 const int32_t* block_table, int32_t max_blocks_per_seq, const int32_t* new_table,
                 int32_t new_max_blocks, const int32_t* seq_lens, const int32_t* new_lens,

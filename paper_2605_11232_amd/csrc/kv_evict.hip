@@ -378,9 +378,13 @@ int launch_kv_evict(const float* w, float* w_out, int64_t w_stride, const int32_
   const int64_t heads = int64_t(n_seqs) * hkv;
   const int64_t blocks = min((kept_stride + kBlock - 1) / kBlock, int64_t(max_new));
   const int64_t groups = (blocks + 3) / 4;
-  if (heads * max(groups, int64_t(4)) > INT32_MAX) return static_cast<int>(hipErrorInvalidValue);
+  const bool narrow = w_stride <= 16 * 256;
+  // A launch has fewer than 2^32 work-items.  Both launches' are looked at before the first: the
+  // selection may write the new weights over the old ones, and a move would then not follow.
+  const int64_t threads = max(int64_t(narrow ? 256 : 1024), in_place ? int64_t(1024) : 256 * groups);
+  if (heads > UINT32_MAX / threads) return static_cast<int>(hipErrorInvalidValue);
   a.groups = int32_t(groups);
-  if (w_stride <= 16 * 256)
+  if (narrow)
     hipLaunchKernelGGL(evict_select_kernel<256>, dim3(unsigned(heads)), dim3(256), 0, stream, a);
   else
     hipLaunchKernelGGL(evict_select_kernel<1024>, dim3(unsigned(heads)), dim3(1024), 0, stream, a);

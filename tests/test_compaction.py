@@ -196,3 +196,15 @@ def test_eviction_refuses_tables_of_no_blocks():
         with pytest.raises(B.PaError) as e:
             B.kv_evict(w, tables[0], sl, nl, k, v, kept, new_table=tables[1])
         assert e.value.code == "arg" and "tables" in str(e.value)
+
+
+@pytest.mark.parametrize("n, kept, blocks, w_stride, in_place", [
+    (4096, 1 << 15, 2048, 4096, False), (4096, 1 << 20, 2048, 4096, False), (4096, 1 << 15, 4096, 4096, False),
+    (1 << 19, 40, 3, 5000, False), (1 << 19, 40, 3, 100, True), (2**31 - 1, 2**62, 2**31 - 1, 1, False)])
+def test_evictions_of_too_many_work_items_launch_nothing(n, kept, blocks, w_stride, in_place):
+    """2^32 work-items or more in either launch, 4096 sequences of 8 kv-heads whose move would
+    take four for each of 32768 tokens: refused before the selection changes the weights."""
+    fn, lib = B.lib().pa_kv_evict, B.lib()
+    assert fn(1 << 40, 1 << 40, w_stride, 64, 1 << 20, None if in_place else 128, blocks, 64, 64, None, 2,
+              n, 1024, 2048, None, 16, 8, 128, 16, B.PA_BF16, 64, kept, None) == B.PA_ERR_LAUNCH
+    assert b"invalid argument" in lib.pa_last_error(), lib.pa_last_error()
