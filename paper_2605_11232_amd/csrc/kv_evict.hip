@@ -344,17 +344,16 @@ __global__ __launch_bounds__(IN_PLACE ? 1024 : 256) void evict_move_kernel(Evict
   const int blocks = (n.keep + kBlock - 1) / kBlock;
   // Where all tokens stay, blocks that are in both tables hold what they have to already, and
   // may be other sequences' too: they are not written.
-  const bool all = n.keep == n.len;
-  if (IN_PLACE && all) return;
+  if (IN_PLACE && n.keep == n.len) return;
   const int first = n.front / kBlock + (IN_PLACE ? 0 : (blockIdx.x - x * a.groups) * kWaves);
   for (int b0 = first; b0 < (IN_PLACE ? blocks : min(blocks, first + kWaves)); b0 += kWaves) {
     const int b = b0 + wv, count = min(kBlock, n.keep - b * kBlock);
+    if (!IN_PLACE && n.keep == n.len && count > 0 && to[b] == bt[b]) continue;
     Moved<D, ELEM, NS> m;
     int id = -1;
     if (count > 0) {
       m.load(a, g, s0, kept[b * kBlock + min(lane % kBlock, count - 1)], bt, lane);
       id = to[b];
-      if (!IN_PLACE && all && id == bt[b]) id = -1;
     }
     if constexpr (IN_PLACE) {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
