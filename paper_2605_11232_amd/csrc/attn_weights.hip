@@ -631,10 +631,20 @@ int launch_attn_weights(const void* q, const float* lse, const void* kc, const u
   const int64_t chunks = min((keys + 4 * a.range - 1) / (4 * a.range), max(int64_t(1), 32768 / heads));
   a.chunks = int32_t(chunks);
   // Prompts among requests of few rows: a launch of its own for sequences of more than `limit`
-  // rows, as many as there can be, unless all have the same number (us with one launch and
-  // two: 95 requests of 500-1500 keys, 32/8 heads of 64 dims on the 4-bit cache, and prompts of
-  // 512 and 100 tokens 166 and 46, 199 of 200-1000 and one of 1000 804 and 97, 64 of 2000-6000
-  // and one of 512 341 and 175).
+  // rows, as many as there can be (us with one launch and two: 95 requests of 500-1500 keys,
+  // 32/8 heads of 64 dims on the 4-bit cache, and prompts of 512 and 100 tokens 166 and 46, 199
+  // of 200-1000 and one of 1000 804 and 97, 64 of 2000-6000 and one of 512 341 and 175; the
+  // other way, 186 of 500-1500 4-bit keys and 8 of 150 tokens 129 and 176).  The host does not
+  // have the lengths: a total that divides by the sequences is taken for the same number of rows
+  // in each, and each sequence for one of a row or more.  Where that is not so the prompts stay
+  // with the others, in one launch, to the same formula in more time.
+  // The limit, one prompt among 96 requests of 500-1500 keys, 32/8 heads of 128, one launch and
+  // two: bf16 80 rows a kv-head 39 and 45, 112 41 and 46, 160 48 and 47, 288 71 and 51, 4 bits
+  // 48 rows 22.7 and 27.8, 80 22.8 and 28.9, 160 32 and 31; among 64 of 2000-6000: bf16 160
+  // 133 and 108, 4 bits 80 43 and 46, 112 53 and 47.
+  // Prompts reckoned with, 1, 2 and 4: two of 300 tokens among 128 requests of 2000-6000 bf16
+  // keys 344, 261 and 261, four among 190 of 500-1500 166, 166 and 137, one of 136 among 96 of
+  // these 49, 48 and 60.
   const int64_t G = hq / hkv, limit = bits == 16 ? 128 : 64, longs = min(int64_t(n_seqs), total_q * G / (limit + 1));
   const bool mixed = total_q % n_seqs != 0 && (int64_t(total_q) - n_seqs + 1) * G > limit;
   if (mixed) a.limit = int32_t(limit);

@@ -60,11 +60,12 @@ constexpr int kHeld = 16;  // weights of a thread that stay in registers
 
 // NT threads (256 where rows of weights are short: its barriers are cheaper).  A wavefront
 // takes an even share of the positions, 64 at a time; up to 16 NT of them are read once, all
-// loads issued together, further ones in each pass again, as many at a time.  Bound by the passes' barriers and
-// LDS atomics, not by bytes (8 kv-heads of 16 contexts of 6000-16000 tokens 18 us, 33 with the
-// weights read in each pass; of 64 contexts of 1000-2000, with 256 threads, 12, 15; an eviction
-// from one 4-bit context of 45000 tokens 61, 72 with the further ones read one by one, 67 with
-// 32 NT held, which costs one of 6000 17 -> 21).
+// loads issued together, further ones in each pass again, as many at a time.  Bound by its
+// passes one after the other (atomics on LDS, the scan of 2048 counts, barriers), not by bytes:
+// 8 kv-heads of 16 contexts of 6000-16000 tokens 18 us for 8.6 MB, 33 with the weights read in
+// each pass; of 64 contexts of 1000-2000, with 256 threads, 12, 15; an eviction from one 4-bit
+// context of 45000 tokens 61, 72 with the further ones read one by one, 67 with 32 NT held,
+// which costs one of 6000 17 -> 21.
 template <int NT>
 __global__ __launch_bounds__(NT) void evict_select_kernel(EvictArgs a) {
   constexpr int kWaves = NT / 64, kBinsPer = 2048 / NT;
