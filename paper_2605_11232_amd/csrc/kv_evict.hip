@@ -324,7 +324,7 @@ struct Moved {
 
 // To other blocks: one workgroup per four blocks; bound by the caches' lines, of which values
 // are read whole, since a dim's 16 tokens lie together (16 contexts of 6000-16000 bf16 tokens
-// to a quarter: 528 MB read, 177 written, 150 us, 4.7 TB/s).  In place: one per (sequence, kv-head),
+// to a quarter: 520 MB read, 176 written, 150 us, 4.6 TB/s).  In place: one per (sequence, kv-head),
 // which takes 16 blocks at a time, or, SLICED, per slice of it: slices do not wait for each
 // other.  Sliced is faster while the workgroups do not fill the chip (one context of 16000
 // tokens to a quarter, 8 kv-heads, 300 -> 107 us, 16 of 11000 tokens 325 -> 201), and slower
