@@ -138,11 +138,11 @@ int pa_seq_truncate(pa_pool* pool, int64_t seq_id, int32_t new_len);
 int pa_seq_compact(pa_pool* pool, int64_t seq_id, int32_t new_len, int32_t first, int32_t in_place);
 
 /* The same for n sequences that one pa_kv_evict call shortens: sequence i to new_lens[i]
- * tokens, of which the first first[i] (first NULL: none) stay as they are.  All new blocks
- * are taken before any old one is released, so that no block of a new table from entry
- * first[i] / block_size on is in any of the old tables.  A sequence of new_lens[i] tokens or
- * fewer stays as it is, its blocks and what of them is cached included (pa_kv_evict keeps all
- * of its tokens).  The other rules are those of pa_seq_compact; that pa_kv_evict call comes
+ * tokens, of which the first first[i] (first NULL: none) stay as they are.  With in_place =
+ * 0 all new blocks are taken before any old one is released, so that a shortened sequence's
+ * new table has, from entry first[i] / block_size on, no block of any old table.  A sequence
+ * of new_lens[i] tokens or fewer stays as it is, its blocks and what of them is cached
+ * included (pa_kv_evict keeps all of its tokens).  The other rules are those of pa_seq_compact; that pa_kv_evict call comes
  * before any device call that writes to blocks handed out later.  The call is all or
  * nothing.  Errors (pool unchanged): PA_ERR_UNKNOWN_SEQ, PA_ERR_ARG (also an id that appears
  * twice), PA_ERR_NO_BLOCKS. */
