@@ -142,10 +142,10 @@ int pa_seq_compact(pa_pool* pool, int64_t seq_id, int32_t new_len, int32_t first
  * 0 all new blocks are taken before any old one is released, so that a shortened sequence's
  * new table has, from entry first[i] / block_size on, no block of any old table.  A sequence
  * of new_lens[i] tokens or fewer stays as it is, its blocks and what of them is cached
- * included (pa_kv_evict keeps all of its tokens).  The other rules are those of pa_seq_compact; that pa_kv_evict call comes
- * before any device call that writes to blocks handed out later.  The call is all or
- * nothing.  Errors (pool unchanged): PA_ERR_UNKNOWN_SEQ, PA_ERR_ARG (also an id that appears
- * twice), PA_ERR_NO_BLOCKS. */
+ * included (pa_kv_evict keeps all of its tokens).  The other rules are those of
+ * pa_seq_compact; that pa_kv_evict call comes before any device call that writes to blocks
+ * handed out later.  The call is all or nothing.  Errors (pool unchanged):
+ * PA_ERR_UNKNOWN_SEQ, PA_ERR_ARG (also an id that appears twice), PA_ERR_NO_BLOCKS. */
 int pa_seqs_compact(pa_pool* pool, int32_t n, const int64_t* seq_ids, const int32_t* new_lens,
                     const int32_t* first, int32_t in_place);
 
